@@ -7,6 +7,8 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -14,15 +16,14 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libnoble.so")
 BINDING = os.path.join(PKG, "_noble_torch.so")
-SOURCES = ["noble_api.hip"]
-HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_binding.h", "noble_torch.cpp"]
+SOURCES = ["noble_api.hip", "noble_attn.hip"]
+HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_binding.h", "noble_torch.cpp"]
 
 HIP_FLAGS = [
     "-O3",
     "-std=c++20",
     "--offload-arch=gfx950",
     "-fPIC",
-    "-shared",
     "-munsafe-fp-atomics",
     # no packed-FP32 instructions in device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -37,16 +38,24 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build libnoble)")
 
 
-def build(verbose: bool = False) -> str:
-    """Compile libnoble.so; always recompiles.  Returns the library path."""
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
+def _hipcc(args, verbose: bool) -> None:
+    cmd = [hipcc(), *HIP_FLAGS, *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+
+
+def build(verbose: bool = False) -> str:
+    """Compile libnoble.so; always recompiles.  Returns the library path."""
+    tmp = LIB + ".tmp"
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor() as pool:
+        objs = [os.path.join(d, s + ".o") for s in SOURCES]
+        # the sources side by side, then one link
+        list(pool.map(lambda so: _hipcc(["-c", "-I", INCLUDE, "-I", CSRC, os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
+                      zip(SOURCES, objs)))
+        _hipcc(["-shared", *objs, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     build_binding(verbose)
     return LIB

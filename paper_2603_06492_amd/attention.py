@@ -1,0 +1,389 @@
+"""Python binding of libnoble's attention side (include/noble_attn.h): the operators between the grouped Q/K/V layer and
+the O layer of a transformer block.
+
+The functions keep the C names and take torch tensors: ``noble_qk_rope_fwd`` / ``_bwd``, ``noble_kv_append``,
+``noble_attn_fwd`` / ``_bwd``, ``noble_attn_paged``, ``noble_rope_table``, ``noble_mask_rows``.  They check their
+arguments, allocate the outputs that are not given and the scratch, and enqueue on ``stream`` (default: torch's current
+stream).  ``QKRope``, ``Attention`` and ``RopeAttention`` are the ``torch.autograd.Function`` forms, ``PagedCache``
+keeps the pages of a batch of sequences, and ``NobleSelfAttention`` is the block's attention from x to the O layer's
+output, for training, prompts and single tokens.
+
+There is no fallback: without the built library or a gfx950 device, calls raise.
+"""
+
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from . import noble
+from .noble import NobleError, _dtype_code, _on, _stream
+
+_vp = ctypes.c_void_p
+_i64, _i32 = ctypes.c_int64, ctypes.c_int32
+_f32, _f64 = ctypes.c_float, ctypes.c_double
+
+SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class noble_heads(ctypes.Structure):
+    _fields_ = [("data", _vp), ("row", _i64), ("head", _i64)]
+
+
+class noble_rope_desc(ctypes.Structure):
+    _fields_ = [("T", _i64), ("x_row", _i64), ("table_rows", _i64), ("heads", _i32), ("kv_heads", _i32),
+                ("head_dim", _i32), ("rot", _i32), ("interleaved", _i32), ("dtype", _i32), ("eps", _f32),
+                ("reserved", _i32)]
+
+
+class noble_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", _i32), ("reserved", _i32), ("base", _f64), ("factor", _f64), ("trained", _f64),
+                ("fast", _f64), ("slow", _f64), ("gain", _f64)]
+
+
+class noble_cache_desc(ctypes.Structure):
+    _fields_ = [("pages", _i64), ("page", _i32), ("reserved", _i32)]
+
+
+class noble_attn_desc(ctypes.Structure):
+    _fields_ = [("Tq", _i64), ("Tk", _i64), ("offset", _i64), ("heads", _i32), ("kv_heads", _i32),
+                ("head_dim", _i32), ("dtype", _i32), ("causal", _i32), ("scale", _f32), ("softcap", _f32),
+                ("reserved", _i32)]
+
+
+class noble_paged_desc(ctypes.Structure):
+    _fields_ = [("B", _i64), ("table_row", _i64), ("pages", _i64), ("page", _i32), ("new_tokens", _i32),
+                ("window", _i32), ("heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("dtype", _i32),
+                ("scale", _f32), ("softcap", _f32), ("reserved", _i32)]
+
+
+_P = ctypes.POINTER
+_hp = _P(noble_heads)
+_sz = ctypes.c_size_t
+_SIGNATURES = {
+    "noble_qk_rope_fwd": [_P(noble_rope_desc)] + [_vp] * 9,
+    "noble_qk_rope_scratch_size": [_P(noble_rope_desc), _P(_sz)],
+    "noble_qk_rope_bwd": [_P(noble_rope_desc)] + [_vp] * 12 + [_sz, _vp],
+    "noble_kv_append": [_P(noble_rope_desc), _P(noble_cache_desc)] + [_vp] * 10,
+    "noble_rope_table": [_P(noble_rope_scaling), _i64, _i32, _vp, _vp, _vp],
+    "noble_attn_scratch_size": [_P(noble_attn_desc), _P(_sz), _P(_sz)],
+    "noble_attn_fwd": [_P(noble_attn_desc), _hp, _hp, _hp, _vp, _vp, _vp, _hp, _vp, _vp, _sz, _vp],
+    "noble_attn_bwd": [_P(noble_attn_desc), _hp, _hp, _hp, _hp, _hp, _vp, _vp, _vp, _vp, _hp, _hp, _hp, _vp, _sz, _vp],
+    "noble_attn_paged_scratch_size": [_P(noble_paged_desc), _P(_sz)],
+    "noble_attn_paged": [_P(noble_paged_desc), _hp, _vp, _vp, _vp, _vp, _hp, _vp, _sz, _vp],
+    "noble_mask_rows": [_i64, _i64, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp],
+}
+_ready = False
+
+
+def lib() -> ctypes.CDLL:
+    """The loaded libnoble.so with these functions' signatures (raises if it has not been built)."""
+    global _ready
+    L = noble.lib()
+    if not _ready:
+        for name, args in _SIGNATURES.items():
+            f = getattr(L, name)
+            f.restype, f.argtypes = ctypes.c_int, args
+        _ready = True
+    return L
+
+
+def _call(name, *args) -> None:
+    st = getattr(lib(), name)(*args)
+    if st != 0:
+        raise NobleError(st, name)
+
+
+# ----------------------------------------------------------------- tensors --
+
+def _tensor(t, name, dtype, shape, device):
+    """Checks a dense tensor and returns its address."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the call runs on {device}: all tensors must share one device")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr() or None
+
+
+def _heads(t, name, dtype, device, shape=None) -> noble_heads:
+    """Checks a [rows, heads, D] tensor whose elements of a head are adjacent; any row and head strides."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the call runs on {device}: all tensors must share one device")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [rows, heads, head_dim], got {tuple(t.shape)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must have adjacent elements along head_dim, got strides {t.stride()}")
+    return noble_heads(t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _rows(x, name, cols) -> int:
+    """Row stride of a [T, cols] tensor with adjacent columns."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU (got {x.device})")
+    if x.dim() != 2 or (cols is not None and x.shape[1] != cols):
+        raise ValueError(f"{name} must be [tokens, {cols}], got {tuple(x.shape)}")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name} must have adjacent columns, got strides {x.stride()}")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _gpu(t, name) -> torch.device:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU (got {t.device})")
+    return t.device
+
+
+def _used_on(stream, *tensors) -> None:
+    """Tensors allocated here for a call on another stream than the current one: kept until that stream is past it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _scratch(n, device, stream):
+    s = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    _used_on(stream, s)
+    return s
+
+
+# ------------------------------------------------------- norm and rotation --
+
+def noble_rope_table(length: int, rot: int, *, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                     trained: float = 0.0, fast: float = 32.0, slow: float = 1.0, gain: float = 1.0, device="cuda",
+                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """cos and sin, float32 [length, rot / 2], of the positions 0 .. length - 1.  ``scaling`` for contexts longer than
+    the trained ones: "linear" (positions / factor), "base" (a larger base), "ramp" (the slow frequencies / factor,
+    the fast ones kept; needs ``trained``)."""
+    if scaling not in SCALINGS:
+        raise ValueError(f"unknown scaling {scaling!r}; expected one of {sorted(SCALINGS)}")
+    dev = torch.empty(0, device=device).device
+    if dev.type != "cuda":
+        raise ValueError(f"the tables live on the GPU (got {dev})")
+    cos, sin = (torch.empty((max(length, 0), max(rot, 0) // 2), device=dev) for _ in range(2))
+    s = noble_rope_scaling(SCALINGS[scaling], 0, base, factor, trained, fast, slow, gain)
+    with _on(dev):
+        _call("noble_rope_table", ctypes.byref(s), length, rot, cos.data_ptr() or None, sin.data_ptr() or None,
+              _stream(stream, dev))
+    _used_on(stream, cos, sin)
+    return cos, sin
+
+
+def _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved):
+    """The descriptor and the addresses of x, the weights, the tables and the positions."""
+    dev = _gpu(qkv, "qkv")
+    groups = heads + 2 * kv_heads
+    if qkv.dim() != 2 or groups < 1 or qkv.shape[1] % groups:
+        raise ValueError(f"qkv must be [tokens, (heads + 2 kv_heads) head_dim], got {tuple(qkv.shape)} for {heads} and "
+                         f"{kv_heads} heads")
+    T, D = qkv.shape[0], qkv.shape[1] // groups
+    x_row = _rows(qkv, "qkv", None)
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin must be given together")
+    if (q_weight is None) != (k_weight is None):
+        raise ValueError("q_weight and k_weight must be given together")
+    rows, half = (0, 0) if cos is None else cos.shape if cos.dim() == 2 else (None, None)
+    if rows is None:
+        raise ValueError(f"cos must be [positions, rot / 2], got {tuple(cos.shape)}")
+    f32 = torch.float32
+    d = noble_rope_desc(T, x_row, rows, heads, kv_heads, D, 2 * half, int(interleaved), _dtype_code(qkv), eps, 0)
+    return dev, d, [qkv.data_ptr() or None, _tensor(q_weight, "q_weight", f32, (D,), dev),
+                    _tensor(k_weight, "k_weight", f32, (D,), dev), _tensor(cos, "cos", f32, None, dev),
+                    _tensor(sin, "sin", f32, None if cos is None else tuple(cos.shape), dev),
+                    _tensor(positions, "positions", torch.int32, (T,), dev)]
+
+
+def noble_qk_rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, *, heads: int, kv_heads: int, eps: float = 1e-6,
+                      interleaved: bool = False, q=None, k=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """q [T, heads, D] and k [T, kv_heads, D] from the Q/K/V layer's rows [T, (heads + 2 kv_heads) D]: each head normed
+    (weights float32 [D]; None: not) and its first 2 cos.shape[1] elements rotated by the token's position (int32 [T],
+    None: the row's number; cos None: not)."""
+    dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
+    T, D = d.T, d.head_dim
+    q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
+    k = torch.empty((T, kv_heads, D), dtype=qkv.dtype, device=dev) if k is None else k
+    out = [_tensor(q, "q", qkv.dtype, (T, heads, D), dev), _tensor(k, "k", qkv.dtype, (T, kv_heads, D), dev)]
+    with _on(dev):
+        _call("noble_qk_rope_fwd", ctypes.byref(d), *args, *out, _stream(stream, dev))
+    _used_on(stream, q, k)
+    return q, k
+
+
+def noble_qk_rope_bwd(dq, dk, qkv, q_weight, k_weight, cos, sin, positions, *, heads: int, kv_heads: int,
+                      eps: float = 1e-6, interleaved: bool = False, dqkv=None, stream=None):
+    """(dqkv, dq_weight, dk_weight): the query and key columns of dqkv are written, the value columns left as they are
+    (zeros in a tensor allocated here).  The weights' gradients are None without weights."""
+    dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
+    T, D = d.T, d.head_dim
+    grads = [_tensor(dq, "dq", qkv.dtype, (T, heads, D), dev), _tensor(dk, "dk", qkv.dtype, (T, kv_heads, D), dev)]
+    if dqkv is None:
+        dqkv = torch.zeros_like(qkv, memory_format=torch.contiguous_format)
+    if dqkv.device != dev or dqkv.dtype != qkv.dtype or dqkv.shape != qkv.shape:
+        raise ValueError("dqkv must have qkv's shape, dtype and device")
+    if T > 1 and _rows(dqkv, "dqkv", qkv.shape[1]) != d.x_row:
+        qkv = qkv.contiguous() if dqkv.is_contiguous() else qkv
+        if _rows(qkv, "qkv", None) != dqkv.stride(0):
+            raise ValueError("dqkv must have qkv's row stride, or be contiguous")
+        d.x_row, args[0] = dqkv.stride(0), qkv.data_ptr()
+    w = [None, None] if q_weight is None else [torch.empty(D, device=dev) for _ in range(2)]
+    n = _sz(0)
+    _call("noble_qk_rope_scratch_size", ctypes.byref(d), ctypes.byref(n))
+    scratch = _scratch(n.value if q_weight is not None else 0, dev, stream)
+    with _on(dev):
+        _call("noble_qk_rope_bwd", ctypes.byref(d), *grads, *args, dqkv.data_ptr() or None,
+              *[None if t is None else t.data_ptr() for t in w], scratch.data_ptr(), scratch.numel(),
+              _stream(stream, dev))
+    _used_on(stream, dqkv, *w)
+    return dqkv, w[0], w[1]
+
+
+def _cache_shape(cache, kv_heads, D, dtype, dev):
+    if not isinstance(cache, torch.Tensor) or cache.dim() != 5 or cache.shape[1] != 2:
+        raise ValueError("cache must be [pages, 2, kv_heads, page, head_dim]")
+    pages, _, _, page, _ = cache.shape
+    return pages, page, _tensor(cache, "cache", dtype, (pages, 2, kv_heads, page, D), dev)
+
+
+def noble_kv_append(qkv, q_weight, k_weight, cos, sin, positions, slots, cache, *, heads: int, kv_heads: int,
+                    eps: float = 1e-6, interleaved: bool = False, q=None, stream=None) -> torch.Tensor:
+    """Writes each row's keys, normed and rotated, and values to its slot (int64 [T], page number x page size + place;
+    outside the cache: not written) of cache [pages, 2, kv_heads, page, D], and returns the queries, normed and
+    rotated."""
+    dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
+    T, D = d.T, d.head_dim
+    pages, page, pc = _cache_shape(cache, kv_heads, D, qkv.dtype, dev)
+    q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
+    c = noble_cache_desc(pages, page, 0)
+    rest = [_tensor(slots, "slots", torch.int64, (T,), dev), _tensor(q, "q", qkv.dtype, (T, heads, D), dev), pc]
+    with _on(dev):
+        _call("noble_kv_append", ctypes.byref(d), ctypes.byref(c), *args, *rest, _stream(stream, dev))
+    _used_on(stream, q)
+    return q
+
+
+# --------------------------------------------------------------- attention --
+
+def noble_mask_rows(starts, T: int, *, prefix=None, causal: bool = True, window: int = 0, stream=None):
+    """(key_lo, key_hi, positions), int32 [T], of packed documents: document n holds the rows starts[n] .. starts[n + 1]
+    - 1 (int32 [documents + 1]).  A row sees its document up to itself (``causal``) or all of it, the document's first
+    prefix[n] rows in any case, and with a window only that many rows, the last ones."""
+    dev = _gpu(starts, "starts")
+    if starts.dim() != 1 or starts.shape[0] < 1:
+        raise ValueError("starts must be int32 [documents + 1]")
+    n = starts.shape[0] - 1
+    out = [torch.empty(max(T, 0), dtype=torch.int32, device=dev) for _ in range(3)]
+    with _on(dev):
+        _call("noble_mask_rows", T, n, _tensor(starts, "starts", torch.int32, (n + 1,), dev),
+              _tensor(prefix, "prefix", torch.int32, (n,), dev), int(causal), window,
+              *[t.data_ptr() or None for t in out], _stream(stream, dev))
+    _used_on(stream, *out)
+    return tuple(out)
+
+
+def _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap):
+    dev = _gpu(q, "q")
+    code, dt = _dtype_code(q), q.dtype
+    if q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("q, k and v must be [rows, heads, head_dim]")
+    (Tq, H, D), (Tk, K, _) = q.shape, k.shape
+    heads = [_heads(q, "q", dt, dev), _heads(k, "k", dt, dev, (Tk, K, D)), _heads(v, "v", dt, dev, (Tk, K, D))]
+    i32 = torch.int32
+    if (key_lo is None) != (key_hi is None):
+        raise ValueError("key_lo and key_hi must be given together")
+    mask = [_tensor(key_lo, "key_lo", i32, (Tq,), dev), _tensor(key_hi, "key_hi", i32, (Tq,), dev),
+            _tensor(slopes, "slopes", torch.float32, (H,), dev)]
+    d = noble_attn_desc(Tq, Tk, Tk - Tq if offset is None else offset, H, K, D, code, int(causal),
+                        D ** -0.5 if scale is None else scale, softcap, 0)
+    return dev, d, heads, mask
+
+
+def noble_attn_fwd(q, k, v, key_lo=None, key_hi=None, slopes=None, *, causal: bool = False, offset: Optional[int] = None,
+                   scale: Optional[float] = None, softcap: float = 0.0, o=None, lse=None, stream=None):
+    """(o, lse) of attention of q [Tq, heads, D] over k, v [Tk, kv_heads, D] (any row and head strides): row i sees the
+    keys [key_lo[i], key_hi[i]) (int32; None: all), with ``causal`` only those up to i + offset (default: the last row
+    sees the last key).  Scores are scale q.k (default D^-1/2), capped by softcap tanh(. / softcap) and lowered by
+    slopes[head] |i + offset - j|.  o: like q, dense; lse: float32 [heads, Tq]."""
+    dev, d, heads, mask = _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap)
+    shape = tuple(q.shape)
+    o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
+    lse = torch.empty(shape[1::-1], device=dev) if lse is None else lse
+    n = _sz(0)
+    _call("noble_attn_scratch_size", ctypes.byref(d), ctypes.byref(n), None)
+    scratch = _scratch(n.value, dev, stream) if n.value else None
+    with _on(dev):
+        _call("noble_attn_fwd", ctypes.byref(d), *map(ctypes.byref, heads), *mask,
+              ctypes.byref(_heads(o, "o", q.dtype, dev, shape)), _tensor(lse, "lse", torch.float32, shape[1::-1], dev),
+              None if scratch is None else scratch.data_ptr(), n.value, _stream(stream, dev))
+    _used_on(stream, o, lse)
+    return o, lse
+
+
+def noble_attn_bwd(do, q, k, v, o, lse, key_lo=None, key_hi=None, slopes=None, *, causal: bool = False,
+                   offset: Optional[int] = None, scale: Optional[float] = None, softcap: float = 0.0, dq=None, dk=None,
+                   dv=None, stream=None):
+    """(dq, dk, dv) for the upstream gradient ``do`` of noble_attn_fwd's o, with the same inputs and its o and lse."""
+    dev, d, heads, mask = _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap)
+    dt, sq, sk = q.dtype, tuple(q.shape), tuple(k.shape)
+    dq, dk, dv = (torch.empty(s, dtype=dt, device=dev) if t is None else t for t, s in ((dq, sq), (dk, sk), (dv, sk)))
+    g, oo = _heads(do, "do", dt, dev, sq), _heads(o, "o", dt, dev, sq)
+    outs = [_heads(t, n, dt, dev, s) for t, n, s in ((dq, "dq", sq), (dk, "dk", sk), (dv, "dv", sk))]
+    n = _sz(0)
+    _call("noble_attn_scratch_size", ctypes.byref(d), None, ctypes.byref(n))
+    scratch = _scratch(n.value, dev, stream)
+    with _on(dev):
+        _call("noble_attn_bwd", ctypes.byref(d), ctypes.byref(g), *map(ctypes.byref, heads), ctypes.byref(oo),
+              _tensor(lse, "lse", torch.float32, sq[1::-1], dev), *mask, *map(ctypes.byref, outs), scratch.data_ptr(),
+              scratch.numel(), _stream(stream, dev))
+    _used_on(stream, dq, dk, dv)
+    return dq, dk, dv
+
+
+def noble_attn_paged(q, cache, page_table, lengths, slopes=None, *, scale: Optional[float] = None, softcap: float = 0.0,
+                     window: int = 0, o=None, stream=None) -> torch.Tensor:
+    """Attention of each sequence's last tokens over the paged cache, which holds them already: q [B n, heads, D], n rows
+    a sequence; page_table int32 [B, pages of a sequence], lengths int32 [B] (the tokens held).  The row of token t
+    sees the tokens 0 .. t, with a window only its last ``window``."""
+    dev = _gpu(q, "q")
+    if q.dim() != 3 or not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] < 1:
+        raise ValueError("q must be [rows, heads, head_dim] and page_table [sequences, pages]")
+    rows, H, D = q.shape
+    B, per = page_table.shape
+    if rows % B or rows < B:
+        raise ValueError(f"{rows} rows of q are not the same number for each of {B} sequences")
+    K = cache.shape[2] if isinstance(cache, torch.Tensor) and cache.dim() == 5 else 0
+    pages, page, pc = _cache_shape(cache, K, D, q.dtype, dev)
+    o = torch.empty((rows, H, D), dtype=q.dtype, device=dev) if o is None else o
+    i32 = torch.int32
+    d = noble_paged_desc(B, per, pages, page, rows // B, window, H, K, D, _dtype_code(q),
+                         D ** -0.5 if scale is None else scale, softcap, 0)
+    n = _sz(0)
+    _call("noble_attn_paged_scratch_size", ctypes.byref(d), ctypes.byref(n))
+    scratch = _scratch(n.value, dev, stream) if n.value else None
+    with _on(dev):
+        _call("noble_attn_paged", ctypes.byref(d), ctypes.byref(_heads(q, "q", q.dtype, dev)), pc,
+              _tensor(page_table, "page_table", i32, (B, per), dev), _tensor(lengths, "lengths", i32, (B,), dev),
+              _tensor(slopes, "slopes", torch.float32, (H,), dev),
+              ctypes.byref(_heads(o, "o", q.dtype, dev, (rows, H, D))),
+              None if scratch is None else scratch.data_ptr(), n.value, _stream(stream, dev))
+    _used_on(stream, o)
+    return o
