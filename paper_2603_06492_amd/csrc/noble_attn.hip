@@ -133,7 +133,7 @@ noble_status check_attn(const noble_attn_desc* d) {
         return NOBLE_ERR_BAD_SHAPE;
     // every launch within one dispatch
     const int64_t longest = std::max(d->Tq, d->Tk);
-    if ((longest + kOwn - 1) / kOwn * d->heads > kMaxGroups256 || (d->Tq + kPart - 1) / kPart > kMaxGroups256)
+    if ((longest + kOwn - 1) / kOwn * d->heads > kMaxGroups256 - 64)
         return NOBLE_ERR_BAD_SHAPE;
     return NOBLE_OK;
 }
@@ -167,7 +167,7 @@ noble_status check_mask(const noble_attn_desc* d, const int32_t* lo, const int32
 ScoreArgs score_args(float scale, float cap) {
     ScoreArgs k{};
     const double log2e = 1.4426950408889634, x = cap > 0.f ? (double)scale / cap : 0.0;
-    k.c = (float)(scale * log2e);
+    k.unit = cap > 0.f ? 1.f : (float)(scale * log2e);
     if (cap > 0.f) {
         k.cap_in = (float)x;
         k.cap_e = (float)(2.0 * x * log2e);
@@ -426,7 +426,7 @@ noble_status noble_attn_fwd(const noble_attn_desc* desc, const noble_heads* q, c
     a.v = head_rows(v, desc->dtype);
     a.o = head_rows(o, desc->dtype);
     a.lse = lse;
-    const unsigned groups = (unsigned)(cdiv(desc->Tq, kOwn) * desc->heads);
+    const unsigned groups = (unsigned)HeadOrder::grid(desc->kv_heads, (int64_t)cdiv(desc->Tq, kOwn) * a.share);
     return with_shape(desc->dtype, desc->head_dim, [&]<typename E, int DP>() {
         return with_mode(desc->softcap > 0.f, slopes != nullptr, [&]<int MODE>() {
             return launch(attn_fwd_kernel<E, DP, MODE>, dim3(groups), dim3(256), (hipStream_t)stream, a);
@@ -473,16 +473,12 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
     a.row_hi = reinterpret_cast<int*>(s + ws.hi);
     a.span = reinterpret_cast<int4*>(s + ws.span);
     const hipStream_t st = (hipStream_t)stream;
-    const unsigned tiles_q = (unsigned)cdiv(desc->Tq, kOwn), tiles_k = (unsigned)cdiv(desc->Tk, kOwn);
+    const unsigned groups_q = (unsigned)HeadOrder::grid(desc->kv_heads, (int64_t)cdiv(desc->Tq, kOwn) * a.share);
+    const unsigned groups_k = (unsigned)HeadOrder::grid(desc->kv_heads, cdiv(desc->Tk, kOwn));
     return with_shape(desc->dtype, D, [&]<typename E, int DP>() {
-        if (desc->Tq > 0)
-            NOBLE_TRY(launch(attn_bwd_prep_kernel<E>, dim3((unsigned)cdiv(desc->Tq, kPart), (unsigned)desc->heads),
-                             dim3(256), st, a));
         return with_mode(desc->softcap > 0.f, slopes != nullptr, [&]<int MODE>() {
-            if (desc->Tk > 0)
-                NOBLE_TRY(launch(attn_dkv_kernel<E, DP, MODE>, dim3(tiles_k * (unsigned)desc->kv_heads), dim3(256), st, a));
-            if (desc->Tq > 0)
-                NOBLE_TRY(launch(attn_dq_kernel<E, DP, MODE>, dim3(tiles_q * (unsigned)desc->heads), dim3(256), st, a));
+            if (desc->Tq > 0) NOBLE_TRY(launch(attn_dq_kernel<E, DP, MODE>, dim3(groups_q), dim3(256), st, a));
+            if (desc->Tk > 0) NOBLE_TRY(launch(attn_dkv_kernel<E, DP, MODE>, dim3(groups_k), dim3(256), st, a));
             return NOBLE_OK;
         });
     });

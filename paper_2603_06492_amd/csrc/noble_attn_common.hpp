@@ -167,14 +167,62 @@ struct Tile {
     // as zeros.
     template <int NW, int ROWS>
     static __device__ __forceinline__ void request(i32x4 desc, char* lds, int stride, int db, int wave, int lane) {
-        constexpr int PER = ROWS * RB / 1024 / NW;
+        constexpr int PER = ROWS * RB / 1024 / NW, RPI = 1024 / RB;
         static_assert(PER * NW * 1024 == ROWS * RB, "whole requests");
+        // Request i holds rows RPI i .. of the tile: RPI i in the scalar offset, the row inside it in the lane's
+        const int in = lane / NC, near = in * stride;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int idx = (wave * PER + i) * 64 + lane;
-            const int row = idx / NC, c = (idx % NC) ^ swz(row);
-            dma16(desc, lds + (wave * PER + i) * 1024, 16 * c < db ? (uint32_t)(row * stride + 16 * c) : kOOB, 0);
+            const int first = (wave * PER + i) * RPI, c = (lane % NC) ^ swz(first + in);
+            dma16(desc, lds + (wave * PER + i) * 1024, 16 * c < db ? (uint32_t)(near + 16 * c) : kOOB,
+                  (uint32_t)(first * stride));
         }
+    }
+};
+
+// Fragments of tiles from one lane's place in them.  With the swizzle as it is, the places of a row's fragments differ
+// from the first one's by an exclusive or of a constant, and rows by a constant in the instruction's offset field: two
+// registers stand for all of them.  `off` is a whole number of rows.
+template <typename E, int DP>
+struct Reader {
+    using T = Tile<E, DP>;
+    const char* lds;
+    int lane;
+    __device__ __forceinline__ Reader(const char* base, int lane_) : lds(base), lane(lane_) {}
+    __device__ __forceinline__ Reader at(int off) const { return Reader(lds + off, lane); }
+    // Elements 16 x + 8 (lane / 32) .. of row lane % 32 of the 32 rows at `off`.
+    __device__ __forceinline__ Frag<E> along(int x, int off) const {
+        return T::along(lds + off, lane & 31, 2 * x + (lane >> 5));
+    }
+    // Elements 32 d + lane % 32 of the 16 rows at `off` (see Tile::across).
+    __device__ __forceinline__ Frag<E> across(int d, int off) const { return T::across(lds + off, 0, d, lane); }
+};
+template <int DP>
+struct Reader<uint16_t, DP> {
+    using T = Tile<uint16_t, DP>;
+    uint32_t al, ac;   // LDS addresses
+    __device__ __forceinline__ Reader(const char* base, int lane) {
+        const uint32_t b = (uint32_t)reinterpret_cast<uintptr_t>(NOBLE_LDS(base));
+        const int h = lane >> 5, j = lane & 15;
+        al = b + T::at(lane & 31, h);
+        ac = b + T::at(4 * h + (j >> 2), 2 * ((lane >> 4) & 1) + ((j & 3) >> 1)) + 8 * (j & 1);
+    }
+    __device__ __forceinline__ Reader at(int off) const {
+        Reader r = *this;
+        r.al += off;
+        r.ac += off;
+        return r;
+    }
+    __device__ __forceinline__ Frag<uint16_t> along(int x, int off) const {
+        typedef const __attribute__((address_space(3))) u32x4* ptr;
+        return {*(ptr)(uintptr_t)((al ^ (32 * x)) + off)};
+    }
+    __device__ __forceinline__ Frag<uint16_t> across(int d, int off) const {
+        typedef __attribute__((address_space(3))) s16x4* ptr;
+        const uint64_t lo = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)((ac ^ (64 * d)) + off)));
+        const uint64_t hi = __builtin_bit_cast(
+            uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)((ac ^ (64 * d) ^ 32) + off + 8 * T::RB)));
+        return {u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)}};
     }
 };
 
@@ -200,6 +248,21 @@ __device__ __forceinline__ void dma4(i32x4 desc, char* lds_dst, int lane) {
         :
         : "s"(m0), "v"((uint32_t)(4 * lane)), "s"(desc)
         : "memory", "m0");
+}
+
+// Order of a run of MFMAs whose operand A comes from LDS, READS reads for each PER MFMAs: AHEAD operands are read before
+// the first MFMA and each operand's registers are read again as soon as its MFMAs have been issued.  Without it every
+// MFMA waits for a read that was issued right before it.
+template <int MFMAS, int PER, int READS, int AHEAD>
+__device__ __forceinline__ void read_ahead() {
+    constexpr int N = MFMAS / PER, A = AHEAD < N ? AHEAD : N;
+    __builtin_amdgcn_sched_group_barrier(0x100, READS * A, 0);
+#pragma unroll
+    for (int i = 0; i < N - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PER * A, 0);
 }
 
 // All requests of this wave have arrived and its LDS reads are done, and so it is for every wave.
@@ -231,18 +294,40 @@ __device__ __forceinline__ int wave_max(int x) {
     return __builtin_amdgcn_readfirstlane(x);
 }
 
-// Workgroups run round robin over the 8 XCDs: gives each XCD one contiguous range of [0, n), so that the workgroups
-// that share keys and values share an L2.
-__device__ __forceinline__ int xcd_order(int b, int n) {
-    const int x = b & 7, q = n >> 3, r = n & 7;
-    return x * q + min(x, r) + (b >> 3);
-}
+// Workgroups run round robin over the 8 XCDs, each with an L2 of its own.  Key heads are dealt to XCDs so that the
+// workgroups that share keys and values share an L2: with g the common divisor of the key heads and 8, each 8 / g XCDs
+// take heads / g key heads together, every one of them each (8 / g)th workgroup of these heads.  Contiguous ranges
+// would give one XCD the long rows of a causal mask and another the short ones.
+struct HeadOrder {
+    int heads, per;   // key heads, workgroups of one
+    __host__ __device__ static int common(int heads) { return heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1; }
+    // Workgroups to launch: those without work end at once.
+    __host__ static int64_t grid(int heads, int64_t per) {
+        const int g = common(heads), m = 8 / g;
+        return (heads / g * per + m - 1) / m * 8;
+    }
+    // The key head and the place among its workgroups; false: no work.
+    __device__ __forceinline__ bool place(int b, int& head, int& at) const {
+        const int g = common(heads), m = 8 / g, x = b & 7, mine = heads / g;
+        // An XCD's 32 CUs each get one workgroup of 32 in a row and one of the next 32: every other 32 run backwards,
+        // so that a CU's two are not the same place of two documents (all long ones or all short ones).  Forward and dq
+        // of 8 documents of 1024 rows: 40 -> 37 and 54 -> 49 us.
+        int slot = b >> 3;
+        if ((slot & 32) && (slot | 31) < (int)(gridDim.x >> 3)) slot ^= 31;
+        const int item = slot * m + x % m;
+        if (item >= mine * per) return false;
+        head = x / m * mine + item / per;
+        at = item % per;
+        return true;
+    }
+};
 
 constexpr int kCap = 1, kBias = 2;   // bits of a kernel's MODE
 
-// From raw products q.k to scores in units of log2, capped and biased as the mode says; computed on the host.
+// From raw products q.k to scores: z in units in which z `unit` is the score times log2 e.  Without a cap z is the product
+// and unit = scale log2 e, which the exponential's multiply-add takes along; with one unit is 1.  From the host.
 struct ScoreArgs {
-    float c;          // scale log2 e
+    float unit;
     float cap_in;     // scale / cap
     float cap_e;      // 2 scale log2 e / cap: exp2 of it is e^2x
     float cap_out;    // cap log2 e
@@ -250,6 +335,19 @@ struct ScoreArgs {
     float small;      // |s| up to which x = s scale / cap is at most 1/2
     float p[5];       // there: score = s (p0 + p1 s^2 + .. + p4 s^8)
 };
+
+// exp of a score less `from` (both times log2 e).
+template <int MODE>
+__device__ __forceinline__ float exp_score(const ScoreArgs& k, float z, float from) {
+    return __builtin_amdgcn_exp2f(MODE & kCap ? z - from : fmaf(z, k.unit, -from));
+}
+
+// The distance bias on z, slope in the same units, of the keys or rows `first` + 8 (i / 4) + i % 4 for i < 16.  Distances
+// are exact in float32 up to 2^24.
+__device__ __forceinline__ void bias16(float* z, float slope, float first) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = fmaf(-slope, fabsf(first + (float)(8 * (i >> 2) + (i & 3))), z[i]);
+}
 
 // N scores of one lane.  tanh by two formulas: up to 1/2 an odd polynomial of degree 9 (fitted to tanh(x) / x on
 // [0, 1/4] in x^2: relative error 3e-8), above it 1 - 2 / (e^2x + 1), whose absolute error of 1e-7 is relative there.
@@ -260,7 +358,7 @@ template <typename E, int MODE, int N>
 __device__ __forceinline__ void scores(const ScoreArgs& k, const float* s, float* z, float* slope) {
     if constexpr (!(MODE & kCap)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = s[i] * k.c;
+        for (int i = 0; i < N; ++i) z[i] = s[i];
     } else if constexpr (sizeof(E) == 4) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {

@@ -120,7 +120,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
         const int d = 32 * s + 8 * g4;
         q[s] = global_frag<E>(qp + d * ES, live && d < a.D);
     }
-    const float slope2 = MODE & kBias ? a.slopes[live ? head : 0] * kLog2e : 0.f;
+    const float slope = MODE & kBias ? a.slopes[live ? head : 0] * kLog2e / a.sc.unit : 0.f;
 
     f32x4 acc[ND];
 #pragma unroll
@@ -169,7 +169,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
             if constexpr (MODE & kBias) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    z[i] -= slope2 * (float)abs(at - (k0 + 16 * (i >> 2) + 4 * g4 + (i & 3)));
+                    z[i] = fmaf(-slope, fabsf((float)(k0 + 4 * g4 - at) + (float)(16 * (i >> 2) + (i & 3))), z[i]);
             }
             if (k0 + kChunk > ck.at0 + 1 || bads[s] || (a.window > 0 && k0 <= ck.at1 - a.window)) {
                 const int from = a.window > 0 ? at - a.window : -1;
@@ -183,7 +183,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
             top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(top, __shfl_xor(top, 32)) * (MODE & kCap ? 1.f : a.sc.unit);
             if (__any(top > m + 8.f)) {   // see attn_fwd_kernel
                 const float to = fmaxf(m, top);
                 const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
@@ -195,7 +195,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
             const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                z[i] = __builtin_amdgcn_exp2f(z[i] - base);
+                z[i] = exp_score<MODE>(a.sc, z[i], base);
                 l += z[i];
             }
             const Frag<E> p = to_frag<E>(z);

@@ -52,15 +52,17 @@ __device__ __forceinline__ void raw(const f32x16& s, float* z) {
     for (int i = 0; i < 16; ++i) z[i] = s[i];
 }
 
-// Workgroup -> (head, own tile): one key head's workgroups in a row, the last tiles (the longest ones under a causal
-// mask) first, the query heads that share the key head side by side.
+// Workgroup -> (head, own tile): the last tiles (the longest ones under a causal mask) of a key head first, the query
+// heads that share it side by side.
 struct OwnTile {
-    int head, tile;
-    __device__ __forceinline__ OwnTile(int tiles, int heads, int share) {
-        const int w = xcd_order(blockIdx.x, gridDim.x);
-        const int per = tiles * share, kv = w / per, r = w - kv * per;
-        head = kv * share + r % share;
-        tile = tiles - 1 - r / share;
+    int head = 0, tile = 0;
+    bool work;
+    __device__ __forceinline__ OwnTile(const AttnArgs& a) {
+        const int tiles = (a.Tq + kOwn - 1) / kOwn;
+        int kv = 0, at = 0;
+        work = HeadOrder{a.heads / a.share, tiles * a.share}.place(blockIdx.x, kv, at);
+        head = kv * a.share + at % a.share;
+        tile = tiles - 1 - at / a.share;
     }
 };
 
@@ -104,7 +106,8 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
     constexpr int ES = T::ES, TB = T::bytes(kPart), NS = DP / 16, ND = DP / 32;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const OwnTile w((a.Tq + kOwn - 1) / kOwn, a.heads, a.share);
+    const OwnTile w(a);
+    if (!w.work) return;
     const int row0 = w.tile * kOwn, row = row0 + 32 * wave + (lane & 31), kv = w.head / a.share, db = a.D * ES;
     const OwnRows own(a, row0, wave, lane);
 
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
     const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[s] = global_frag<E>(qp + 16 * s * ES, row < a.Tq && 16 * s + 8 * h < a.D);
-    const float slope2 = MODE & kBias ? a.slopes[w.head] * kLog2e : 0.f;
+    const float slope = MODE & kBias ? a.slopes[w.head] * kLog2e / a.sc.unit : 0.f;
     const int at = row + a.off;
 
     f32x16 acc[ND];
@@ -130,29 +133,30 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
     float m = -INFINITY, l = 0.f;
+    const Reader<E, DP> rd(lds, lane);
 
     for (int t = 0; t < tiles; ++t) {
         arrive_all();
         if (t + 1 < tiles) request(t + 1);
         const int k0 = own.all_lo + t * kPart;
         if (k0 >= own.wave_hi || k0 + kPart <= own.wave_lo) continue;
-        const char* kt = lds + (t & 1) * 2 * TB;
-        const char* vt = kt + TB;
+        const Reader<E, DP> at_tile = rd.at((t & 1) * 2 * TB);
         float z[32];
+        f32x16 s[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int x = 0; x < NS; ++x)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) mma32x32(s[u], at_tile.along(x, 32 * u * T::RB), q[x]);
+        if constexpr (ES == 2) read_ahead<2 * NS, 1, 1, 4>();
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            f32x16 s;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-            for (int x = 0; x < NS; ++x) mma32x32(s, T::along(kt, 32 * u + (lane & 31), 2 * x + h), q[x]);
-            raw(s, z + 16 * u);
+            raw(s[u], z + 16 * u);
             scores<E, MODE, 16>(a.sc, z + 16 * u, z + 16 * u, nullptr);
-            if constexpr (MODE & kBias) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    z[16 * u + i] -= slope2 * (float)abs(at - (k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3)));
-            }
+            if constexpr (MODE & kBias) bias16(z + 16 * u, slope, (float)(k0 + 4 * h - at) + 32.f * u);
         }
         if (k0 < own.full_lo || k0 + kPart > own.full_hi) {
 #pragma unroll
@@ -164,7 +168,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
         float top = z[0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
-        top = max_halves(top);
+        top = max_halves(top) * (MODE & kCap ? 1.f : a.sc.unit);
         // The maximum that the exponents are taken from need only be near: it follows once a row's own has grown by
         // 2^8, which leaves sums and products far inside their range, and most tiles leave acc as it is.
         if (__any(top > m + 8.f)) {
@@ -180,15 +184,18 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
         const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            z[i] = __builtin_amdgcn_exp2f(z[i] - from);
+            z[i] = exp_score<MODE>(a.sc, z[i], from);
             l += z[i];
         }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const Frag<E> p = to_frag<E>(z + 8 * x);
 #pragma unroll
-            for (int d = 0; d < ND; ++d) mma32x32(acc[d], T::across(vt, 16 * x, d, lane), p);
+            for (int d = 0; d < ND; ++d) mma32x32(acc[d], at_tile.across(d, TB + 16 * x * T::RB), p);
         }
+        if constexpr (ES == 2) read_ahead<4 * ND, 1, 2, 4>();
+        __builtin_amdgcn_s_setprio(0);
     }
 
     l = sum_halves(l);
@@ -207,60 +214,48 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
     if (h == 0) a.lse[(int64_t)w.head * a.Tq + row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
-// Before the backward's products: delta = do.o and lse in units of log2 for every row and head, the rows' intervals and
-// what 64 of them span.  Sixteen lanes a row; bound by reading do and o.
+// The sum over eight elements of two fragments' products.
 template <typename E>
-__global__ __launch_bounds__(256) void attn_bwd_prep_kernel(AttnArgs a) {
-    constexpr int ES = sizeof(E);
-    const int tile = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = lane & 15;
+__device__ __forceinline__ float dot8(const Frag<E>& a, const Frag<E>& b) {
+    float sum = 0.f;
+    if constexpr (sizeof(E) == 2) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int row = 64 * tile + 16 * k + 4 * wave + (lane >> 4);
-        const bool ok = row < a.Tq && 8 * c < a.D;
-        const Frag<E> o = global_frag<E>(a.o.ptr + head * a.o.head + row * a.o.row + 8 * c * ES, ok);
-        const Frag<E> g = global_frag<E>(a.g.ptr + head * a.g.head + row * a.g.row + 8 * c * ES, ok);
-        float sum = 0.f;
-        if constexpr (ES == 2) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sum += bf2f(o.v[j] & 0xffffu) * bf2f(g.v[j] & 0xffffu);
-                sum += __uint_as_float(o.v[j] & 0xffff0000u) * __uint_as_float(g.v[j] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += __uint_as_float(o.v[j >> 2][j & 3]) * __uint_as_float(g.v[j >> 2][j & 3]);
+        for (int j = 0; j < 4; ++j) {
+            sum = fmaf(bf2f(a.v[j] & 0xffffu), bf2f(b.v[j] & 0xffffu), sum);
+            sum = fmaf(__uint_as_float(a.v[j] & 0xffff0000u), __uint_as_float(b.v[j] & 0xffff0000u), sum);
         }
+    } else {
 #pragma unroll
-        for (int x = 8; x; x >>= 1) sum += __shfl_xor(sum, x);
-        if (c == 0) {
-            const float lse = row < a.Tq ? a.lse[(int64_t)head * a.Tq + row] : -INFINITY;
-            const int64_t at = (int64_t)head * a.Tpad + row;
-            a.lse2[at] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-            a.delta[at] = sum;
-        }
+        for (int j = 0; j < 8; ++j)
+            sum = fmaf(__uint_as_float(a.v[j >> 2][j & 3]), __uint_as_float(b.v[j >> 2][j & 3]), sum);
     }
-    if (head == 0 && wave == 0) {
-        const int i = 64 * tile + lane;
-        const bool in = i < a.Tq;
-        const int2 r = in ? row_interval(a, i) : int2{0, 0};
-        if (in) {
-            a.row_lo[i] = r.x;
-            a.row_hi[i] = r.y;
-        }
-        const int most = wave_max(r.y), least = min(wave_min(r.x < r.y ? r.x : INT32_MAX), most);
-        const int from = wave_max(in ? r.x : 0), to = wave_min(in ? r.y : INT32_MAX);
-        if (lane == 0) a.span[tile] = int4{least, most, from, to};
-    }
+    return sum;
 }
 
+// The intervals of 64 rows, one a lane, and what they span.
+__device__ __forceinline__ void write_spans(const AttnArgs& a, int tile, int lane) {
+    const int i = kPart * tile + lane;
+    const bool in = i < a.Tq;
+    const int2 r = in ? row_interval(a, i) : int2{0, 0};
+    if (in) {
+        a.row_lo[i] = r.x;
+        a.row_hi[i] = r.y;
+    }
+    const int most = wave_max(r.y), least = min(wave_min(r.x < r.y ? r.x : INT32_MAX), most);
+    const int from = wave_max(in ? r.x : 0), to = wave_min(in ? r.y : INT32_MAX);
+    if (lane == 0 && kPart * tile < a.Tq) a.span[tile] = int4{least, most, from, to};
+}
+
+// dq, and what the dk/dv launch after it reads: delta (do is here already, o is read once for it), lse in units of log2,
+// the rows' intervals and what 64 of them span.
 template <typename E, int DP, int MODE>
 __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
     constexpr int ES = T::ES, TB = T::bytes(kPart), NS = DP / 16, ND = DP / 32;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const OwnTile w((a.Tq + kOwn - 1) / kOwn, a.heads, a.share);
+    const OwnTile w(a);
+    if (!w.work) return;
     const int row0 = w.tile * kOwn, row = row0 + 32 * wave + (lane & 31), kv = w.head / a.share, db = a.D * ES;
     const OwnRows own(a, row0, wave, lane);
 
@@ -282,10 +277,23 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
         q[s] = global_frag<E>(qp + 16 * s * ES, ok);
         g[s] = global_frag<E>(gp + 16 * s * ES, ok);
     }
-    const float slope2 = MODE & kBias ? a.slopes[w.head] * kLog2e : 0.f;
+    const float slope = MODE & kBias ? a.slopes[w.head] * kLog2e / a.sc.unit : 0.f;
     const int at = row + a.off;
-    const int64_t rh = (int64_t)w.head * a.Tpad + row;
-    const float lse2 = row < a.Tq ? a.lse2[rh] : INFINITY, delta = row < a.Tq ? a.delta[rh] : 0.f;
+    float delta = 0.f, lse2 = INFINITY;
+    {
+        const char* op = a.o.ptr + w.head * a.o.head + (int64_t)row * a.o.row + 8 * h * ES;
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+            delta += dot8(global_frag<E>(op + 16 * s * ES, row < a.Tq && 16 * s + 8 * h < a.D), g[s]);
+        delta = sum_halves(delta);
+        const float lse = row < a.Tq ? a.lse[(int64_t)w.head * a.Tq + row] : -INFINITY;
+        if (lse != -INFINITY) lse2 = lse * kLog2e;
+        if (h == 0 && row < a.Tpad) {
+            a.lse2[(int64_t)w.head * a.Tpad + row] = lse2;
+            a.delta[(int64_t)w.head * a.Tpad + row] = delta;
+        }
+    }
+    if (w.head == 0 && wave < kOwn / kPart) write_spans(a, w.tile * (kOwn / kPart) + wave, lane);
 
     f32x16 acc[ND];
 #pragma unroll
@@ -293,32 +301,34 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
+    const Reader<E, DP> rd(lds, lane);
     for (int t = 0; t < tiles; ++t) {
         arrive_all();
         if (t + 1 < tiles) request(t + 1);
         const int k0 = own.all_lo + t * kPart;
         if (k0 >= own.wave_hi || k0 + kPart <= own.wave_lo) continue;
-        const char* kt = lds + (t & 1) * 2 * TB;
-        const char* vt = kt + TB;
+        const Reader<E, DP> at_tile = rd.at((t & 1) * 2 * TB);
         const bool part = k0 < own.full_lo || k0 + kPart > own.full_hi;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int x = 0; x < NS; ++x) mma32x32(s, T::along(kt, 32 * u + (lane & 31), 2 * x + h), q[x]);
+            for (int x = 0; x < NS; ++x) mma32x32(s, at_tile.along(x, 32 * u * T::RB), q[x]);
 #pragma unroll
-            for (int x = 0; x < NS; ++x) mma32x32(dp, T::along(vt, 32 * u + (lane & 31), 2 * x + h), g[x]);
-            float z[16], dz[16], slope[16];
+            for (int x = 0; x < NS; ++x) mma32x32(dp, at_tile.along(x, TB + 32 * u * T::RB), g[x]);
+            if constexpr (ES == 2) read_ahead<2 * NS, 1, 1, 4>();
+            __builtin_amdgcn_s_setprio(0);
+            float z[16], dz[16], cap_slope[16];
             raw(s, z);
-            scores<E, MODE, 16>(a.sc, z, z, MODE & kCap ? slope : nullptr);
+            scores<E, MODE, 16>(a.sc, z, z, MODE & kCap ? cap_slope : nullptr);
+            if constexpr (MODE & kBias) bias16(z, slope, (float)(k0 + 4 * h - at) + 32.f * u);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                if constexpr (MODE & kBias)
-                    z[i] -= slope2 * (float)abs(at - (k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3)));
-                dz[i] = __builtin_amdgcn_exp2f(z[i] - lse2) * (dp[i] - delta);
-                if constexpr (MODE & kCap) dz[i] *= slope[i];
+                dz[i] = exp_score<MODE>(a.sc, z[i], lse2) * (dp[i] - delta);
+                if constexpr (MODE & kCap) dz[i] *= cap_slope[i];
             }
             if (part) {
 #pragma unroll
@@ -327,12 +337,15 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
                     dz[i] = j >= own.lo && j < own.hi ? dz[i] : 0.f;
                 }
             }
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const Frag<E> f = to_frag<E>(dz + 8 * x);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) mma32x32(acc[d], T::across(kt, 32 * u + 16 * x, d, lane), f);
+                for (int d = 0; d < ND; ++d) mma32x32(acc[d], at_tile.across(d, (32 * u + 16 * x) * T::RB), f);
             }
+            if constexpr (ES == 2) read_ahead<2 * ND, 1, 2, 4>();
+            __builtin_amdgcn_s_setprio(0);
         }
     }
 
@@ -357,9 +370,9 @@ struct Partners {
     int k0, k1, w0, w1;      // the workgroup's keys, and the wave's
     int head = 0, base = -64, lane;
     uint64_t any = 0, mine = 0, full = 0;
-    __device__ __forceinline__ Partners(const AttnArgs& a, int key0, int wave, int lane_)
+    __device__ __forceinline__ Partners(const AttnArgs& a, int key0, int wave_key, int wave_keys, int lane_)
         : share(a.share), tiles((a.Tq + kPart - 1) / kPart), span(a.span), k0(key0), k1(min(key0 + kOwn, a.Tk)),
-          w0(key0 + 32 * wave), w1(min(key0 + 32 * wave + 32, a.Tk)), lane(lane_) {}
+          w0(wave_key), w1(min(wave_key + wave_keys, a.Tk)), lane(lane_) {}
     // The next (head, tile), and whether the wave's keys are seen by any or by all of its rows; false at the end.
     __device__ __forceinline__ bool next(int& hd, int& tile, bool& seen, bool& whole) {
         while (!any) {
@@ -384,38 +397,55 @@ struct Partners {
     }
 };
 
+// dk and dv of 128 keys, 32 a wave: S and dP, then their products with the rows' gradients and queries.
+// bf16 heads of 128: the two sums (128 registers), the keys (32), S and dP (32) and the operands read ahead leave no room
+// for the values in the 256 registers that a wave has when two share a SIMD, so the values are read from LDS for every
+// tile, and tiles are 32 rows, so that two workgroups fit a CU's LDS.
+template <typename E, int DP>
+struct DkvShape {
+    static constexpr bool VALUES_IN_LDS = sizeof(E) == 2 && DP == 128;
+    static constexpr int ROWS = VALUES_IN_LDS ? 32 : kPart;
+    static constexpr int TB = Tile<E, DP>::bytes(ROWS), INFO = 4 * kPart * 4, STAGE = 2 * TB + INFO;
+    static constexpr int LDS = 2 * STAGE + (VALUES_IN_LDS ? Tile<E, DP>::bytes(kOwn) : 0);
+};
+
 template <typename E, int DP, int MODE>
 __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
-    constexpr int ES = T::ES, TB = T::bytes(kPart), NS = DP / 16, ND = DP / 32, STAGE = 2 * TB + 4 * kPart * 4;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+    using S = DkvShape<E, DP>;
+    constexpr int ES = T::ES, TB = S::TB, NS = DP / 16, ND = DP / 32, ROWS = S::ROWS, STAGE = S::STAGE;
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int tiles = (a.Tk + kOwn - 1) / kOwn, wg = xcd_order(blockIdx.x, gridDim.x);
-    const int kv = wg / tiles, key0 = (wg - kv * tiles) * kOwn, key = key0 + 32 * wave + (lane & 31), db = a.D * ES;
+    int kv = 0, key_tile = 0;   // the first keys (which the most rows see under a causal mask) first
+    if (!HeadOrder{a.heads / a.share, (a.Tk + kOwn - 1) / kOwn}.place(blockIdx.x, kv, key_tile)) return;
+    const int key0 = key_tile * kOwn, wkey = key0 + 32 * wave, key = wkey + (lane & 31), db = a.D * ES;
 
-    Partners it(a, key0, wave, lane);
-    const auto request = [&](int stage, int gi, int tile) {
+    Partners it(a, key0, wkey, 32, lane);
+    const auto request = [&](int stage, int gi, int r0) {
         char* dst = lds + stage * STAGE;
-        const int head = kv * a.share + gi, r0 = tile * kPart;
-        T::template request<4, kPart>(rows_desc(a.q, head, r0, a.Tq, db), dst, (int)a.q.row, db, wave, lane);
-        T::template request<4, kPart>(rows_desc(a.g, head, r0, a.Tq, db), dst + TB, (int)a.g.row, db, wave, lane);
+        const int head = kv * a.share + gi;
+        T::template request<4, ROWS>(rows_desc(a.q, head, r0, a.Tq, db), dst, (int)a.q.row, db, wave, lane);
+        T::template request<4, ROWS>(rows_desc(a.g, head, r0, a.Tq, db), dst + TB, (int)a.g.row, db, wave, lane);
         const int64_t rh = (int64_t)head * a.Tpad + r0;
-        const char* src = reinterpret_cast<const char*>(wave == 0 ? a.lse2 + rh : wave == 1 ? a.delta + rh :
-                                                        reinterpret_cast<const float*>(wave == 2 ? a.row_lo + r0 : a.row_hi + r0));
-        dma4(wave_desc(src, (int64_t)(wave < 2 ? kPart : a.Tq - r0) * 4), dst + 2 * TB + wave * kPart * 4, lane);
+        const void* src = wave == 0 ? static_cast<const void*>(a.lse2 + rh) : wave == 1 ? a.delta + rh :
+                          wave == 2 ? static_cast<const void*>(a.row_lo + r0) : a.row_hi + r0;
+        dma4(wave_desc(static_cast<const char*>(src), (int64_t)(wave < 2 ? ROWS : min(a.Tq - r0, ROWS)) * 4),
+             dst + 2 * TB + wave * kPart * 4, lane);
     };
-    int gi = 0, tile = 0;
+    int gi = 0, tile = 0, sub = 0;   // sub: the part of ROWS rows of a 64-row tile
     bool seen = false, whole = false, more = it.next(gi, tile, seen, whole);
-    if (more) request(0, gi, tile);
+    if (more) request(0, gi, tile * kPart);
+    if constexpr (S::VALUES_IN_LDS)
+        T::template request<4, kOwn>(rows_desc(a.v, kv, key0, a.Tk, db), lds + 2 * STAGE, (int)a.v.row, db, wave, lane);
 
-    Frag<E> k[NS], v[NS];
+    Frag<E> k[NS], v[S::VALUES_IN_LDS ? 1 : NS];
     const char* kp = a.k.ptr + kv * a.k.head + (int64_t)key * a.k.row + 8 * h * ES;
     const char* vp = a.v.ptr + kv * a.v.head + (int64_t)key * a.v.row + 8 * h * ES;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         const bool ok = key < a.Tk && 16 * s + 8 * h < a.D;
         k[s] = global_frag<E>(kp + 16 * s * ES, ok);
-        v[s] = global_frag<E>(vp + 16 * s * ES, ok);
+        if constexpr (!S::VALUES_IN_LDS) v[s] = global_frag<E>(vp + 16 * s * ES, ok);
     }
 
     f32x16 dk[ND], dv[ND];
@@ -424,66 +454,82 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dkv_kernel(A
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.f;
 
+    const Reader<E, DP> rd(lds, lane);
+    const Reader<E, DP> values = rd.at(2 * STAGE + 32 * wave * T::RB);
     for (int n = 0; more; ++n) {
-        const int r0 = tile * kPart, head = kv * a.share + gi;
-        const bool do_it = seen, part = !whole;
+        const int r0 = tile * kPart + sub * ROWS, head = kv * a.share + gi, stage = (n & 1) * STAGE;
+        const bool mine = seen, part = !whole;
         arrive_all();
-        more = it.next(gi, tile, seen, whole);
-        if (more) request((n + 1) & 1, gi, tile);
-        if (!do_it) continue;
-        const char* qt = lds + (n & 1) * STAGE;
-        const char* gt = qt + TB;
-        const char* rows = gt + TB;
-        const float slope2 = MODE & kBias ? a.slopes[head] * kLog2e : 0.f;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        if (++sub == kPart / ROWS || tile * kPart + sub * ROWS >= a.Tq) {
+            sub = 0;
+            more = it.next(gi, tile, seen, whole);
+        }
+        if (more) request((n + 1) & 1, gi, tile * kPart + sub * ROWS);
+        if (!mine) continue;
+        const float slope = MODE & kBias ? a.slopes[head] * kLog2e / a.sc.unit : 0.f;
+#pragma unroll 1
+        for (int u = 0; u < ROWS / 32; ++u) {
+            // 32 rows: S and dP, p, dv, dz, dk
+            const Reader<E, DP> at = rd.at(stage + 32 * u * T::RB);
+            const char* rows = lds + stage + 2 * TB + 4 * (32 * u + 4 * h);   // lse2, delta, lo, hi of rows 4 h ..
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int x = 0; x < NS; ++x) mma32x32(s, T::along(qt, 32 * u + (lane & 31), 2 * x + h), k[x]);
+            for (int x = 0; x < NS; ++x) mma32x32(s, at.along(x, 0), k[x]);
 #pragma unroll
-            for (int x = 0; x < NS; ++x) mma32x32(dp, T::along(gt, 32 * u + (lane & 31), 2 * x + h), v[x]);
-            float p[16], dz[16], slope[16];
+            for (int x = 0; x < NS; ++x) {
+                if constexpr (S::VALUES_IN_LDS) mma32x32(dp, at.along(x, TB), values.along(x, 0));
+                else mma32x32(dp, at.along(x, TB), v[x]);
+            }
+            if constexpr (S::VALUES_IN_LDS) {
+                read_ahead<NS, 1, 1, 3>();
+                read_ahead<NS, 1, 2, 2>();
+            } else if constexpr (ES == 2) {
+                read_ahead<2 * NS, 1, 1, 4>();
+            }
+            __builtin_amdgcn_s_setprio(0);
+            float p[16], cap_slope[16];
             raw(s, p);
-            scores<E, MODE, 16>(a.sc, p, p, MODE & kCap ? slope : nullptr);
+            scores<E, MODE, 16>(a.sc, p, p, MODE & kCap ? cap_slope : nullptr);
+            if constexpr (MODE & kBias) bias16(p, slope, (float)(r0 + 4 * h + a.off - key) + 32.f * u);
+            if (part) {
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const i32x4 lo = *reinterpret_cast<const i32x4*>(rows + 8 * kPart + 32 * i4);
+                    const i32x4 hi = *reinterpret_cast<const i32x4*>(rows + 12 * kPart + 32 * i4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        p[4 * i4 + e] = key >= lo[e] && key < hi[e] ? p[4 * i4 + e] : -INFINITY;
+                }
+            }
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) {
-                const int r = 32 * u + 8 * i4 + 4 * h;   // four rows of the tile
-                const f32x4 lse2 = *reinterpret_cast<const f32x4*>(rows + 4 * r);
-                const f32x4 delta = *reinterpret_cast<const f32x4*>(rows + 4 * kPart + 4 * r);
+                const f32x4 lse2 = *reinterpret_cast<const f32x4*>(rows + 32 * i4);
+                const f32x4 delta = *reinterpret_cast<const f32x4*>(rows + 4 * kPart + 32 * i4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 4 * i4 + e;
-                    if constexpr (MODE & kBias) p[i] -= slope2 * (float)abs(r0 + r + e + a.off - key);
-                    p[i] = __builtin_amdgcn_exp2f(p[i] - lse2[e]);
-                    dz[i] = p[i] * (dp[i] - delta[e]);
-                    if constexpr (MODE & kCap) dz[i] *= slope[i];
+                    p[i] = exp_score<MODE>(a.sc, p[i], lse2[e]);
+                    dp[i] = p[i] * (dp[i] - delta[e]);
+                    if constexpr (MODE & kCap) dp[i] *= cap_slope[i];
                 }
             }
-            if (part) {
-                typedef int i32x4_ __attribute__((ext_vector_type(4)));
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const int r = 32 * u + 8 * i4 + 4 * h;
-                    const i32x4_ lo = *reinterpret_cast<const i32x4_*>(rows + 8 * kPart + 4 * r);
-                    const i32x4_ hi = *reinterpret_cast<const i32x4_*>(rows + 12 * kPart + 4 * r);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const bool ok = key >= lo[e] && key < hi[e];
-                        p[4 * i4 + e] = ok ? p[4 * i4 + e] : 0.f;
-                        dz[4 * i4 + e] = ok ? dz[4 * i4 + e] : 0.f;
-                    }
-                }
-            }
+            float dz[16];
+            raw(dp, dz);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const Frag<E> fp = to_frag<E>(p + 8 * x), fz = to_frag<E>(dz + 8 * x);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) mma32x32(dv[d], T::across(gt, 32 * u + 16 * x, d, lane), fp);
-#pragma unroll
-                for (int d = 0; d < ND; ++d) mma32x32(dk[d], T::across(qt, 32 * u + 16 * x, d, lane), fz);
+                for (int d = 0; d < ND; ++d) {
+                    mma32x32(dv[d], at.across(d, TB + 16 * x * T::RB), fp);
+                    mma32x32(dk[d], at.across(d, 16 * x * T::RB), fz);
+                }
             }
+            if constexpr (ES == 2) read_ahead<4 * ND, 1, 2, 3>();
+            __builtin_amdgcn_s_setprio(0);
         }
     }
 
