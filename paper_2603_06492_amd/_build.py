@@ -1,5 +1,6 @@
 """Builds libnoble.so (the HIP kernels and the C ABI) in-tree for gfx950, and
-_noble_torch.so, the binding's calls on torch tensors (host code)."""
+_noble_torch.so and _noble_attn_torch.so, the binding's calls on torch tensors
+(host code)."""
 
 from __future__ import annotations
 
@@ -16,8 +17,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libnoble.so")
 BINDING = os.path.join(PKG, "_noble_torch.so")
+BINDINGS = [("noble_torch.cpp", BINDING), ("noble_attn_torch.cpp", os.path.join(PKG, "_noble_attn_torch.so"))]
 SOURCES = ["noble_api.hip", "noble_attn.hip"]
-HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_binding.h", "noble_torch.cpp"]
+HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_binding.h", "noble_torch.cpp", "noble_attn_torch.cpp"]
 
 HIP_FLAGS = [
     "-O3",
@@ -62,22 +64,24 @@ def build(verbose: bool = False) -> str:
 
 
 def build_binding(verbose: bool = False) -> str:
-    """Compile _noble_torch.so (a CPython extension on torch's C++ headers)."""
+    """Compile the bindings (CPython extensions on torch's C++ headers)."""
     import torch
     root = os.path.dirname(torch.__file__)
-    inc, tmp = os.path.join(root, "include"), BINDING + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, "-isystem", inc,
-           "-isystem", os.path.join(inc, "torch/csrc/api/include"), "-isystem", "/opt/rocm/include",
-           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "noble_torch.cpp"),
-           "-L", os.path.join(root, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python",
-           "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError(f"g++ failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
-    os.replace(tmp, BINDING)
+    inc = os.path.join(root, "include")
+    for source, target in BINDINGS:
+        tmp = target + ".tmp"
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, "-isystem", inc,
+               "-isystem", os.path.join(inc, "torch/csrc/api/include"), "-isystem", "/opt/rocm/include",
+               "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, source),
+               "-L", os.path.join(root, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python",
+               "-o", tmp]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError(f"g++ failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+        os.replace(tmp, target)
     return BINDING
 
 

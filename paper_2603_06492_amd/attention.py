@@ -14,6 +14,8 @@ There is no fallback: without the built library or a gfx950 device, calls raise.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import os
 from typing import Optional, Tuple
 
 import torch
@@ -88,6 +90,36 @@ def lib() -> ctypes.CDLL:
             f.restype, f.argtypes = ctypes.c_int, args
         _ready = True
     return L
+
+
+BINDING_PATH = os.path.join(noble.PKG_DIR, "_noble_attn_torch.so")
+_native_module = None
+
+
+def _native():
+    """The native calls (_noble_attn_torch.so), given the library's entry points.  They serve well-formed calls on
+    ordinary tensors and the current stream and return None for any other, which the Python code then checks and runs."""
+    global _native_module
+    if _native_module is None:
+        L = lib()
+        if not os.path.exists(BINDING_PATH):
+            raise RuntimeError(f"{BINDING_PATH} is missing: build it with __graft_entry__.build() "
+                               "(or python -m paper_2603_06492_amd._build)")
+        spec = importlib.util.spec_from_file_location("_noble_attn_torch", BINDING_PATH)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        m.init(*(ctypes.cast(getattr(L, n), _vp).value for n in (
+            "noble_qk_rope_fwd", "noble_qk_rope_bwd", "noble_qk_rope_scratch_size", "noble_kv_append", "noble_attn_fwd",
+            "noble_attn_bwd", "noble_attn_scratch_size", "noble_attn_paged", "noble_attn_paged_scratch_size")))
+        _native_module = m
+    return _native_module
+
+
+def _served(out, name) -> bool:
+    """Whether the native code served a call; raises for a status."""
+    if isinstance(out, int):
+        raise NobleError(out, name)
+    return out is not None
 
 
 def _call(name, *args) -> None:
@@ -218,6 +250,10 @@ def noble_qk_rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, *, heads: in
     """q [T, heads, D] and k [T, kv_heads, D] from the Q/K/V layer's rows [T, (heads + 2 kv_heads) D]: each head normed
     (weights float32 [D]; None: not) and its first 2 cos.shape[1] elements rotated by the token's position (int32 [T],
     None: the row's number; cos None: not)."""
+    if stream is None:
+        out = _native().rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved, q, k)
+        if _served(out, "noble_qk_rope_fwd"):
+            return out
     dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
     T, D = d.T, d.head_dim
     q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
@@ -233,6 +269,11 @@ def noble_qk_rope_bwd(dq, dk, qkv, q_weight, k_weight, cos, sin, positions, *, h
                       eps: float = 1e-6, interleaved: bool = False, dqkv=None, stream=None):
     """(dqkv, dq_weight, dk_weight): the query and key columns of dqkv are written, the value columns left as they are
     (zeros in a tensor allocated here).  The weights' gradients are None without weights."""
+    if stream is None and dqkv is not None:
+        out = _native().rope_bwd(dq, dk, qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved,
+                                 dqkv)
+        if _served(out, "noble_qk_rope_bwd"):
+            return dqkv, *out
     dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
     T, D = d.T, d.head_dim
     grads = [_tensor(dq, "dq", qkv.dtype, (T, heads, D), dev), _tensor(dk, "dk", qkv.dtype, (T, kv_heads, D), dev)]
@@ -269,6 +310,11 @@ def noble_kv_append(qkv, q_weight, k_weight, cos, sin, positions, slots, cache, 
     """Writes each row's keys, normed and rotated, and values to its slot (int64 [T], page number x page size + place;
     outside the cache: not written) of cache [pages, 2, kv_heads, page, D], and returns the queries, normed and
     rotated."""
+    if stream is None:
+        out = _native().append(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved, slots, cache,
+                               q)
+        if _served(out, "noble_kv_append"):
+            return out[0]
     dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
     T, D = d.T, d.head_dim
     pages, page, pc = _cache_shape(cache, kv_heads, D, qkv.dtype, dev)
@@ -323,6 +369,10 @@ def noble_attn_fwd(q, k, v, key_lo=None, key_hi=None, slopes=None, *, causal: bo
     keys [key_lo[i], key_hi[i]) (int32; None: all), with ``causal`` only those up to i + offset (default: the last row
     sees the last key).  Scores are scale q.k (default D^-1/2), capped by softcap tanh(. / softcap) and lowered by
     slopes[head] |i + offset - j|.  o: like q, dense; lse: float32 [heads, Tq]."""
+    if stream is None:
+        out = _native().attn_fwd(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap, o, lse)
+        if _served(out, "noble_attn_fwd"):
+            return out
     dev, d, heads, mask = _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap)
     shape = tuple(q.shape)
     o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
@@ -342,6 +392,10 @@ def noble_attn_bwd(do, q, k, v, o, lse, key_lo=None, key_hi=None, slopes=None, *
                    offset: Optional[int] = None, scale: Optional[float] = None, softcap: float = 0.0, dq=None, dk=None,
                    dv=None, stream=None):
     """(dq, dk, dv) for the upstream gradient ``do`` of noble_attn_fwd's o, with the same inputs and its o and lse."""
+    if stream is None:
+        out = _native().attn_bwd(do, o, lse, q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap, dq, dk, dv)
+        if _served(out, "noble_attn_bwd"):
+            return out
     dev, d, heads, mask = _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap)
     dt, sq, sk = q.dtype, tuple(q.shape), tuple(k.shape)
     dq, dk, dv = (torch.empty(s, dtype=dt, device=dev) if t is None else t for t, s in ((dq, sq), (dk, sk), (dv, sk)))
@@ -363,6 +417,10 @@ def noble_attn_paged(q, cache, page_table, lengths, slopes=None, *, scale: Optio
     """Attention of each sequence's last tokens over the paged cache, which holds them already: q [B n, heads, D], n rows
     a sequence; page_table int32 [B, pages of a sequence], lengths int32 [B] (the tokens held).  The row of token t
     sees the tokens 0 .. t, with a window only its last ``window``."""
+    if stream is None:
+        out = _native().paged(q, cache, page_table, lengths, slopes, scale, softcap, window, o)
+        if _served(out, "noble_attn_paged"):
+            return out[0]
     dev = _gpu(q, "q")
     if q.dim() != 3 or not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] < 1:
         raise ValueError("q must be [rows, heads, head_dim] and page_table [sequences, pages]")

@@ -71,11 +71,23 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
     w /= a.kv_heads;
     const int rt = w % a.row_tiles;
     w /= a.row_tiles;
-    const int piece = w % a.pieces, b = w / a.pieces;
+    const int piece = w % a.pieces, b = w / a.pieces, db = a.D * ES;
+    // this lane's row, whose loads go out before anything that waits for the lengths
+    const int r = rt * kRows16 + n16, rows = a.fresh * a.share;
+    const bool live = r < rows;
+    const int tok = r / a.share, head = kv * a.share + r % a.share;
+    Frag<E> q[NS];
+    const char* qp = a.q.ptr + (int64_t)(live ? head : 0) * a.q.head + ((int64_t)b * a.fresh + (live ? tok : 0)) * a.q.row;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int d = 32 * s + 8 * g4;
+        q[s] = global_frag<E>(qp + d * ES, live && d < a.D);
+    }
+    const float slope = MODE & kBias ? a.slopes[live ? head : 0] * kLog2e / a.sc.unit : 0.f;
     const Chunks ck(a, b, rt, W);
     if (piece >= ck.pieces) return;
+    const int at = live ? ck.len - a.fresh + tok : ck.at1;
     const int c0 = ck.bound(piece) + wave, c1 = ck.bound(piece + 1);
-    const int db = a.D * ES;
 
     char* ring = lds + wave * NST * S::STAGE;
     typedef const __attribute__((address_space(4))) int* table_ptr;
@@ -108,19 +120,6 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
         }
     };
 
-    // this lane's row
-    const int r = rt * kRows16 + n16, rows = a.fresh * a.share;
-    const bool live = r < rows;
-    const int tok = r / a.share, head = kv * a.share + r % a.share;
-    const int at = live ? ck.len - a.fresh + tok : ck.at1;
-    Frag<E> q[NS];
-    const char* qp = a.q.ptr + (int64_t)(live ? head : 0) * a.q.head + ((int64_t)b * a.fresh + (live ? tok : 0)) * a.q.row;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        const int d = 32 * s + 8 * g4;
-        q[s] = global_frag<E>(qp + d * ES, live && d < a.D);
-    }
-    const float slope = MODE & kBias ? a.slopes[live ? head : 0] * kLog2e / a.sc.unit : 0.f;
 
     f32x4 acc[ND];
 #pragma unroll
@@ -271,15 +270,32 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs j) {
     if (ck.pieces == 1) return;
     const int64_t step = (int64_t)a.row_tiles * a.kv_heads * kRows16 * LD;   // from piece to piece
     const float* p = a.part + ((((int64_t)b * a.pieces * a.row_tiles + rt) * a.kv_heads + kv) * kRows16 + row % kRows16) * LD;
-    float top = -INFINITY;
-    for (int x = 0; x < ck.pieces; ++x) top = fmaxf(top, p[x * step + DP]);
-    const float base = top == -INFINITY ? 0.f : top;
+    // eight pieces at a time, their loads all in flight
+    constexpr int N = 8;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-    for (int x = 0; x < ck.pieces; ++x) {
-        const float f = __builtin_amdgcn_exp2f(p[x * step + DP] - base);
-        sum += *reinterpret_cast<const f32x4*>(p + x * step + d) * f;
-        total += p[x * step + DP + 1] * f;
+    float total = 0.f, top = -INFINITY;
+    for (int x0 = 0; x0 < ck.pieces; x0 += N) {
+        f32x4 v[N];
+        float m[N], l[N], next = top;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float* q = p + min(x0 + n, ck.pieces - 1) * step;
+            v[n] = *reinterpret_cast<const f32x4*>(q + d);
+            m[n] = x0 + n < ck.pieces ? q[DP] : -INFINITY;
+            l[n] = q[DP + 1];
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) next = fmaxf(next, m[n]);
+        const float base = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - base);
+        sum *= keep;
+        total *= keep;
+        top = next;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float f = __builtin_amdgcn_exp2f(m[n] - base);
+            sum += v[n] * f;
+            total += l[n] * f;
+        }
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     if (d < a.D)

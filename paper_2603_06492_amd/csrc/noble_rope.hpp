@@ -145,13 +145,17 @@ __global__ __launch_bounds__(256) void qk_rope_kernel(RopeArgs a) {
         row = a.cache + ((slot >> a.page_shift) * 2 * a.kv_heads * a.page + (slot & (a.page - 1))) * db;
     const int first = APPEND && !a.q ? a.heads : 0;   // no queries wanted
     const int steps = (total - first + a.split - 1) / a.split;
+    // the next head is on its way while this one is worked on
+    const auto head_at = [&](int n) { return min(first + part + n * a.split, total - 1); };
+    Frag<E> next{};
+    if (steps > 0) next = global_frag<E>(xr + head_at(0) * db, in);
     for (int n = 0; n < steps; ++n) {
-        const int hh = first + part + n * a.split;
-        const bool have = hh < total;
-        const int h = have ? hh : total - 1;
+        const bool have = first + part + n * a.split < total;
+        const int h = head_at(n);
         const bool isq = h < a.heads;
         float x[8];
-        to_f32(global_frag<E>(xr + h * db, in), x);
+        to_f32(next, x);
+        if (n + 1 < steps) next = global_frag<E>(xr + head_at(n + 1) * db, in);
         if (norm) {
             float sum = 0.f;
 #pragma unroll
@@ -200,15 +204,25 @@ __global__ __launch_bounds__(256) void qk_rope_bwd_kernel(RopeArgs a) {
         const int part = (int)(item - tok * a.split);
         const Angles<INTER> ang(a, a.positions ? a.positions[t] : t, c);
         const int steps = (total + a.split - 1) / a.split;
+        const auto head_at = [&](int n) { return min(part + n * a.split, total - 1); };
+        const auto grad = [&](int n) {
+            const int h = head_at(n);
+            const char* gp = h < a.heads ? a.q + (t * a.heads + h) * db : a.k + (t * a.kv_heads + h - a.heads) * db;
+            return global_frag<E>(gp + off, in);
+        };
+        const auto value = [&](int n) { return global_frag<E>(a.x + t * a.x_row + head_at(n) * db + off, in && norm); };
+        Frag<E> next_g = grad(0), next_x = value(0);
         for (int n = 0; n < steps; ++n) {
-            const int hh = part + n * a.split;
-            const bool have = live && hh < total;
-            const int h = have ? hh : total - 1;
+            const bool have = live && part + n * a.split < total;
+            const int h = head_at(n);
             const bool isq = h < a.heads;
-            const char* gp = isq ? a.q + (t * a.heads + h) * db : a.k + (t * a.kv_heads + h - a.heads) * db;
             float x[8], du[8];
-            to_f32(global_frag<E>(gp + off, in), du);
-            if (norm) to_f32(global_frag<E>(a.x + t * a.x_row + h * db + off, in), x);
+            to_f32(next_g, du);
+            to_f32(next_x, x);
+            if (n + 1 < steps) {
+                next_g = grad(n + 1);
+                next_x = value(n + 1);
+            }
             if (a.rot) ang.turn(du, a.rot, c, -1.f);
             if (norm) {
                 float sum = 0.f, dot = 0.f;
@@ -246,23 +260,26 @@ __global__ __launch_bounds__(256) void qk_rope_bwd_kernel(RopeArgs a) {
     }
 }
 
-// The workgroups' sums of the weights' gradients, 16 rows of lanes a column, in a fixed order.
+// The workgroups' sums of the weights' gradients, 64 lanes a column, in a fixed order.
 struct RopeDwArgs {
     const float* partial;
     float* dwq;
     float* dwk;
     int parts, D;
 };
-static __global__ __launch_bounds__(256) void rope_dw_kernel(RopeDwArgs a) {
-    __shared__ float part[16][17];
+static __global__ __launch_bounds__(1024) void rope_dw_kernel(RopeDwArgs a) {
+    constexpr int ROWS = 64;
+    __shared__ float part[ROWS][17];
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4, col = blockIdx.x * 16 + x, which = blockIdx.y;
     float s = 0.f;
-    for (int p = y; p < a.parts; p += 16) s += a.partial[((int64_t)p * 2 + which) * 128 + col];
+    // eight loads in flight: one by one, 2048 partial sums took 50 us, a quarter of the backward
+#pragma unroll 8
+    for (int p = y; p < a.parts; p += ROWS) s += a.partial[((int64_t)p * 2 + which) * 128 + col];
     part[y][x] = s;
     __syncthreads();
     if (y == 0 && col < a.D) {
         float t = 0.f;
-        for (int i = 0; i < 16; ++i) t += part[i][x];
+        for (int i = 0; i < ROWS; ++i) t += part[i][x];
         (which ? a.dwk : a.dwq)[col] = t;
     }
 }
