@@ -150,9 +150,9 @@ noble_status noble_kv_append(const noble_rope_desc* desc,
  *   s = softcap tanh(z / softcap) (softcap 0: z) - slope[h] |i + offset - j|
  *   o_i = sum_j exp(s_j - lse_i) v_j,   lse_i = log sum_j exp(s_j)
  * (slopes float32 [heads], NULL: no bias; constants, without a gradient).
- * Query head h uses key head h / (heads / kv_heads).  A value that a row does
- * not see does not reach it, unless it is infinite or NaN and lies between
- * keys that the row's neighbours in a tile of 128 rows see. */
+ * Query head h uses key head h / (heads / kv_heads).  Infinite and NaN values
+ * reach the rows that see them and no other (such rows, and those beside
+ * them, are slow). */
 typedef struct noble_attn_desc {
     int64_t Tq, Tk;       /* rows of q, and of k and v: up to 2^31 - 4096 */
     int64_t offset;       /* key index of query row 0, |offset| < 2^31 - 4096 */
@@ -197,7 +197,10 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
  * the cache holds already.  The row of token t sees the tokens 0 .. t, with a
  * window only the last `window` of them (0: all).  A token whose page is
  * outside the cache is not seen; nor is, for a row of a token before the
- * first, anything, which gives zeros.  Scores as in noble_attn_fwd. */
+ * first, anything, which gives zeros.  Scores as in noble_attn_fwd.  Slots
+ * past a sequence's tokens, and before every row's window, may hold anything;
+ * an infinite or NaN value of a new token may also reach the sequence's new
+ * tokens before it. */
 typedef struct noble_paged_desc {
     int64_t B;
     int64_t table_row;    /* entries of one sequence's page table */

@@ -33,7 +33,7 @@ constexpr int kRows16 = 16;      // rows of a workgroup
 // A sequence's keys as a row tile sees them, in chunks, and the pieces that they are split into: at least one chunk for
 // every wave of a piece.
 struct Chunks {
-    int len, first, count, end, pieces, at0, at1;   // chunks [first, first + count); keys end at `end`
+    int len, first, count, start, end, pieces, at0, at1;   // chunks [first, first + count) of the keys [start, end)
     __device__ __forceinline__ Chunks(const PagedArgs& a, int b, int row_tile, int waves) {
         const int64_t held = a.table_row * a.page;
         len = (int)min((int64_t)max(a.lengths[b], 0), held);
@@ -41,7 +41,7 @@ struct Chunks {
         at0 = len - a.fresh + row_tile * kRows16 / a.share;
         at1 = len - a.fresh + r1 / a.share;
         end = max(at1 + 1, 0);
-        const int start = a.window > 0 ? max(at0 - a.window + 1, 0) : 0;
+        start = a.window > 0 ? max(at0 - a.window + 1, 0) : 0;
         first = start / kChunk;
         count = end > start ? (end + kChunk - 1) / kChunk - first : 0;
         pieces = max(1, min(a.pieces, count / waves));
@@ -113,7 +113,8 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
             if (!ok) bad |= ((1u << RPI) - 1u) << (i * RPI);
             const char* src = base + (int64_t)(ok ? page : 0) * a.page_bytes + (int64_t)i * RPI * db;
             const int row = i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(row);
-            const uint32_t vo = 16 * ch < db ? (uint32_t)((lane / T::NC) * db + 16 * ch) : kOOB;
+            // a key before every row's window is not read either: what it holds may be anything
+            const uint32_t vo = 16 * ch < db && (k0 >= ck.start || k0 + row >= ck.start) ? (uint32_t)((lane / T::NC) * db + 16 * ch) : kOOB;
             const int64_t bytes = ok ? (int64_t)left * db : 0;
             dma16(wave_desc(src, bytes), dst + i * 1024, vo, 0);
             dma16(wave_desc(src + (int64_t)a.kv_heads * a.page * db, bytes), dst + S::STAGE / 2 + i * 1024, vo, 0);

@@ -99,6 +99,74 @@ struct OwnRows {
     }
 };
 
+// ---- rows whose sums came out infinite or NaN ------------------------------------------------------------------------
+// A product over a tile multiplies a key (or row) that is not seen by a probability of zero, and zero times an infinite
+// or NaN element is NaN.  So a wave that finds such a result forms these rows again, one after the other and over the
+// seen partners alone, with two elements of the head a lane: unseen values do not reach a row, seen ones do.
+
+// The sums' zeroes: NaN if any element is infinite or NaN.
+template <int ND>
+__device__ __forceinline__ float zero_of(const f32x16 (&acc)[ND], float t) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t = fmaf(acc[d][i], 0.f, t);
+    return t;
+}
+// The own rows (bit r: row r of 32) that the lanes l and l + 32 say no to.
+__device__ __forceinline__ uint32_t rows_of(bool bad) {
+    const uint64_t b = __ballot(bad);
+    return (uint32_t)b | (uint32_t)(b >> 32);
+}
+struct Pair {
+    float x = 0.f, y = 0.f;
+};
+// Elements 2 lane and 2 lane + 1 of one row (zeros past the head).
+template <typename E>
+__device__ __forceinline__ Pair load_pair(const HeadRows& t, int head, int64_t row, int D, int lane) {
+    Pair p;
+    if (2 * lane < D) {
+        const char* at = t.ptr + head * t.head + row * t.row + 2 * lane * (int)sizeof(E);
+        if constexpr (sizeof(E) == 2) {
+            const uint32_t v = *reinterpret_cast<const uint32_t*>(at);
+            p.x = __uint_as_float(v << 16);
+            p.y = __uint_as_float(v & 0xffff0000u);
+        } else {
+            p.x = reinterpret_cast<const float*>(at)[0];
+            p.y = reinterpret_cast<const float*>(at)[1];
+        }
+    }
+    return p;
+}
+template <typename E>
+__device__ __forceinline__ void store_pair(const HeadRows& t, int head, int64_t row, int D, int lane, float x, float y) {
+    if (2 * lane >= D) return;
+    char* at = t.ptr + head * t.head + row * t.row + 2 * lane * (int)sizeof(E);
+    if constexpr (sizeof(E) == 2) {
+        *reinterpret_cast<uint32_t*>(at) = pack_bf16(x, y);
+    } else {
+        reinterpret_cast<float*>(at)[0] = x;
+        reinterpret_cast<float*>(at)[1] = y;
+    }
+}
+__device__ __forceinline__ float wave_dot(const Pair& a, const Pair& b) {
+    float s = a.x * b.x + a.y * b.y;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    return s;
+}
+// The probability of key j for row i of one head, and the cap's slope.
+template <typename E, int MODE>
+__device__ __forceinline__ float one_probability(const AttnArgs& a, const Pair& q, const Pair& k, float slope, int i, int j,
+                                                 float lse2, float& cap_slope) {
+    const float s = wave_dot(q, k);
+    float z;
+    cap_slope = 1.f;
+    scores<E, MODE, 1>(a.sc, &s, &z, MODE & kCap ? &cap_slope : nullptr);
+    if constexpr (MODE & kBias) z = fmaf(-slope, fabsf((float)((int64_t)i + a.off - j)), z);
+    return exp_score<MODE>(a.sc, z, lse2);
+}
+
 // What bounds it: the matrix cores and the exponentials, about evenly, at long rows.
 template <typename E, int DP, int MODE>
 __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
@@ -199,19 +267,37 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
     }
 
     l = sum_halves(l);
-    if (row >= a.Tq) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    char* op = a.o.ptr + w.head * a.o.head + (int64_t)row * a.o.row;
+    uint32_t again = rows_of(row < a.Tq && !(zero_of(acc, 0.f) == 0.f));
+    if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
+        char* op = a.o.ptr + w.head * a.o.head + (int64_t)row * a.o.row;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = 32 * d + 8 * i + 4 * h;
-            if (e < a.D)
-                store4<E>(op + e * ES, acc[d][4 * i] * inv, acc[d][4 * i + 1] * inv, acc[d][4 * i + 2] * inv,
-                          acc[d][4 * i + 3] * inv);
+            for (int i = 0; i < 4; ++i) {
+                const int e = 32 * d + 8 * i + 4 * h;
+                if (e < a.D)
+                    store4<E>(op + e * ES, acc[d][4 * i] * inv, acc[d][4 * i + 1] * inv, acc[d][4 * i + 2] * inv,
+                              acc[d][4 * i + 3] * inv);
+            }
+    }
+    const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+    if (h == 0 && row < a.Tq) a.lse[(int64_t)w.head * a.Tq + row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+    for (; again; again &= again - 1) {
+        const int r = __builtin_ctz(again), i = row0 + 32 * wave + r;
+        const int lo = __shfl(own.lo, r), hi = __shfl(own.hi, r);
+        const float from = __shfl(lse2, r);
+        const Pair qi = load_pair<E>(a.q, w.head, i, a.D, lane);
+        Pair sum;
+        for (int j = lo; j < hi; ++j) {
+            float unused;
+            const float p = one_probability<E, MODE>(a, qi, load_pair<E>(a.k, kv, j, a.D, lane), slope, i, j, from, unused);
+            const Pair v = load_pair<E>(a.v, kv, j, a.D, lane);
+            sum.x += p * v.x;
+            sum.y += p * v.y;
         }
-    if (h == 0) a.lse[(int64_t)w.head * a.Tq + row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+        store_pair<E>(a.o, w.head, i, a.D, lane, sum.x, sum.y);
+    }
 }
 
 // The sum over eight elements of two fragments' products.
@@ -349,17 +435,35 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
         }
     }
 
-    if (row >= a.Tq) return;
-    char* op = a.dq.ptr + w.head * a.dq.head + (int64_t)row * a.dq.row;
+    uint32_t again = rows_of(row < a.Tq && !(zero_of(acc, 0.f) == 0.f));
+    if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
+        char* op = a.dq.ptr + w.head * a.dq.head + (int64_t)row * a.dq.row;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = 32 * d + 8 * i + 4 * h;
-            if (e < a.D)
-                store4<E>(op + e * ES, acc[d][4 * i] * a.scale, acc[d][4 * i + 1] * a.scale, acc[d][4 * i + 2] * a.scale,
-                          acc[d][4 * i + 3] * a.scale);
+            for (int i = 0; i < 4; ++i) {
+                const int e = 32 * d + 8 * i + 4 * h;
+                if (e < a.D)
+                    store4<E>(op + e * ES, acc[d][4 * i] * a.scale, acc[d][4 * i + 1] * a.scale,
+                              acc[d][4 * i + 2] * a.scale, acc[d][4 * i + 3] * a.scale);
+            }
+    }
+    for (; again; again &= again - 1) {
+        const int r = __builtin_ctz(again), i = row0 + 32 * wave + r;
+        const int lo = __shfl(own.lo, r), hi = __shfl(own.hi, r);
+        const float from = __shfl(lse2, r), less = __shfl(delta, r);
+        const Pair qi = load_pair<E>(a.q, w.head, i, a.D, lane), gi = load_pair<E>(a.g, w.head, i, a.D, lane);
+        Pair sum;
+        for (int j = lo; j < hi; ++j) {
+            float cap_slope;
+            const Pair k = load_pair<E>(a.k, kv, j, a.D, lane);
+            const float p = one_probability<E, MODE>(a, qi, k, slope, i, j, from, cap_slope);
+            const float dz = p * (wave_dot(gi, load_pair<E>(a.v, kv, j, a.D, lane)) - less) * cap_slope * a.scale;
+            sum.x += dz * k.x;
+            sum.y += dz * k.y;
         }
+        store_pair<E>(a.dq, w.head, i, a.D, lane, sum.x, sum.y);
+    }
 }
 
 // The 64-row tiles of queries that see a workgroup's keys, in order, over the query heads that share the key head.
@@ -533,20 +637,44 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dkv_kernel(A
         }
     }
 
-    if (key >= a.Tk) return;
-    char* okp = a.dk.ptr + kv * a.dk.head + (int64_t)key * a.dk.row;
-    char* ovp = a.dv.ptr + kv * a.dv.head + (int64_t)key * a.dv.row;
+    uint32_t again = rows_of(key < a.Tk && !(zero_of(dv, zero_of(dk, 0.f)) == 0.f));
+    if (key < a.Tk && !((again >> (lane & 31)) & 1u)) {
+        char* okp = a.dk.ptr + kv * a.dk.head + (int64_t)key * a.dk.row;
+        char* ovp = a.dv.ptr + kv * a.dv.head + (int64_t)key * a.dv.row;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = 32 * d + 8 * i + 4 * h;
-            if (e < a.D) {
-                store4<E>(okp + e * ES, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale, dk[d][4 * i + 2] * a.scale,
-                          dk[d][4 * i + 3] * a.scale);
-                store4<E>(ovp + e * ES, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+            for (int i = 0; i < 4; ++i) {
+                const int e = 32 * d + 8 * i + 4 * h;
+                if (e < a.D) {
+                    store4<E>(okp + e * ES, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale, dk[d][4 * i + 2] * a.scale,
+                              dk[d][4 * i + 3] * a.scale);
+                    store4<E>(ovp + e * ES, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+                }
+            }
+    }
+    for (; again; again &= again - 1) {
+        const int j = wkey + __builtin_ctz(again);
+        const Pair kj = load_pair<E>(a.k, kv, j, a.D, lane), vj = load_pair<E>(a.v, kv, j, a.D, lane);
+        Pair sk, sv;
+        for (int head = kv * a.share; head < (kv + 1) * a.share; ++head) {
+            const float slope = MODE & kBias ? a.slopes[head] * kLog2e / a.sc.unit : 0.f;
+            for (int i = 0; i < a.Tq; ++i) {
+                if (j < a.row_lo[i] || j >= a.row_hi[i]) continue;
+                const int64_t at = (int64_t)head * a.Tpad + i;
+                float cap_slope;
+                const Pair q = load_pair<E>(a.q, head, i, a.D, lane), g = load_pair<E>(a.g, head, i, a.D, lane);
+                const float p = one_probability<E, MODE>(a, q, kj, slope, i, j, a.lse2[at], cap_slope);
+                const float dz = p * (wave_dot(g, vj) - a.delta[at]) * cap_slope * a.scale;
+                sv.x += p * g.x;
+                sv.y += p * g.y;
+                sk.x += dz * q.x;
+                sk.y += dz * q.y;
             }
         }
+        store_pair<E>(a.dk, kv, j, a.D, lane, sk.x, sk.y);
+        store_pair<E>(a.dv, kv, j, a.D, lane, sv.x, sv.y);
+    }
 }
 
 }  // namespace noble

@@ -170,6 +170,50 @@ def test_large_scores():
     check("lse", got["lse"], want["lse"], BF)
 
 
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (20.0, True)])
+def test_unseen_infinities_and_nan(dt, cap, bias):
+    """Rows of no document, and one document, hold infinities and NaN in every input: the other documents' results are
+    those of clean inputs, an empty row's are zero, and the one that sees them is not finite."""
+    T, H, K, D = 300, 4, 2, 64
+    print(f"[attn] nan {dt} {cap} {bias}", flush=True)
+    g = _gen(11)
+    starts = torch.tensor([3, 60, 61, 130, 131, 290], dtype=torch.int32, device="cuda")   # document 3 is row 130 alone
+    lo, hi, _ = na.noble_mask_rows(starts, T, causal=False)
+    q, k, v, do = (_rand(g, s, dt) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
+    slopes = _slopes(H) if bias else None
+    seen = dense_mask(T, T, lo.cpu(), hi.cpu())
+    want = attention(q, k, v, seen, softcap=cap, slopes=slopes, do=do)
+    bad = torch.zeros(T, dtype=torch.bool, device="cuda")
+    bad[:3] = bad[290:] = bad[130] = True
+    for n, t in enumerate((q, k, v, do)):
+        t[bad] = (math.nan, math.inf, -math.inf, math.nan)[n]
+    got = _run(q, k, v, do, lo.cpu(), hi.cpu(), slopes, softcap=cap)
+    ok = ~bad.cpu()
+    for n, t in got.items():
+        pick = (lambda x: x[:, ok]) if n == "lse" else (lambda x: x[ok])
+        check(n, pick(t.cpu()), tuple(map(pick, want[n])), dt)
+    empty = torch.cat([torch.arange(3), torch.arange(290, T)])
+    for n in ("o", "dq", "dk", "dv"):
+        assert bool((got[n][empty] == 0).all()), n
+        assert not got[n][130].isfinite().any(), n
+    assert bool((got["lse"][:, empty] == -math.inf).all())
+
+
+def test_one_nan_reaches_the_rows_that_see_it():
+    T, H, D = 200, 1, 128
+    g = _gen(12)
+    q, k, v, do = (_rand(g, (T, H, D), BF) for _ in range(4))
+    v[100, 0, 5] = math.nan
+    got = _run(q, k, v, do, None, None, None, causal=True)
+    assert got["o"][:100].isfinite().all() and got["o"][100:, 0, 5].isnan().all()
+    assert got["o"][100:, 0, :5].isfinite().all() and got["o"][100:, 0, 6:].isfinite().all()
+    assert got["dq"][:100].isfinite().all()
+    k[100, 0, 5], v[100, 0, 5] = math.inf, 0.0
+    got = _run(q, k, v, do, None, None, None, causal=True)
+    assert got["o"][:100].isfinite().all() and got["dq"][:100].isfinite().all()
+
+
 # ------------------------------------------------------- norm and rotation --
 
 ROPE = [
@@ -338,6 +382,23 @@ def test_append_and_paged_attention(c):
         seen = dense_mask(new, n, lo, at + 1)
         want = attention(queries[b * new:(b + 1) * new], *held, seen, softcap=cap, slopes=slopes)
         check("o", o[b * new:(b + 1) * new], want["o"], dt)
+
+
+def test_paged_window_leaves_older_slots_alone():
+    """Slots before the window hold NaN, as those of pages that a program has given away may."""
+    g = _gen(7)
+    page, D, n, window = 16, 64, 200, 37
+    cache = _rand(g, (16, 2, 2, page, D), BF)
+    table = torch.arange(13, dtype=torch.int32, device="cuda")[None]
+    q = _rand(g, (1, 4, D), BF)
+    t = torch.arange(n, device="cuda")
+    held = [cache[t // page, i, :, t % page] for i in (0, 1)]
+    want = attention(q, *(x[n - window:] for x in held), dense_mask(1, window))
+    old = torch.arange(n - window, device="cuda")
+    for i in (0, 1):
+        cache[old // page, i, :, old % page] = math.nan
+    o = na.noble_attn_paged(q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), window=window)
+    check("o", o, want["o"], BF)
 
 
 def test_paged_pages_outside_the_cache_are_not_seen():
