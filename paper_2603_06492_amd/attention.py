@@ -445,3 +445,181 @@ def noble_attn_paged(q, cache, page_table, lengths, slopes=None, *, scale: Optio
               None if scratch is None else scratch.data_ptr(), n.value, _stream(stream, dev))
     _used_on(stream, o)
     return o
+
+
+# ---------------------------------------------------------------- autograd --
+
+class QKRope(torch.autograd.Function):
+    """``noble_qk_rope_fwd`` and ``_bwd``: apply(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps,
+    interleaved) -> (q, k)."""
+
+    @staticmethod
+    def forward(ctx, qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps=1e-6, interleaved=False):
+        ctx.how = dict(heads=heads, kv_heads=kv_heads, eps=eps, interleaved=interleaved)
+        ctx.save_for_backward(qkv, q_weight, k_weight, cos, sin, positions)
+        return noble_qk_rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, **ctx.how)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        dqkv, dqw, dkw = noble_qk_rope_bwd(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, **ctx.how)
+        return (dqkv, dqw, dkw) + (None,) * 7
+
+
+class Attention(torch.autograd.Function):
+    """``noble_attn_fwd`` and ``_bwd``: apply(q, k, v, key_lo, key_hi, slopes, causal, scale, softcap) -> o.  The mask and
+    the slopes are constants."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, key_lo=None, key_hi=None, slopes=None, causal=False, scale=None, softcap=0.0):
+        ctx.how = dict(causal=causal, scale=scale, softcap=softcap)
+        o, lse = noble_attn_fwd(q, k, v, key_lo, key_hi, slopes, **ctx.how)
+        ctx.save_for_backward(q, k, v, o, lse, key_lo, key_hi, slopes)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        return noble_attn_bwd(do.contiguous(), *ctx.saved_tensors, **ctx.how) + (None,) * 6
+
+
+class RopeAttention(torch.autograd.Function):
+    """From the Q/K/V layer's rows to the O layer's: norm, rotation and attention, apply(qkv, q_weight, k_weight, cos, sin,
+    positions, key_lo, key_hi, slopes, heads, kv_heads, eps, interleaved, causal, scale, softcap) -> o [T, heads, D].  The
+    backward writes every part of dqkv in place, the values' by the attention, the others' by the rotation."""
+
+    @staticmethod
+    def forward(ctx, qkv, q_weight, k_weight, cos, sin, positions, key_lo, key_hi, slopes, heads, kv_heads, eps=1e-6,
+                interleaved=False, causal=False, scale=None, softcap=0.0):
+        ctx.rope = dict(heads=heads, kv_heads=kv_heads, eps=eps, interleaved=interleaved)
+        ctx.attn = dict(causal=causal, scale=scale, softcap=softcap)
+        q, k = noble_qk_rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, **ctx.rope)
+        o, lse = noble_attn_fwd(q, k, _values(qkv, k), key_lo, key_hi, slopes, **ctx.attn)
+        ctx.save_for_backward(qkv, q_weight, k_weight, cos, sin, positions, q, k, o, lse, key_lo, key_hi, slopes)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        qkv, q_weight, k_weight, cos, sin, positions, q, k, o, lse, *mask = ctx.saved_tensors
+        dqkv = torch.empty_like(qkv)
+        dq, dk, _ = noble_attn_bwd(do.contiguous(), q, k, _values(qkv, k), o, lse, *mask, dv=_values(dqkv, k), **ctx.attn)
+        _, dqw, dkw = noble_qk_rope_bwd(dq, dk, qkv, q_weight, k_weight, cos, sin, positions, dqkv=dqkv, **ctx.rope)
+        return (dqkv, dqw, dkw) + (None,) * 13
+
+
+def _values(qkv, k):
+    """The value columns of Q/K/V rows as [T, kv_heads, D]."""
+    T, K, D = k.shape
+    return qkv[:, qkv.shape[1] - K * D:].view(T, K, D)
+
+
+# ------------------------------------------------------------- paged cache --
+
+class PagedCache:
+    """Keys and values of a batch of sequences in pages of ``page`` tokens, for ``layers`` layers that share one page table
+    (``data[layer]`` is [pages, 2, kv_heads, page, head_dim]).  Which page belongs to which sequence is kept here."""
+
+    def __init__(self, sequences: int, longest: int, pages: int, *, kv_heads: int, head_dim: int, page: int = 16,
+                 layers: int = 1, dtype=torch.bfloat16, device="cuda"):
+        per = -(-longest // page)
+        self.page, self.longest = page, longest
+        self.data = [torch.empty((pages, 2, kv_heads, page, head_dim), dtype=dtype, device=device) for _ in range(layers)]
+        self.page_table = torch.full((sequences, per), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self._table = [[] for _ in range(sequences)]
+        self._held = [0] * sequences
+        self._free = list(range(pages - 1, -1, -1))
+
+    def extend(self, new: int):
+        """Room for ``new`` more tokens of every sequence: (positions int32, slots int64), both [sequences * new], a
+        sequence's tokens in a row.  Raises MemoryError when the pages run out and ValueError past ``longest``; nothing has
+        changed then."""
+        if max(self._held) + new > self.longest:
+            raise ValueError(f"sequences of up to {self.longest} tokens: {max(self._held)} held, {new} more")
+        need = [-(-(n + new) // self.page) - len(t) for n, t in zip(self._held, self._table)]
+        if sum(need) > len(self._free):
+            raise MemoryError(f"{sum(need)} more pages needed, {len(self._free)} free")
+        positions, slots = [], []
+        for b, pages in enumerate(self._table):
+            pages += [self._free.pop() for _ in range(need[b])]
+            at = range(self._held[b], self._held[b] + new)
+            positions += at
+            slots += [pages[t // self.page] * self.page + t % self.page for t in at]
+            self._held[b] += new
+        dev = self.lengths.device
+        if any(need):
+            per = self.page_table.shape[1]
+            self.page_table.copy_(torch.tensor([p + [-1] * (per - len(p)) for p in self._table], dtype=torch.int32))
+        self.lengths += new
+        return (torch.tensor(positions, dtype=torch.int32, device=dev),
+                torch.tensor(slots, dtype=torch.int64, device=dev))
+
+    def release(self, sequence: int) -> None:
+        """Gives a sequence's pages back; it holds no tokens then."""
+        self._free += reversed(self._table[sequence])
+        self._table[sequence], self._held[sequence] = [], 0
+        self.page_table[sequence] = -1
+        self.lengths[sequence] = 0
+
+
+# ------------------------------------------------------------------ module --
+
+class NobleSelfAttention(torch.nn.Module):
+    """The attention half of a transformer block: a NOBLE layer for Q, K and V (one call, a branch for each where the
+    widths allow it), norm and rotation of the heads, attention, and a NOBLE layer for O.  Parameters and initialisation
+    of the two layers are NobleLinear's; the norms' weights are float32 ones.
+
+    ``forward`` takes packed rows or a batch and trains; ``step`` serves prompts and single tokens from a PagedCache."""
+
+    def __init__(self, d: int, heads: int, r: int, *, kv_heads: Optional[int] = None, head_dim: Optional[int] = None,
+                 rot: Optional[int] = None, base: float = 10000.0, longest: int = 2048, scaling: Optional[dict] = None,
+                 norm: bool = True, eps: float = 1e-6, interleaved: bool = False, softcap: float = 0.0, alibi: bool = False,
+                 dtype=torch.bfloat16, device="cuda", seed: int = 0, **layer):
+        super().__init__()
+        self.heads, self.kv_heads = heads, heads if kv_heads is None else kv_heads
+        self.head_dim = d // heads if head_dim is None else head_dim
+        self.softcap, self.longest = softcap, longest
+        self.how = dict(heads=self.heads, kv_heads=self.kv_heads, eps=eps, interleaved=interleaved)
+        D = self.head_dim
+        self.qkv = noble.NobleLinear(d, (self.heads + 2 * self.kv_heads) * D, r, dtype=dtype, device=device, seed=seed,
+                                     groups=3 if self.heads == self.kv_heads and r else 1, **layer)
+        self.out = noble.NobleLinear(self.heads * D, d, r, dtype=dtype, device=device, seed=seed + 1, **layer)
+        ones = lambda: torch.nn.Parameter(torch.ones(D, device=device)) if norm else None  # noqa: E731
+        self.q_weight, self.k_weight = ones(), ones()
+        rot = D // 16 * 16 if rot is None else rot
+        cos, sin = noble_rope_table(longest, rot, base=base, device=device, **(scaling or {})) if rot else (None, None)
+        self.register_buffer("cos", cos, persistent=False)
+        self.register_buffer("sin", sin, persistent=False)
+        slopes = torch.tensor([2.0 ** (-8.0 * (h + 1) / heads) for h in range(heads)], device=device) if alibi else None
+        self.register_buffer("slopes", slopes, persistent=False)
+
+    def mask(self, starts, T: int, prefix=None, causal: bool = True, window: int = 0):
+        """The mask of packed rows, for every layer and step over them: noble_mask_rows."""
+        return noble_mask_rows(starts, T, prefix=prefix, causal=causal, window=window)
+
+    def forward(self, x, mask=None, causal: bool = True):
+        """x [T, d] (one sequence, or packed documents with their ``mask``) or [B, S, d]."""
+        shape = x.shape
+        x = x.reshape(-1, shape[-1])
+        T = x.shape[0]
+        if mask is None:
+            S = shape[-2]
+            mask = self.mask(torch.arange(0, T + 1, max(S, 1), dtype=torch.int32, device=x.device), T, causal=causal)
+        key_lo, key_hi, positions = mask
+        o = RopeAttention.apply(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, key_lo, key_hi,
+                                self.slopes, self.heads, self.kv_heads, self.how["eps"], self.how["interleaved"], False,
+                                None, self.softcap)
+        return self.out(o.reshape(T, -1)).reshape(shape)
+
+    @torch.no_grad()
+    def step(self, x, cache: PagedCache, positions, slots, layer: int = 0):
+        """The newest tokens of every sequence, x [sequences * new, d], with the positions and slots that
+        ``cache.extend(new)`` gave: their keys and values go into the cache, their attention runs over it.  A whole prompt
+        is a step too."""
+        q = noble_kv_append(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, slots,
+                            cache.data[layer], **self.how)
+        o = noble_attn_paged(q, cache.data[layer], cache.page_table, cache.lengths, self.slopes, softcap=self.softcap)
+        return self.out(o.reshape(x.shape[0], -1))
+
+    def param_groups(self, lr):
+        """Optimizer parameter groups: the two layers' learning-rate multipliers, the base rate for the norms."""
+        groups = self.qkv.param_groups(lr) + self.out.param_groups(lr)
+        return groups + ([{"params": [self.q_weight, self.k_weight], "lr": lr}] if self.q_weight is not None else [])
