@@ -134,7 +134,7 @@ noble_status check_attn(const noble_attn_desc* d) {
         return NOBLE_ERR_BAD_SHAPE;
     // every launch within one dispatch
     const int64_t longest = std::max(d->Tq, d->Tk);
-    if ((longest + kOwn - 1) / kOwn * d->heads > kMaxGroups256 - 64)
+    if ((longest + 31) / 32 * d->heads > kMaxGroups256 - 64)
         return NOBLE_ERR_BAD_SHAPE;
     return NOBLE_OK;
 }
@@ -197,6 +197,16 @@ AttnArgs attn_args(const noble_attn_desc* d, const int32_t* lo, const int32_t* h
     a.scale = d->scale;
     a.sc = score_args(d->scale, d->softcap);
     return a;
+}
+
+// Whether a launch over `rows` rows of `heads` heads runs split workgroups (TileShape): float32 always, bf16 as long as
+// workgroups of 128 rows are too few for the 256 CUs.  Split and not split (us), bf16, 8 heads over all keys, forward and
+// backward: heads of 128, 64 workgroups (1024 rows) 15.9 + 43 and 25.7 + 90, 128 workgroups 47.6 + 130 and 47.1 + 167, 192
+// workgroups 91.7 + 259 and 66.5 + 231; heads of 64, 128 workgroups 22.3 + 65 and 35.4 + 107, 192 workgroups 53.6 + 141 and
+// 51.2 + 142, 256 workgroups 71.7 + 205 and 66.1 + 197.
+template <typename E, int DP>
+bool split_rows(int64_t rows, int64_t heads) {
+    return sizeof(E) == 4 || cdiv(rows, kOwn) * heads < (DP == 64 ? 192 : 128);
 }
 
 // The backward's scratch: lse in units of log2 and delta [heads, Tq padded to tiles], the rows' intervals [Tq], their spans.
@@ -429,10 +439,12 @@ noble_status noble_attn_fwd(const noble_attn_desc* desc, const noble_heads* q, c
     a.v = head_rows(v, desc->dtype);
     a.o = head_rows(o, desc->dtype);
     a.lse = lse;
-    const unsigned groups = (unsigned)HeadOrder::grid(desc->kv_heads, (int64_t)cdiv(desc->Tq, kOwn) * a.share);
     return with_shape(desc->dtype, desc->head_dim, [&]<typename E, int DP>() {
         return with_mode(desc->softcap > 0.f, slopes != nullptr, [&]<int MODE>() {
-            return launch(attn_fwd_kernel<E, DP, MODE>, dim3(groups), dim3(256), (hipStream_t)stream, a);
+            const bool split = split_rows<E, DP>(desc->Tq, desc->heads);
+            const int64_t tiles = cdiv(desc->Tq, split ? 32 : kOwn);
+            return launch(split ? attn_fwd_kernel<E, DP, MODE, true> : attn_fwd_kernel<E, DP, MODE, sizeof(E) == 4>,
+                          dim3((unsigned)HeadOrder::grid(desc->kv_heads, tiles * a.share)), dim3(256), (hipStream_t)stream, a);
         });
     });
 }
@@ -476,12 +488,20 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
     a.row_hi = reinterpret_cast<int*>(s + ws.hi);
     a.span = reinterpret_cast<int4*>(s + ws.span);
     const hipStream_t st = (hipStream_t)stream;
-    const unsigned groups_q = (unsigned)HeadOrder::grid(desc->kv_heads, (int64_t)cdiv(desc->Tq, kOwn) * a.share);
-    const unsigned groups_k = (unsigned)HeadOrder::grid(desc->kv_heads, cdiv(desc->Tk, kOwn));
     return with_shape(desc->dtype, D, [&]<typename E, int DP>() {
         return with_mode(desc->softcap > 0.f, slopes != nullptr, [&]<int MODE>() {
-            if (desc->Tq > 0) NOBLE_TRY(launch(attn_dq_kernel<E, DP, MODE>, dim3(groups_q), dim3(256), st, a));
-            if (desc->Tk > 0) NOBLE_TRY(launch(attn_dkv_kernel<E, DP, MODE>, dim3(groups_k), dim3(256), st, a));
+            if (desc->Tq > 0) {
+                const bool split = split_rows<E, DP>(desc->Tq, desc->heads);
+                const int64_t tiles = cdiv(desc->Tq, split ? 32 : kOwn);
+                NOBLE_TRY(launch(split ? attn_dq_kernel<E, DP, MODE, true> : attn_dq_kernel<E, DP, MODE, sizeof(E) == 4>,
+                                 dim3((unsigned)HeadOrder::grid(desc->kv_heads, tiles * a.share)), dim3(256), st, a));
+            }
+            if (desc->Tk > 0) {
+                const bool split = split_rows<E, DP>(desc->Tk, desc->kv_heads);
+                const int64_t tiles = cdiv(desc->Tk, split ? 32 : kOwn);
+                NOBLE_TRY(launch(split ? attn_dkv_kernel<E, DP, MODE, true> : attn_dkv_kernel<E, DP, MODE, sizeof(E) == 4>,
+                                 dim3((unsigned)HeadOrder::grid(desc->kv_heads, tiles)), dim3(256), st, a));
+            }
             return NOBLE_OK;
         });
     });

@@ -36,6 +36,81 @@ struct AttnArgs {
 constexpr int kOwn = 128;   // rows of a workgroup: 32 for each of four waves
 constexpr int kPart = 64;   // partner rows of a tile
 
+// How a workgroup of four waves divides its work.  Each wave owns 32 rows of its own and all four share tiles of 64 partner
+// rows (two stages in LDS, a barrier a tile); or, split, the four share 32 own rows and take turns at tiles of 32
+// partner rows, each through stages of its own without a barrier, and their sums meet at the end.  Split workgroups are
+// four times as many with a quarter of the steps one after the other: for calls that do not fill the CUs, and for
+// float32, whose products are 16 times the bf16 ones' time and leave the reading of tiles out of account.
+template <typename E, int DP, bool SPLIT>
+struct TileShape {
+    static constexpr int OWN = SPLIT ? 32 : kOwn, PART = SPLIT ? 32 : kPart, U = PART / 32;
+    static constexpr int TB = Tile<E, DP>::bytes(PART), STAGE = 2 * TB;
+    static constexpr int STAGES = SPLIT && 8 * STAGE > 131072 ? 1 : 2;
+    static constexpr int LDS = (SPLIT ? 4 : 1) * STAGES * STAGE;
+    static constexpr int REQUESTS = STAGE / 1024;   // of a split wave and stage
+};
+
+// Where a wave's tiles are and when: the n-th of `count`.  request(n, address) asks for one; at(n) waits until it is there
+// and has the next one asked for; done(n) says that it has been read.
+template <typename E, int DP, bool SPLIT, typename Request>
+struct Tiles {
+    using S = TileShape<E, DP, SPLIT>;
+    char* lds;
+    int count;
+    const Request& request;
+    __device__ __forceinline__ Tiles(char* lds_, int wave, int count_, const Request& r)
+        : lds(SPLIT ? lds_ + wave * S::STAGES * S::STAGE : lds_), count(count_), request(r) {
+        if (count > 0) request(0, lds);
+    }
+    __device__ __forceinline__ int offset(int n) const { return S::STAGES == 2 ? (n & 1) * S::STAGE : 0; }
+    __device__ __forceinline__ void at(int n) const {
+        if constexpr (!SPLIT) {
+            arrive_all();
+            if (n + 1 < count) request(n + 1, lds + offset(n + 1));
+        } else {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other stage has been read
+            if (S::STAGES == 2 && n + 1 < count) {
+                request(n + 1, lds + offset(n + 1));
+                wait_vmcnt<S::REQUESTS>();
+            } else {
+                wait_vmcnt<0>();
+            }
+            asm volatile("" ::: "memory");
+        }
+    }
+    __device__ __forceinline__ void done(int n) const {
+        if constexpr (S::STAGES == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (n + 1 < count) request(n + 1, lds);
+        }
+    }
+};
+
+// The four waves' sums of the same 32 rows, acc of lane l's row l % 32, as [wave][32][DP + 4] float32 in LDS.
+template <int DP>
+struct Meeting {
+    static constexpr int LD = DP + 4, BYTES = 4 * 32 * LD * 4;
+    float* at;
+    int wave, lane;
+    __device__ __forceinline__ Meeting(char* lds, int wave_, int lane_)
+        : at(reinterpret_cast<float*>(lds)), wave(wave_), lane(lane_) {}
+    __device__ __forceinline__ void put(const f32x16 (&acc)[DP / 32], float x, float y) const {
+        float* p = at + (wave * 32 + (lane & 31)) * LD;
+        const int h = lane >> 5;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(p + 32 * d + 8 * i + 4 * h) =
+                    f32x4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+        if (h == 0) {
+            p[DP] = x;
+            p[DP + 1] = y;
+        }
+    }
+    __device__ __forceinline__ const float* get(int w, int row) const { return at + (w * 32 + row) * LD; }
+};
+
 // The keys that row i sees, within [0, Tk): {0, 0} for a row that sees none.
 __device__ __forceinline__ int2 row_interval(const AttnArgs& a, int i) {
     int lo = 0, hi = a.Tk;
@@ -57,8 +132,8 @@ __device__ __forceinline__ void raw(const f32x16& s, float* z) {
 struct OwnTile {
     int head = 0, tile = 0;
     bool work;
-    __device__ __forceinline__ OwnTile(const AttnArgs& a) {
-        const int tiles = (a.Tq + kOwn - 1) / kOwn;
+    __device__ __forceinline__ OwnTile(const AttnArgs& a, int rows) {
+        const int tiles = (a.Tq + rows - 1) / rows;
         int kv = 0, at = 0;
         work = HeadOrder{a.heads / a.share, tiles * a.share}.place(blockIdx.x, kv, at);
         head = kv * a.share + at % a.share;
@@ -73,20 +148,9 @@ struct OwnRows {
     int wave_lo, wave_hi;   // the keys that any row of the wave sees
     int full_lo, full_hi;   // the keys that every row of the wave sees
     int all_lo, all_hi;     // the keys that any row of the workgroup sees
-    __device__ __forceinline__ OwnRows(const AttnArgs& a, int row0, int wave, int lane) {
-        int least = INT32_MAX, most = 0;
-#pragma unroll
-        for (int k = 0; k < kOwn / 64; ++k) {
-            const int i = row0 + 64 * k + lane;
-            const int2 r = i < a.Tq ? row_interval(a, i) : int2{0, 0};
-            if (r.x < r.y) {
-                least = min(least, r.x);
-                most = max(most, r.y);
-            }
-        }
-        all_hi = wave_max(most);
-        all_lo = min(wave_min(least), all_hi);
-        const int i = row0 + 32 * wave + (lane & 31);
+    // `all`: also the workgroup's, which has the 128 rows from row0; the wave has the 32 from wave_row.
+    __device__ __forceinline__ OwnRows(const AttnArgs& a, int row0, int wave_row, bool all, int lane) {
+        const int i = wave_row + (lane & 31);
         const bool in = i < a.Tq;
         const int2 r = in ? row_interval(a, i) : int2{0, 0};
         lo = r.x;
@@ -96,6 +160,21 @@ struct OwnRows {
         // rows past the end do not count: their queries are zeros and nothing of them is stored
         full_lo = wave_max(in ? lo : 0);
         full_hi = wave_min(in ? hi : INT32_MAX);
+        all_lo = wave_lo;
+        all_hi = wave_hi;
+        if (!all) return;
+        int least = INT32_MAX, most = 0;
+#pragma unroll
+        for (int k = 0; k < kOwn / 64; ++k) {
+            const int n = row0 + 64 * k + lane;
+            const int2 t = n < a.Tq ? row_interval(a, n) : int2{0, 0};
+            if (t.x < t.y) {
+                least = min(least, t.x);
+                most = max(most, t.y);
+            }
+        }
+        all_hi = wave_max(most);
+        all_lo = min(wave_min(least), all_hi);
     }
 };
 
@@ -168,25 +247,28 @@ __device__ __forceinline__ float one_probability(const AttnArgs& a, const Pair& 
 }
 
 // What bounds it: the matrix cores and the exponentials, about evenly, at long rows.
-template <typename E, int DP, int MODE>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
+template <typename E, int DP, int MODE, bool SPLIT>
+__global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
-    constexpr int ES = T::ES, TB = T::bytes(kPart), NS = DP / 16, ND = DP / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
+    using S = TileShape<E, DP, SPLIT>;
+    constexpr int ES = T::ES, TB = S::TB, NS = DP / 16, ND = DP / 32, U = S::U, PART = S::PART;
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const OwnTile w(a);
+    const OwnTile w(a, S::OWN);
     if (!w.work) return;
-    const int row0 = w.tile * kOwn, row = row0 + 32 * wave + (lane & 31), kv = w.head / a.share, db = a.D * ES;
-    const OwnRows own(a, row0, wave, lane);
+    const int row0 = w.tile * S::OWN, wave_row = SPLIT ? row0 : row0 + 32 * wave, row = wave_row + (lane & 31);
+    const int kv = w.head / a.share, db = a.D * ES;
+    const OwnRows own(a, row0, wave_row, !SPLIT, lane);
 
-    const auto request = [&](int t) {
-        char* dst = lds + (t & 1) * 2 * TB;
-        const int k0 = own.all_lo + t * kPart;
-        T::template request<4, kPart>(rows_desc(a.k, kv, k0, own.all_hi, db), dst, (int)a.k.row, db, wave, lane);
-        T::template request<4, kPart>(rows_desc(a.v, kv, k0, own.all_hi, db), dst + TB, (int)a.v.row, db, wave, lane);
+    const int tiles = (own.all_hi - own.all_lo + PART - 1) / PART;
+    const auto key_of = [&](int n) { return own.all_lo + (SPLIT ? 4 * n + wave : n) * PART; };
+    const auto request = [&](int n, char* dst) {
+        const int k0 = key_of(n), who = SPLIT ? 0 : wave;
+        constexpr int NW = SPLIT ? 1 : 4;
+        T::template request<NW, PART>(rows_desc(a.k, kv, k0, own.all_hi, db), dst, (int)a.k.row, db, who, lane);
+        T::template request<NW, PART>(rows_desc(a.v, kv, k0, own.all_hi, db), dst + TB, (int)a.v.row, db, who, lane);
     };
-    const int tiles = (own.all_hi - own.all_lo + kPart - 1) / kPart;
-    if (tiles > 0) request(0);
+    const Tiles<E, DP, SPLIT, decltype(request)> ts(lds, wave, SPLIT ? (tiles - wave + 3) >> 2 : tiles, request);
 
     Frag<E> q[NS];
     const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
@@ -201,41 +283,42 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
     float m = -INFINITY, l = 0.f;
-    const Reader<E, DP> rd(lds, lane);
+    const Reader<E, DP> rd(ts.lds, lane);
 
-    for (int t = 0; t < tiles; ++t) {
-        arrive_all();
-        if (t + 1 < tiles) request(t + 1);
-        const int k0 = own.all_lo + t * kPart;
-        if (k0 >= own.wave_hi || k0 + kPart <= own.wave_lo) continue;
-        const Reader<E, DP> at_tile = rd.at((t & 1) * 2 * TB);
-        float z[32];
-        f32x16 s[2];
+    for (int n = 0; n < ts.count; ++n) {
+        ts.at(n);
+        const int k0 = key_of(n);
+        if (!SPLIT && (k0 >= own.wave_hi || k0 + PART <= own.wave_lo)) continue;
+        const Reader<E, DP> at_tile = rd.at(ts.offset(n));
+        float z[16 * U];
+        f32x16 s[U];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int x = 0; x < NS; ++x)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) mma32x32(s[u], at_tile.along(x, 32 * u * T::RB), q[x]);
-        if constexpr (ES == 2) read_ahead<2 * NS, 1, 1, 4>();
+            for (int u = 0; u < U; ++u) mma32x32(s[u], at_tile.along(x, 32 * u * T::RB), q[x]);
+        if constexpr (ES == 2) read_ahead<U * NS, 1, 1, 4>();
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
             raw(s[u], z + 16 * u);
             scores<E, MODE, 16>(a.sc, z + 16 * u, z + 16 * u, nullptr);
             if constexpr (MODE & kBias) bias16(z + 16 * u, slope, (float)(k0 + 4 * h - at) + 32.f * u);
         }
-        if (k0 < own.full_lo || k0 + kPart > own.full_hi) {
+        if (k0 < own.full_lo || k0 + PART > own.full_hi) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < 16 * U; ++i) {
                 const int j = k0 + 8 * (i >> 2) + 4 * h + (i & 3);
                 z[i] = j >= own.lo && j < own.hi ? z[i] : -INFINITY;
             }
         }
         float top = z[0];
 #pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
+        for (int i = 1; i < 16 * U; ++i) top = fmaxf(top, z[i]);
         top = max_halves(top) * (MODE & kCap ? 1.f : a.sc.unit);
         // The maximum that the exponents are taken from need only be near: it follows once a row's own has grown by
         // 2^8, which leaves sums and products far inside their range, and most tiles leave acc as it is.
@@ -251,40 +334,82 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_fwd_kernel(A
         }
         const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16 * U; ++i) {
             z[i] = exp_score<MODE>(a.sc, z[i], from);
             l += z[i];
         }
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
+        for (int x = 0; x < 2 * U; ++x) {
             const Frag<E> p = to_frag<E>(z + 8 * x);
 #pragma unroll
             for (int d = 0; d < ND; ++d) mma32x32(acc[d], at_tile.across(d, TB + 16 * x * T::RB), p);
         }
-        if constexpr (ES == 2) read_ahead<4 * ND, 1, 2, 4>();
+        if constexpr (ES == 2) read_ahead<2 * U * ND, 1, 2, 4>();
         __builtin_amdgcn_s_setprio(0);
+        ts.done(n);
     }
 
     l = sum_halves(l);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint32_t again = rows_of(row < a.Tq && !(zero_of(acc, 0.f) == 0.f));
-    if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
-        char* op = a.o.ptr + w.head * a.o.head + (int64_t)row * a.o.row;
+    const bool ok = zero_of(acc, 0.f) == 0.f;
+    uint32_t again = rows_of(row < a.Tq && !ok);
+    if constexpr (!SPLIT) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
+            char* op = a.o.ptr + w.head * a.o.head + (int64_t)row * a.o.row;
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = 32 * d + 8 * i + 4 * h;
-                if (e < a.D)
-                    store4<E>(op + e * ES, acc[d][4 * i] * inv, acc[d][4 * i + 1] * inv, acc[d][4 * i + 2] * inv,
-                              acc[d][4 * i + 3] * inv);
+                for (int i = 0; i < 4; ++i) {
+                    const int e = 32 * d + 8 * i + 4 * h;
+                    if (e < a.D)
+                        store4<E>(op + e * ES, acc[d][4 * i] * inv, acc[d][4 * i + 1] * inv, acc[d][4 * i + 2] * inv,
+                                  acc[d][4 * i + 3] * inv);
+                }
+        }
+    } else {
+        const Meeting<DP> meet(lds, wave, lane);
+        static_assert(Meeting<DP>::BYTES + 16 <= S::LDS, "the sums fit the stages");
+        uint32_t* flags = reinterpret_cast<uint32_t*>(lds + Meeting<DP>::BYTES);
+        __syncthreads();   // the stages have been read
+        meet.put(acc, m, l);
+        if (lane == 0) flags[wave] = again;
+        __syncthreads();
+        again = flags[0] | flags[1] | flags[2] | flags[3];
+        // every lane's statistics of its row, over the waves
+        float top = -INFINITY, total = 0.f, f[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top = fmaxf(top, meet.get(x, lane & 31)[DP]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            total += meet.get(x, lane & 31)[DP + 1] * __builtin_amdgcn_exp2f(meet.get(x, lane & 31)[DP] - (top == -INFINITY ? 0.f : top));
+        m = top;
+        l = total;
+        for (int e = threadIdx.x; e < 32 * (DP / 4); e += 256) {
+            const int r = e / (DP / 4), d = e % (DP / 4) * 4;
+            float most = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) most = fmaxf(most, meet.get(x, r)[DP]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                f[x] = __builtin_amdgcn_exp2f(meet.get(x, r)[DP] - (most == -INFINITY ? 0.f : most));
+                sum += meet.get(x, r)[DP + 1] * f[x];
             }
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v += *reinterpret_cast<const f32x4*>(meet.get(x, r) + d) * f[x];
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            if (d < a.D && row0 + r < a.Tq && !((again >> r) & 1u))
+                store4<E>(a.o.ptr + w.head * a.o.head + (int64_t)(row0 + r) * a.o.row + d * ES, v[0] * inv, v[1] * inv,
+                          v[2] * inv, v[3] * inv);
+        }
+        again &= 0x11111111u << wave;   // a quarter of the rows for each wave
     }
     const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
-    if (h == 0 && row < a.Tq) a.lse[(int64_t)w.head * a.Tq + row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+    if (h == 0 && row < a.Tq && (!SPLIT || wave == 0))
+        a.lse[(int64_t)w.head * a.Tq + row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
     for (; again; again &= again - 1) {
-        const int r = __builtin_ctz(again), i = row0 + 32 * wave + r;
+        const int r = __builtin_ctz(again), i = wave_row + r;
         const int lo = __shfl(own.lo, r), hi = __shfl(own.hi, r);
         const float from = __shfl(lse2, r);
         const Pair qi = load_pair<E>(a.q, w.head, i, a.D, lane);
@@ -333,26 +458,30 @@ __device__ __forceinline__ void write_spans(const AttnArgs& a, int tile, int lan
 }
 
 // dq, and what the dk/dv launch after it reads: delta (do is here already, o is read once for it), lse in units of log2,
-// the rows' intervals and what 64 of them span.
-template <typename E, int DP, int MODE>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
+// the rows' intervals and what 64 of them span.  delta is do.o of the rounded o, plus what is left of sum p (dp - delta)
+// after the row's keys, which an exact one would make zero: so dk does not carry o's rounding.
+template <typename E, int DP, int MODE, bool SPLIT>
+__global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
-    constexpr int ES = T::ES, TB = T::bytes(kPart), NS = DP / 16, ND = DP / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
+    using S = TileShape<E, DP, SPLIT>;
+    constexpr int ES = T::ES, TB = S::TB, NS = DP / 16, ND = DP / 32, U = S::U, PART = S::PART;
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const OwnTile w(a);
+    const OwnTile w(a, S::OWN);
     if (!w.work) return;
-    const int row0 = w.tile * kOwn, row = row0 + 32 * wave + (lane & 31), kv = w.head / a.share, db = a.D * ES;
-    const OwnRows own(a, row0, wave, lane);
+    const int row0 = w.tile * S::OWN, wave_row = SPLIT ? row0 : row0 + 32 * wave, row = wave_row + (lane & 31);
+    const int kv = w.head / a.share, db = a.D * ES;
+    const OwnRows own(a, row0, wave_row, !SPLIT, lane);
 
-    const auto request = [&](int t) {
-        char* dst = lds + (t & 1) * 2 * TB;
-        const int k0 = own.all_lo + t * kPart;
-        T::template request<4, kPart>(rows_desc(a.k, kv, k0, own.all_hi, db), dst, (int)a.k.row, db, wave, lane);
-        T::template request<4, kPart>(rows_desc(a.v, kv, k0, own.all_hi, db), dst + TB, (int)a.v.row, db, wave, lane);
+    const int tiles = (own.all_hi - own.all_lo + PART - 1) / PART;
+    const auto key_of = [&](int n) { return own.all_lo + (SPLIT ? 4 * n + wave : n) * PART; };
+    const auto request = [&](int n, char* dst) {
+        const int k0 = key_of(n), who = SPLIT ? 0 : wave;
+        constexpr int NW = SPLIT ? 1 : 4;
+        T::template request<NW, PART>(rows_desc(a.k, kv, k0, own.all_hi, db), dst, (int)a.k.row, db, who, lane);
+        T::template request<NW, PART>(rows_desc(a.v, kv, k0, own.all_hi, db), dst + TB, (int)a.v.row, db, who, lane);
     };
-    const int tiles = (own.all_hi - own.all_lo + kPart - 1) / kPart;
-    if (tiles > 0) request(0);
+    const Tiles<E, DP, SPLIT, decltype(request)> ts(lds, wave, SPLIT ? (tiles - wave + 3) >> 2 : tiles, request);
 
     Frag<E> q[NS], g[NS];
     const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
@@ -374,12 +503,15 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
         delta = sum_halves(delta);
         const float lse = row < a.Tq ? a.lse[(int64_t)w.head * a.Tq + row] : -INFINITY;
         if (lse != -INFINITY) lse2 = lse * kLog2e;
-        if (h == 0 && row < a.Tpad) {
-            a.lse2[(int64_t)w.head * a.Tpad + row] = lse2;
-            a.delta[(int64_t)w.head * a.Tpad + row] = delta;
-        }
+        if (h == 0 && row < a.Tpad && (!SPLIT || wave == 0)) a.lse2[(int64_t)w.head * a.Tpad + row] = lse2;
     }
-    if (w.head == 0 && wave < kOwn / kPart) write_spans(a, w.tile * (kOwn / kPart) + wave, lane);
+    if (w.head == 0 && row0 % kPart == 0 && wave < (S::OWN + kPart - 1) / kPart) write_spans(a, row0 / kPart + wave, lane);
+    if (SPLIT && wave == 0 && h == 0 && row0 + 32 == a.Tpad - 32 && row0 + 32 >= a.Tq) {
+        // a last tile of 64 rows whose second half no workgroup owns
+        a.lse2[(int64_t)w.head * a.Tpad + row + 32] = INFINITY;
+        a.delta[(int64_t)w.head * a.Tpad + row + 32] = 0.f;
+    }
+    float rest = 0.f;   // sum of p (dp - delta): what delta lacks, o having been rounded
 
     f32x16 acc[ND];
 #pragma unroll
@@ -387,16 +519,15 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
-    const Reader<E, DP> rd(lds, lane);
-    for (int t = 0; t < tiles; ++t) {
-        arrive_all();
-        if (t + 1 < tiles) request(t + 1);
-        const int k0 = own.all_lo + t * kPart;
-        if (k0 >= own.wave_hi || k0 + kPart <= own.wave_lo) continue;
-        const Reader<E, DP> at_tile = rd.at((t & 1) * 2 * TB);
-        const bool part = k0 < own.full_lo || k0 + kPart > own.full_hi;
+    const Reader<E, DP> rd(ts.lds, lane);
+    for (int n = 0; n < ts.count; ++n) {
+        ts.at(n);
+        const int k0 = key_of(n);
+        if (!SPLIT && (k0 >= own.wave_hi || k0 + PART <= own.wave_lo)) continue;
+        const Reader<E, DP> at_tile = rd.at(ts.offset(n));
+        const bool part = k0 < own.full_lo || k0 + PART > own.full_hi;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -414,7 +545,6 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 dz[i] = exp_score<MODE>(a.sc, z[i], lse2) * (dp[i] - delta);
-                if constexpr (MODE & kCap) dz[i] *= cap_slope[i];
             }
             if (part) {
 #pragma unroll
@@ -422,6 +552,11 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
                     const int j = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
                     dz[i] = j >= own.lo && j < own.hi ? dz[i] : 0.f;
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                rest += dz[i];
+                if constexpr (MODE & kCap) dz[i] *= cap_slope[i];
             }
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -433,23 +568,50 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dq_kernel(At
             if constexpr (ES == 2) read_ahead<2 * ND, 1, 2, 4>();
             __builtin_amdgcn_s_setprio(0);
         }
+        ts.done(n);
     }
 
+    rest = sum_halves(rest);
     uint32_t again = rows_of(row < a.Tq && !(zero_of(acc, 0.f) == 0.f));
-    if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
-        char* op = a.dq.ptr + w.head * a.dq.head + (int64_t)row * a.dq.row;
+    if constexpr (!SPLIT) {
+        if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
+            char* op = a.dq.ptr + w.head * a.dq.head + (int64_t)row * a.dq.row;
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = 32 * d + 8 * i + 4 * h;
-                if (e < a.D)
-                    store4<E>(op + e * ES, acc[d][4 * i] * a.scale, acc[d][4 * i + 1] * a.scale,
-                              acc[d][4 * i + 2] * a.scale, acc[d][4 * i + 3] * a.scale);
-            }
+                for (int i = 0; i < 4; ++i) {
+                    const int e = 32 * d + 8 * i + 4 * h;
+                    if (e < a.D)
+                        store4<E>(op + e * ES, acc[d][4 * i] * a.scale, acc[d][4 * i + 1] * a.scale,
+                                  acc[d][4 * i + 2] * a.scale, acc[d][4 * i + 3] * a.scale);
+                }
+        }
+    } else {
+        const Meeting<DP> meet(lds, wave, lane);
+        static_assert(Meeting<DP>::BYTES + 16 <= S::LDS, "the sums fit the stages");
+        uint32_t* flags = reinterpret_cast<uint32_t*>(lds + Meeting<DP>::BYTES);
+        __syncthreads();   // the stages have been read
+        meet.put(acc, rest, 0.f);
+        if (lane == 0) flags[wave] = again;
+        __syncthreads();
+        again = flags[0] | flags[1] | flags[2] | flags[3];
+        rest = 0.f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) rest += meet.get(x, lane & 31)[DP];
+        for (int e = threadIdx.x; e < 32 * (DP / 4); e += 256) {
+            const int r = e / (DP / 4), d = e % (DP / 4) * 4;
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v += *reinterpret_cast<const f32x4*>(meet.get(x, r) + d);
+            if (d < a.D && row0 + r < a.Tq && !((again >> r) & 1u))
+                store4<E>(a.dq.ptr + w.head * a.dq.head + (int64_t)(row0 + r) * a.dq.row + d * ES, v[0] * a.scale,
+                          v[1] * a.scale, v[2] * a.scale, v[3] * a.scale);
+        }
+        again &= 0x11111111u << wave;   // a quarter of the rows for each wave
     }
+    if (h == 0 && row < a.Tpad && (!SPLIT || wave == 0)) a.delta[(int64_t)w.head * a.Tpad + row] = delta + rest;
     for (; again; again &= again - 1) {
-        const int r = __builtin_ctz(again), i = row0 + 32 * wave + r;
+        const int r = __builtin_ctz(again), i = wave_row + r;
         const int lo = __shfl(own.lo, r), hi = __shfl(own.hi, r);
         const float from = __shfl(lse2, r), less = __shfl(delta, r);
         const Pair qi = load_pair<E>(a.q, w.head, i, a.D, lane), gi = load_pair<E>(a.g, w.head, i, a.D, lane);
@@ -474,8 +636,8 @@ struct Partners {
     int k0, k1, w0, w1;      // the workgroup's keys, and the wave's
     int head = 0, base = -64, lane;
     uint64_t any = 0, mine = 0, full = 0;
-    __device__ __forceinline__ Partners(const AttnArgs& a, int key0, int wave_key, int wave_keys, int lane_)
-        : share(a.share), tiles((a.Tq + kPart - 1) / kPart), span(a.span), k0(key0), k1(min(key0 + kOwn, a.Tk)),
+    __device__ __forceinline__ Partners(const AttnArgs& a, int key0, int keys, int wave_key, int wave_keys, int lane_)
+        : share(a.share), tiles((a.Tq + kPart - 1) / kPart), span(a.span), k0(key0), k1(min(key0 + keys, a.Tk)),
           w0(wave_key), w1(min(wave_key + wave_keys, a.Tk)), lane(lane_) {}
     // The next (head, tile), and whether the wave's keys are seen by any or by all of its rows; false at the end.
     __device__ __forceinline__ bool next(int& hd, int& tile, bool& seen, bool& whole) {
@@ -505,40 +667,66 @@ struct Partners {
 // bf16 heads of 128: the two sums (128 registers), the keys (32), S and dP (32) and the operands read ahead leave no room
 // for the values in the 256 registers that a wave has when two share a SIMD, so the values are read from LDS for every
 // tile, and tiles are 32 rows, so that two workgroups fit a CU's LDS.
-template <typename E, int DP>
+template <typename E, int DP, bool SPLIT>
 struct DkvShape {
-    static constexpr bool VALUES_IN_LDS = sizeof(E) == 2 && DP == 128;
-    static constexpr int ROWS = VALUES_IN_LDS ? 32 : kPart;
+    static constexpr bool VALUES_IN_LDS = !SPLIT && sizeof(E) == 2 && DP == 128;
+    static constexpr int OWN = SPLIT ? 32 : kOwn, ROWS = VALUES_IN_LDS || SPLIT ? 32 : kPart;
     static constexpr int TB = Tile<E, DP>::bytes(ROWS), INFO = 4 * kPart * 4, STAGE = 2 * TB + INFO;
-    static constexpr int LDS = 2 * STAGE + (VALUES_IN_LDS ? Tile<E, DP>::bytes(kOwn) : 0);
+    static constexpr int STAGES = SPLIT && 8 * STAGE > 160 * 1024 ? 1 : 2;
+    static constexpr int LDS = (SPLIT ? 4 : 1) * STAGES * STAGE + (VALUES_IN_LDS ? Tile<E, DP>::bytes(kOwn) : 0);
+    static constexpr int REQUESTS = 2 * TB / 1024 + 4;   // of a split wave and stage
 };
 
-template <typename E, int DP, int MODE>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
+template <typename E, int DP, int MODE, bool SPLIT>
+__global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
-    using S = DkvShape<E, DP>;
+    using S = DkvShape<E, DP, SPLIT>;
     constexpr int ES = T::ES, TB = S::TB, NS = DP / 16, ND = DP / 32, ROWS = S::ROWS, STAGE = S::STAGE;
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     int kv = 0, key_tile = 0;   // the first keys (which the most rows see under a causal mask) first
-    if (!HeadOrder{a.heads / a.share, (a.Tk + kOwn - 1) / kOwn}.place(blockIdx.x, kv, key_tile)) return;
-    const int key0 = key_tile * kOwn, wkey = key0 + 32 * wave, key = wkey + (lane & 31), db = a.D * ES;
+    if (!HeadOrder{a.heads / a.share, (a.Tk + S::OWN - 1) / S::OWN}.place(blockIdx.x, kv, key_tile)) return;
+    const int key0 = key_tile * S::OWN, wkey = SPLIT ? key0 : key0 + 32 * wave, key = wkey + (lane & 31), db = a.D * ES;
 
-    Partners it(a, key0, wkey, 32, lane);
-    const auto request = [&](int stage, int gi, int r0) {
-        char* dst = lds + stage * STAGE;
-        const int head = kv * a.share + gi;
-        T::template request<4, ROWS>(rows_desc(a.q, head, r0, a.Tq, db), dst, (int)a.q.row, db, wave, lane);
-        T::template request<4, ROWS>(rows_desc(a.g, head, r0, a.Tq, db), dst + TB, (int)a.g.row, db, wave, lane);
-        const int64_t rh = (int64_t)head * a.Tpad + r0;
-        const void* src = wave == 0 ? static_cast<const void*>(a.lse2 + rh) : wave == 1 ? a.delta + rh :
-                          wave == 2 ? static_cast<const void*>(a.row_lo + r0) : a.row_hi + r0;
-        dma4(wave_desc(static_cast<const char*>(src), (int64_t)(wave < 2 ? ROWS : min(a.Tq - r0, ROWS)) * 4),
-             dst + 2 * TB + wave * kPart * 4, lane);
-    };
-    int gi = 0, tile = 0, sub = 0;   // sub: the part of ROWS rows of a 64-row tile
+    // Tiles of ROWS rows: of all waves, or every fourth one (`turn`) for each
+    Partners it(a, key0, S::OWN, wkey, 32, lane);
+    char* stages = SPLIT ? lds + wave * S::STAGES * STAGE : lds;
+    int gi = 0, tile = 0, sub = 0, turn = -1;   // sub: the part of ROWS rows of a 64-row tile
     bool seen = false, whole = false, more = it.next(gi, tile, seen, whole);
-    if (more) request(0, gi, tile * kPart);
+    const auto step = [&] {
+        if (++sub == kPart / ROWS || tile * kPart + sub * ROWS >= a.Tq) {
+            sub = 0;
+            more = it.next(gi, tile, seen, whole);
+        }
+    };
+    const auto advance = [&] {   // to this wave's next tile
+        if constexpr (!SPLIT) {
+            step();
+        } else {
+            const int steps = turn < 0 ? wave : 4;
+            turn = 0;
+            for (int x = 0; x < steps && more; ++x) step();
+        }
+    };
+    if constexpr (SPLIT) advance();
+    const auto request = [&](int stage) {
+        char* dst = stages + stage * STAGE;
+        const int head = kv * a.share + gi, r0 = tile * kPart + sub * ROWS;
+        constexpr int NW = SPLIT ? 1 : 4;
+        const int who = SPLIT ? 0 : wave;
+        T::template request<NW, ROWS>(rows_desc(a.q, head, r0, a.Tq, db), dst, (int)a.q.row, db, who, lane);
+        T::template request<NW, ROWS>(rows_desc(a.g, head, r0, a.Tq, db), dst + TB, (int)a.g.row, db, who, lane);
+        const int64_t rh = (int64_t)head * a.Tpad + r0;
+#pragma unroll
+        for (int x = 0; x < 4 / NW; ++x) {
+            const int n = SPLIT ? x : wave;
+            const void* src = n == 0 ? static_cast<const void*>(a.lse2 + rh) : n == 1 ? a.delta + rh :
+                              n == 2 ? static_cast<const void*>(a.row_lo + r0) : a.row_hi + r0;
+            dma4(wave_desc(static_cast<const char*>(src), (int64_t)(n < 2 ? ROWS : min(a.Tq - r0, ROWS)) * 4),
+                 dst + 2 * TB + n * kPart * 4, lane);
+        }
+    };
+    if (more) request(0);
     if constexpr (S::VALUES_IN_LDS)
         T::template request<4, kOwn>(rows_desc(a.v, kv, key0, a.Tk, db), lds + 2 * STAGE, (int)a.v.row, db, wave, lane);
 
@@ -558,24 +746,38 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dkv_kernel(A
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.f;
 
-    const Reader<E, DP> rd(lds, lane);
+    const Reader<E, DP> rd(stages, lane);
     const Reader<E, DP> values = rd.at(2 * STAGE + 32 * wave * T::RB);
+    if constexpr (SPLIT) {
+        // the keys' own loads: their wait must not take a stage's requests with it
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
     for (int n = 0; more; ++n) {
-        const int r0 = tile * kPart + sub * ROWS, head = kv * a.share + gi, stage = (n & 1) * STAGE;
+        const int r0 = tile * kPart + sub * ROWS, head = kv * a.share + gi;
+        const int stage = S::STAGES == 2 ? (n & 1) * STAGE : 0;
         const bool mine = seen, part = !whole;
-        arrive_all();
-        if (++sub == kPart / ROWS || tile * kPart + sub * ROWS >= a.Tq) {
-            sub = 0;
-            more = it.next(gi, tile, seen, whole);
+        if constexpr (!SPLIT) {
+            arrive_all();
+            advance();
+            if (more) request((n + 1) & 1);
+        } else {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other stage has been read
+            advance();
+            if (S::STAGES == 2 && more) {
+                request((n + 1) & 1);
+                wait_vmcnt<S::REQUESTS>();
+            } else {
+                wait_vmcnt<0>();
+            }
+            asm volatile("" ::: "memory");
         }
-        if (more) request((n + 1) & 1, gi, tile * kPart + sub * ROWS);
-        if (!mine) continue;
+        if (!SPLIT && !mine) continue;
         const float slope = MODE & kBias ? a.slopes[head] * kLog2e / a.sc.unit : 0.f;
 #pragma unroll 1
         for (int u = 0; u < ROWS / 32; ++u) {
             // 32 rows: S and dP, p, dv, dz, dk
             const Reader<E, DP> at = rd.at(stage + 32 * u * T::RB);
-            const char* rows = lds + stage + 2 * TB + 4 * (32 * u + 4 * h);   // lse2, delta, lo, hi of rows 4 h ..
+            const char* rows = stages + stage + 2 * TB + 4 * (32 * u + 4 * h);   // lse2, delta, lo, hi of rows 4 h ..
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -635,23 +837,53 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_dkv_kernel(A
             if constexpr (ES == 2) read_ahead<4 * ND, 1, 2, 3>();
             __builtin_amdgcn_s_setprio(0);
         }
+        if constexpr (S::STAGES == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (more) request(0);
+        }
     }
 
     uint32_t again = rows_of(key < a.Tk && !(zero_of(dv, zero_of(dk, 0.f)) == 0.f));
-    if (key < a.Tk && !((again >> (lane & 31)) & 1u)) {
-        char* okp = a.dk.ptr + kv * a.dk.head + (int64_t)key * a.dk.row;
-        char* ovp = a.dv.ptr + kv * a.dv.head + (int64_t)key * a.dv.row;
+    if constexpr (!SPLIT) {
+        if (key < a.Tk && !((again >> (lane & 31)) & 1u)) {
+            char* okp = a.dk.ptr + kv * a.dk.head + (int64_t)key * a.dk.row;
+            char* ovp = a.dv.ptr + kv * a.dv.head + (int64_t)key * a.dv.row;
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = 32 * d + 8 * i + 4 * h;
-                if (e < a.D) {
-                    store4<E>(okp + e * ES, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale, dk[d][4 * i + 2] * a.scale,
-                              dk[d][4 * i + 3] * a.scale);
-                    store4<E>(ovp + e * ES, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+                for (int i = 0; i < 4; ++i) {
+                    const int e = 32 * d + 8 * i + 4 * h;
+                    if (e < a.D) {
+                        store4<E>(okp + e * ES, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale,
+                                  dk[d][4 * i + 2] * a.scale, dk[d][4 * i + 3] * a.scale);
+                        store4<E>(ovp + e * ES, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+                    }
                 }
+        }
+    } else {
+        const Meeting<DP> meet(lds, wave, lane);
+        static_assert(Meeting<DP>::BYTES + 16 <= S::LDS, "the sums fit the stages");
+        uint32_t* flags = reinterpret_cast<uint32_t*>(lds + Meeting<DP>::BYTES);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const HeadRows& to = which ? a.dv : a.dk;
+            const float scale = which ? 1.f : a.scale;
+            __syncthreads();   // the stages, and then dk's sums, have been read
+            meet.put(which ? dv : dk, 0.f, 0.f);
+            if (which == 0 && lane == 0) flags[wave] = again;
+            __syncthreads();
+            if (which == 0) again = flags[0] | flags[1] | flags[2] | flags[3];
+            for (int e = threadIdx.x; e < 32 * (DP / 4); e += 256) {
+                const int r = e / (DP / 4), d = e % (DP / 4) * 4;
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v += *reinterpret_cast<const f32x4*>(meet.get(x, r) + d);
+                if (d < a.D && key0 + r < a.Tk && !((again >> r) & 1u))
+                    store4<E>(to.ptr + kv * to.head + (int64_t)(key0 + r) * to.row + d * ES, v[0] * scale, v[1] * scale,
+                              v[2] * scale, v[3] * scale);
             }
+        }
+        again &= 0x11111111u << wave;   // a quarter of the keys for each wave
     }
     for (; again; again &= again - 1) {
         const int j = wkey + __builtin_ctz(again);

@@ -67,6 +67,13 @@ CASES = [
     (520, 520, 2, 1, 128, "ragged", BF, 15.0, False),
     (70, 70, 2, 2, 64, "none", BF, 0.0, False),
     (1100, 1100, 2, 1, 128, "docs", BF, 0.0, False),
+    # enough workgroups of 128 rows for the form with its own rows for each wave
+    (300, 300, 96, 96, 128, "causal", BF, 0.0, False),
+    (260, 290, 96, 96, 64, "ragged", BF, 20.0, True),
+    (333, 333, 160, 80, 128, "docs", BF, 50.0, False),
+    (170, 170, 120, 120, 96, "prefix", BF, 0.0, True),
+    (150, 150, 128, 128, 40, "window", BF, 0.0, False),
+    (257, 257, 96, 96, 128, "none", BF, 0.0, False),
     (1, 1, 1, 1, 128, "full", F32, 0.0, False),
     (5, 200, 4, 2, 64, "causal", F32, 0.0, True),
     (65, 65, 2, 1, 128, "docs", F32, 25.0, True),
@@ -98,12 +105,17 @@ def test_attention(c):
         check(n, got[n], want[n], dt)
 
 
-@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
-def test_strides_and_broadcasts(dt):
+# the last: workgroups of 128 rows
+STRIDED = pytest.mark.parametrize("dt,H,K,D", [(BF, 4, 2, 64), (F32, 4, 2, 64), (BF, 96, 96, 64), (BF, 96, 96, 128)],
+                                  ids=["bf16", "f32", "bf16_wide64", "bf16_wide128"])
+
+
+@STRIDED
+def test_strides_and_broadcasts(dt, H, K, D):
     """q, k, v as columns of one buffer, heads outermost, and keys shared by expansion; gradients into columns of one
     buffer, whose other columns stay."""
-    T, H, K, D = 150, 4, 2, 64
-    print(f"[attn] strides {dt}", flush=True)
+    T = 150
+    print(f"[attn] strides {dt} {H} {K} {D}", flush=True)
     g = _gen(3)
     qkv = _rand(g, (T, (H + 2 * K) * D + 32), dt)
     q, k, v = (qkv[:, a * D:b * D].view(T, b - a, D) for a, b in ((0, H), (H, H + K), (H + K, H + 2 * K)))
@@ -148,8 +160,9 @@ def test_gradient_against_differences():
         assert abs(num - ana) <= 2e-3 * max(1.0, float(grads[n].norm())), (n, num, ana)
 
 
-def test_repeated_backward_is_bitwise_equal():
-    T, H, K, D = 700, 4, 2, 128
+@pytest.mark.parametrize("H,K", [(4, 2), (64, 32)])
+def test_repeated_backward_is_bitwise_equal(H, K):
+    T, D = 700, 128
     g = _gen(5)
     q, k, v, do = (_rand(g, s, BF) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
     lo, hi = _intervals("docs", T, T)
@@ -170,13 +183,13 @@ def test_large_scores():
     check("lse", got["lse"], want["lse"], BF)
 
 
-@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@STRIDED
 @pytest.mark.parametrize("cap,bias", [(0.0, False), (20.0, True)])
-def test_unseen_infinities_and_nan(dt, cap, bias):
+def test_unseen_infinities_and_nan(dt, H, K, D, cap, bias):
     """Rows of no document, and one document, hold infinities and NaN in every input: the other documents' results are
     those of clean inputs, an empty row's are zero, and the one that sees them is not finite."""
-    T, H, K, D = 300, 4, 2, 64
-    print(f"[attn] nan {dt} {cap} {bias}", flush=True)
+    T = 300
+    print(f"[attn] nan {dt} {H} {K} {D} {cap} {bias}", flush=True)
     g = _gen(11)
     starts = torch.tensor([3, 60, 61, 130, 131, 290], dtype=torch.int32, device="cuda")   # document 3 is row 130 alone
     lo, hi, _ = na.noble_mask_rows(starts, T, causal=False)
