@@ -164,18 +164,17 @@ typedef struct noble_attn_desc {
     int32_t reserved;     /* must be 0 */
 } noble_attn_desc;
 
-/* Scratch bytes of the two calls (either pointer may be NULL).  Contents need
- * no initialisation. */
-noble_status noble_attn_scratch_size(const noble_attn_desc* desc,
-                                     size_t* fwd_bytes, size_t* bwd_bytes);
-
 /* o [Tq, heads, D]; lse float32 [heads, Tq], dense. */
 noble_status noble_attn_fwd(const noble_attn_desc* desc, const noble_heads* q,
                             const noble_heads* k, const noble_heads* v,
                             const int32_t* key_lo, const int32_t* key_hi,
                             const float* slopes, const noble_heads* o,
-                            float* lse, void* scratch, size_t scratch_bytes,
-                            void* stream);
+                            float* lse, void* stream);
+
+/* Bytes of noble_attn_bwd's scratch, whose contents need no
+ * initialisation. */
+noble_status noble_attn_bwd_scratch_size(const noble_attn_desc* desc,
+                                         size_t* scratch_bytes);
 
 /* Gradients for the upstream gradient `grad` of o, from the forward's inputs,
  * o and lse.  dq, dk, dv are overwritten; a key head's gradients are the sums

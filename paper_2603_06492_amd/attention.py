@@ -70,8 +70,8 @@ _SIGNATURES = {
     "noble_qk_rope_bwd": [_P(noble_rope_desc)] + [_vp] * 12 + [_sz, _vp],
     "noble_kv_append": [_P(noble_rope_desc), _P(noble_cache_desc)] + [_vp] * 10,
     "noble_rope_table": [_P(noble_rope_scaling), _i64, _i32, _vp, _vp, _vp],
-    "noble_attn_scratch_size": [_P(noble_attn_desc), _P(_sz), _P(_sz)],
-    "noble_attn_fwd": [_P(noble_attn_desc), _hp, _hp, _hp, _vp, _vp, _vp, _hp, _vp, _vp, _sz, _vp],
+    "noble_attn_fwd": [_P(noble_attn_desc), _hp, _hp, _hp, _vp, _vp, _vp, _hp, _vp, _vp],
+    "noble_attn_bwd_scratch_size": [_P(noble_attn_desc), _P(_sz)],
     "noble_attn_bwd": [_P(noble_attn_desc), _hp, _hp, _hp, _hp, _hp, _vp, _vp, _vp, _vp, _hp, _hp, _hp, _vp, _sz, _vp],
     "noble_attn_paged_scratch_size": [_P(noble_paged_desc), _P(_sz)],
     "noble_attn_paged": [_P(noble_paged_desc), _hp, _vp, _vp, _vp, _vp, _hp, _vp, _sz, _vp],
@@ -110,7 +110,7 @@ def _native():
         spec.loader.exec_module(m)
         m.init(*(ctypes.cast(getattr(L, n), _vp).value for n in (
             "noble_qk_rope_fwd", "noble_qk_rope_bwd", "noble_qk_rope_scratch_size", "noble_kv_append", "noble_attn_fwd",
-            "noble_attn_bwd", "noble_attn_scratch_size", "noble_attn_paged", "noble_attn_paged_scratch_size")))
+            "noble_attn_bwd", "noble_attn_bwd_scratch_size", "noble_attn_paged", "noble_attn_paged_scratch_size")))
         _native_module = m
     return _native_module
 
@@ -377,13 +377,10 @@ def noble_attn_fwd(q, k, v, key_lo=None, key_hi=None, slopes=None, *, causal: bo
     shape = tuple(q.shape)
     o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
     lse = torch.empty(shape[1::-1], device=dev) if lse is None else lse
-    n = _sz(0)
-    _call("noble_attn_scratch_size", ctypes.byref(d), ctypes.byref(n), None)
-    scratch = _scratch(n.value, dev, stream) if n.value else None
     with _on(dev):
         _call("noble_attn_fwd", ctypes.byref(d), *map(ctypes.byref, heads), *mask,
               ctypes.byref(_heads(o, "o", q.dtype, dev, shape)), _tensor(lse, "lse", torch.float32, shape[1::-1], dev),
-              None if scratch is None else scratch.data_ptr(), n.value, _stream(stream, dev))
+              _stream(stream, dev))
     _used_on(stream, o, lse)
     return o, lse
 
@@ -402,7 +399,7 @@ def noble_attn_bwd(do, q, k, v, o, lse, key_lo=None, key_hi=None, slopes=None, *
     g, oo = _heads(do, "do", dt, dev, sq), _heads(o, "o", dt, dev, sq)
     outs = [_heads(t, n, dt, dev, s) for t, n, s in ((dq, "dq", sq), (dk, "dk", sk), (dv, "dv", sk))]
     n = _sz(0)
-    _call("noble_attn_scratch_size", ctypes.byref(d), None, ctypes.byref(n))
+    _call("noble_attn_bwd_scratch_size", ctypes.byref(d), ctypes.byref(n))
     scratch = _scratch(n.value, dev, stream)
     with _on(dev):
         _call("noble_attn_bwd", ctypes.byref(d), ctypes.byref(g), *map(ctypes.byref, heads), ctypes.byref(oo),

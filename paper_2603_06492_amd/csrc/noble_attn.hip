@@ -211,15 +211,15 @@ bool split_rows(int64_t rows, int64_t heads) {
 
 // The backward's scratch: lse in units of log2 and delta [heads, Tq padded to tiles], the rows' intervals [Tq], their spans.
 struct BwdScratch {
-    size_t lse2, delta, lo, hi, span, bytes;
+    size_t lse2, delta, lo, keys, span, bytes;
     static int64_t pad(int64_t rows) { return (rows + kPart - 1) / kPart * kPart; }
     explicit BwdScratch(const noble_attn_desc* d) {
         const size_t per_head = up256((size_t)d->heads * pad(d->Tq) * 4), per_row = up256((size_t)d->Tq * 4);
         lse2 = 0;
         delta = lse2 + per_head;
         lo = delta + per_head;
-        hi = lo + per_row;
-        span = hi + per_row;
+        keys = lo + per_row;
+        span = keys + per_row;
         bytes = span + up256((size_t)((d->Tq + kPart - 1) / kPart) * sizeof(int4));
     }
 };
@@ -412,16 +412,16 @@ noble_status noble_mask_rows(int64_t T, int64_t documents, const int32_t* starts
     return launch(mask_rows_kernel, dim3((unsigned)cdiv(T, 256)), dim3(256), (hipStream_t)stream, a);
 }
 
-noble_status noble_attn_scratch_size(const noble_attn_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes) {
+noble_status noble_attn_bwd_scratch_size(const noble_attn_desc* desc, size_t* scratch_bytes) {
     NOBLE_TRY(check_attn(desc));
-    if (fwd_bytes) *fwd_bytes = 0;
-    if (bwd_bytes) *bwd_bytes = BwdScratch(desc).bytes;
+    if (!scratch_bytes) return NOBLE_ERR_NULL_ARG;
+    *scratch_bytes = BwdScratch(desc).bytes;
     return NOBLE_OK;
 }
 
 noble_status noble_attn_fwd(const noble_attn_desc* desc, const noble_heads* q, const noble_heads* k,
                             const noble_heads* v, const int32_t* key_lo, const int32_t* key_hi, const float* slopes,
-                            const noble_heads* o, float* lse, void* scratch, size_t scratch_bytes, void* stream) {
+                            const noble_heads* o, float* lse, void* stream) {
     NOBLE_TRY(check_attn(desc));
     NOBLE_TRY(check_heads(q, desc->Tq, desc->heads, desc->head_dim, false));
     NOBLE_TRY(check_heads(k, desc->Tk, desc->kv_heads, desc->head_dim, false));
@@ -429,8 +429,6 @@ noble_status noble_attn_fwd(const noble_attn_desc* desc, const noble_heads* q, c
     NOBLE_TRY(check_heads(o, desc->Tq, desc->heads, desc->head_dim, true));
     NOBLE_TRY(check_mask(desc, key_lo, key_hi, slopes));
     NOBLE_TRY(need_array(lse, desc->Tq > 0, 4));
-    (void)scratch;
-    (void)scratch_bytes;
     NOBLE_TRY(check_device());
     if (desc->Tq == 0) return NOBLE_OK;
     AttnArgs a = attn_args(desc, key_lo, key_hi, slopes);
@@ -485,7 +483,7 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
     a.lse2 = reinterpret_cast<float*>(s + ws.lse2);
     a.delta = reinterpret_cast<float*>(s + ws.delta);
     a.row_lo = reinterpret_cast<int*>(s + ws.lo);
-    a.row_hi = reinterpret_cast<int*>(s + ws.hi);
+    a.row_keys = reinterpret_cast<int*>(s + ws.keys);
     a.span = reinterpret_cast<int4*>(s + ws.span);
     const hipStream_t st = (hipStream_t)stream;
     return with_shape(desc->dtype, D, [&]<typename E, int DP>() {

@@ -273,6 +273,13 @@ __device__ __forceinline__ void arrive_all() {
     asm volatile("" ::: "memory");
 }
 
+// The wave's own operands, loaded before a loop, are here.  By the builtin, which the compiler counts: without it, it waits
+// for them at their first use in every turn of the loop, and with them for the tile that was requested right before.
+__device__ __forceinline__ void operands_here() {
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+}
+
 // The larger (or the sum) of a value and that of lane ^ 32.
 __device__ __forceinline__ float max_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

@@ -127,8 +127,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
     for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    // queries first: their wait must not take the ring's requests with it
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    operands_here();
     int ahead = c0;   // next chunk to request
 #pragma unroll
     for (int s = 0; s < NST - 1; ++s) {

@@ -23,8 +23,8 @@ struct AttnArgs {
     float* lse;                  // [heads, Tq], natural logarithm
     float* lse2;                 // backward: lse log2 e, +inf for a row that sees nothing, and delta: [heads, Tpad]
     float* delta;
-    int* row_lo;                 // backward: the rows' intervals, and of each 64 rows the least and largest bounds
-    int* row_hi;
+    int* row_lo;                 // backward: the rows' first keys and numbers of keys, and of each 64 rows the bounds
+    int* row_keys;
     int4* span;
     int Tq, Tk, heads, share, D;   // share: query heads of a key head
     int Tpad;                      // Tq rounded up to a tile: rows past the end have probability zero in lse2
@@ -148,6 +148,8 @@ struct OwnRows {
     int wave_lo, wave_hi;   // the keys that any row of the wave sees
     int full_lo, full_hi;   // the keys that every row of the wave sees
     int all_lo, all_hi;     // the keys that any row of the workgroup sees
+    // j - lo, unsigned, is below this for the keys that the row sees
+    __device__ __forceinline__ uint32_t width() const { return (uint32_t)(hi - lo); }
     // `all`: also the workgroup's, which has the 128 rows from row0; the wave has the 32 from wave_row.
     __device__ __forceinline__ OwnRows(const AttnArgs& a, int row0, int wave_row, bool all, int lane) {
         const int i = wave_row + (lane & 31);
@@ -284,6 +286,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
     float m = -INFINITY, l = 0.f;
     const Reader<E, DP> rd(ts.lds, lane);
+    operands_here();
 
     for (int n = 0; n < ts.count; ++n) {
         ts.at(n);
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
 #pragma unroll
             for (int i = 0; i < 16 * U; ++i) {
                 const int j = k0 + 8 * (i >> 2) + 4 * h + (i & 3);
-                z[i] = j >= own.lo && j < own.hi ? z[i] : -INFINITY;
+                z[i] = (uint32_t)(j - own.lo) < own.width() ? z[i] : -INFINITY;
             }
         }
         float top = z[0];
@@ -450,7 +453,7 @@ __device__ __forceinline__ void write_spans(const AttnArgs& a, int tile, int lan
     const int2 r = in ? row_interval(a, i) : int2{0, 0};
     if (in) {
         a.row_lo[i] = r.x;
-        a.row_hi[i] = r.y;
+        a.row_keys[i] = r.y - r.x;
     }
     const int most = wave_max(r.y), least = min(wave_min(r.x < r.y ? r.x : INT32_MAX), most);
     const int from = wave_max(in ? r.x : 0), to = wave_min(in ? r.y : INT32_MAX);
@@ -520,14 +523,17 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a)
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
     const Reader<E, DP> rd(ts.lds, lane);
+    operands_here();
     for (int n = 0; n < ts.count; ++n) {
         ts.at(n);
         const int k0 = key_of(n);
         if (!SPLIT && (k0 >= own.wave_hi || k0 + PART <= own.wave_lo)) continue;
         const Reader<E, DP> at_tile = rd.at(ts.offset(n));
-        const bool part = k0 < own.full_lo || k0 + PART > own.full_hi;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            const int ku = k0 + 32 * u;
+            if (U > 1 && (ku >= own.wave_hi || ku + 32 <= own.wave_lo)) continue;
+            const bool part = ku < own.full_lo || ku + 32 > own.full_hi;
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -550,7 +556,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int j = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
-                    dz[i] = j >= own.lo && j < own.hi ? dz[i] : 0.f;
+                    dz[i] = (uint32_t)(j - own.lo) < own.width() ? dz[i] : 0.f;
                 }
             }
 #pragma unroll
@@ -721,7 +727,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
         for (int x = 0; x < 4 / NW; ++x) {
             const int n = SPLIT ? x : wave;
             const void* src = n == 0 ? static_cast<const void*>(a.lse2 + rh) : n == 1 ? a.delta + rh :
-                              n == 2 ? static_cast<const void*>(a.row_lo + r0) : a.row_hi + r0;
+                              n == 2 ? static_cast<const void*>(a.row_lo + r0) : a.row_keys + r0;
             dma4(wave_desc(static_cast<const char*>(src), (int64_t)(n < 2 ? ROWS : min(a.Tq - r0, ROWS)) * 4),
                  dst + 2 * TB + n * kPart * 4, lane);
         }
@@ -748,10 +754,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
 
     const Reader<E, DP> rd(stages, lane);
     const Reader<E, DP> values = rd.at(2 * STAGE + 32 * wave * T::RB);
-    if constexpr (SPLIT) {
-        // the keys' own loads: their wait must not take a stage's requests with it
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+    operands_here();
     for (int n = 0; more; ++n) {
         const int r0 = tile * kPart + sub * ROWS, head = kv * a.share + gi;
         const int stage = S::STAGES == 2 ? (n & 1) * STAGE : 0;
@@ -777,7 +780,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
         for (int u = 0; u < ROWS / 32; ++u) {
             // 32 rows: S and dP, p, dv, dz, dk
             const Reader<E, DP> at = rd.at(stage + 32 * u * T::RB);
-            const char* rows = stages + stage + 2 * TB + 4 * (32 * u + 4 * h);   // lse2, delta, lo, hi of rows 4 h ..
+            const char* rows = stages + stage + 2 * TB + 4 * (32 * u + 4 * h);   // lse2, delta, first key, keys of rows 4 h ..
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -804,10 +807,10 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4) {
                     const i32x4 lo = *reinterpret_cast<const i32x4*>(rows + 8 * kPart + 32 * i4);
-                    const i32x4 hi = *reinterpret_cast<const i32x4*>(rows + 12 * kPart + 32 * i4);
+                    const i32x4 keys = *reinterpret_cast<const i32x4*>(rows + 12 * kPart + 32 * i4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        p[4 * i4 + e] = key >= lo[e] && key < hi[e] ? p[4 * i4 + e] : -INFINITY;
+                        p[4 * i4 + e] = (uint32_t)(key - lo[e]) < (uint32_t)keys[e] ? p[4 * i4 + e] : -INFINITY;
                 }
             }
 #pragma unroll
@@ -892,7 +895,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
         for (int head = kv * a.share; head < (kv + 1) * a.share; ++head) {
             const float slope = MODE & kBias ? a.slopes[head] * kLog2e / a.sc.unit : 0.f;
             for (int i = 0; i < a.Tq; ++i) {
-                if (j < a.row_lo[i] || j >= a.row_hi[i]) continue;
+                if ((uint32_t)(j - a.row_lo[i]) >= (uint32_t)a.row_keys[i]) continue;
                 const int64_t at = (int64_t)head * a.Tpad + i;
                 float cap_slope;
                 const Pair q = load_pair<E>(a.q, head, i, a.D, lane), g = load_pair<E>(a.g, head, i, a.D, lane);

@@ -26,7 +26,7 @@ decltype(&noble_qk_rope_scratch_size) p_rope_size;
 decltype(&noble_kv_append) p_append;
 decltype(&noble_attn_fwd) p_attn_fwd;
 decltype(&noble_attn_bwd) p_attn_bwd;
-decltype(&noble_attn_scratch_size) p_attn_size;
+decltype(&noble_attn_bwd_scratch_size) p_bwd_size;
 decltype(&noble_attn_paged) p_paged;
 decltype(&noble_attn_paged_scratch_size) p_paged_size;
 
@@ -321,16 +321,12 @@ PyObject* attn_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Output o(c, a[10], {in.d.Tq, in.d.heads, in.d.head_dim}, c.sd), lse(c, a[11], {in.d.heads, in.d.Tq}, at::kFloat);
     const noble_heads oh = o.heads(c);
     float* pl = static_cast<float*>(lse.dense(c));
-    size_t bytes = 0;
-    if (!c.ok || p_attn_size(&in.d, &bytes, nullptr) != NOBLE_OK) Py_RETURN_NONE;
+    if (!c.ok) Py_RETURN_NONE;
     noble_status st;
     {
         NoGil nogil;
         const c10::DeviceGuard guard(c.dev);
-        at::Tensor scratch;
-        if (bytes) scratch = c.work(bytes);
-        st = p_attn_fwd(&in.d, &in.q, &in.k, &in.v, in.lo, in.hi, in.slopes, &oh, pl,
-                        bytes ? scratch.data_ptr() : nullptr, bytes, c.stream());
+        st = p_attn_fwd(&in.d, &in.q, &in.k, &in.v, in.lo, in.hi, in.slopes, &oh, pl, c.stream());
     }
     return st == NOBLE_OK ? tuple({&o.t, &lse.t}) : PyLong_FromLong(st);
     END_HANDLE_TH_ERRORS
@@ -349,7 +345,7 @@ PyObject* attn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Output dq(c, a[13], {Tq, H, D}, c.sd), dk(c, a[14], {Tk, K, D}, c.sd), dv(c, a[15], {Tk, K, D}, c.sd);
     const noble_heads hq = dq.heads(c), hk = dk.heads(c), hv = dv.heads(c);
     size_t bytes = 0;
-    if (!c.ok || a[2] == Py_None || p_attn_size(&in.d, nullptr, &bytes) != NOBLE_OK) Py_RETURN_NONE;
+    if (!c.ok || a[2] == Py_None || p_bwd_size(&in.d, &bytes) != NOBLE_OK) Py_RETURN_NONE;
     noble_status st;
     {
         NoGil nogil;
@@ -406,7 +402,7 @@ PyObject* paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// init(rope_fwd, rope_bwd, rope_scratch_size, append, attn_fwd, attn_bwd, attn_scratch_size, paged, paged_scratch_size):
+// init(rope_fwd, rope_bwd, rope_scratch_size, append, attn_fwd, attn_bwd, attn_bwd_scratch_size, paged, paged_scratch_size):
 // the library's entry points, as addresses.
 PyObject* init(PyObject*, PyObject* args) {
     unsigned long long p[9];
@@ -417,7 +413,7 @@ PyObject* init(PyObject*, PyObject* args) {
     p_append = reinterpret_cast<decltype(p_append)>(p[3]);
     p_attn_fwd = reinterpret_cast<decltype(p_attn_fwd)>(p[4]);
     p_attn_bwd = reinterpret_cast<decltype(p_attn_bwd)>(p[5]);
-    p_attn_size = reinterpret_cast<decltype(p_attn_size)>(p[6]);
+    p_bwd_size = reinterpret_cast<decltype(p_bwd_size)>(p[6]);
     p_paged = reinterpret_cast<decltype(p_paged)>(p[7]);
     p_paged_size = reinterpret_cast<decltype(p_paged_size)>(p[8]);
     Py_RETURN_NONE;

@@ -113,7 +113,7 @@ def _fwd(d, heads=None, lo=None, hi=None, lse=FAKE[5]):
     for i, new in (heads or {}).items():
         h[i] = new
     q, k, v, o = (None if x is None else REF(x) for x in h)
-    return na.lib().noble_attn_fwd(None if d is None else REF(d), q, k, v, lo, hi, None, o, lse, None, 0, None)
+    return na.lib().noble_attn_fwd(None if d is None else REF(d), q, k, v, lo, hi, None, o, lse, None)
 
 
 BAD_ATTN = [dict(Tq=-1), dict(Tk=2 ** 31), dict(offset=2 ** 31), dict(heads=0), dict(heads=3), dict(heads=2048),
@@ -123,9 +123,9 @@ BAD_ATTN = [dict(Tq=-1), dict(Tk=2 ** 31), dict(offset=2 ** 31), dict(heads=0), 
 
 @pytest.mark.parametrize("bad", BAD_ATTN, ids=str)
 def test_attention_shapes(bad):
-    a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    n = ctypes.c_size_t(0)
     assert _fwd(_attn(**bad)) == SHAPE
-    assert na.lib().noble_attn_scratch_size(REF(_attn(**bad)), REF(a), REF(b)) == SHAPE
+    assert na.lib().noble_attn_bwd_scratch_size(REF(_attn(**bad)), REF(n)) == SHAPE
 
 
 def test_attention_pointers_and_strides():
@@ -147,7 +147,7 @@ def test_attention_pointers_and_strides():
 def test_attention_backward_refusals():
     L, d = na.lib(), _attn()
     n = ctypes.c_size_t(0)
-    assert L.noble_attn_scratch_size(REF(d), None, REF(n)) == 0
+    assert L.noble_attn_bwd_scratch_size(REF(d), REF(n)) == 0
     assert n.value >= 2 * 4 * 4 * 30   # lse and delta of four heads
     def bwd(swap=None, lse=FAKE[10], scratch=FAKE[11], size=n.value):
         # grad, q, k, v, o, dq, dk, dv
