@@ -290,15 +290,23 @@ __device__ __forceinline__ float sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The least or largest of a wave's values, by row shifts and broadcasts (in lane 63 at the end): six dependent VALU
+// operations, where six exchanges through LDS take ten times as long and stand before a kernel's first request.
+template <typename F>
+__device__ __forceinline__ int wave_fold(int x, int none, F f) {
+    x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));   // row_shr:1, 2, 4, 8
+    x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));   // row_bcast:15 into rows 1 and 3
+    x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));   // row_bcast:31 into rows 2 and 3
+    return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x = min(x, __shfl_xor(x, o));
-    return __builtin_amdgcn_readfirstlane(x);
+    return wave_fold(x, INT32_MAX, [](int a, int b) { return min(a, b); });
 }
 __device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x = max(x, __shfl_xor(x, o));
-    return __builtin_amdgcn_readfirstlane(x);
+    return wave_fold(x, INT32_MIN, [](int a, int b) { return max(a, b); });
 }
 
 // Workgroups run round robin over the 8 XCDs, each with an L2 of its own.  Key heads are dealt to XCDs so that the

@@ -260,6 +260,10 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
     if (!w.work) return;
     const int row0 = w.tile * S::OWN, wave_row = SPLIT ? row0 : row0 + 32 * wave, row = wave_row + (lane & 31);
     const int kv = w.head / a.share, db = a.D * ES;
+    Frag<E> q[NS];
+    const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = global_frag<E>(qp + 16 * s * ES, row < a.Tq && 16 * s + 8 * h < a.D);
     const OwnRows own(a, row0, wave_row, !SPLIT, lane);
 
     const int tiles = (own.all_hi - own.all_lo + PART - 1) / PART;
@@ -272,10 +276,6 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
     };
     const Tiles<E, DP, SPLIT, decltype(request)> ts(lds, wave, SPLIT ? (tiles - wave + 3) >> 2 : tiles, request);
 
-    Frag<E> q[NS];
-    const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) q[s] = global_frag<E>(qp + 16 * s * ES, row < a.Tq && 16 * s + 8 * h < a.D);
     const float slope = MODE & kBias ? a.slopes[w.head] * kLog2e / a.sc.unit : 0.f;
     const int at = row + a.off;
 
@@ -474,6 +474,15 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a)
     if (!w.work) return;
     const int row0 = w.tile * S::OWN, wave_row = SPLIT ? row0 : row0 + 32 * wave, row = wave_row + (lane & 31);
     const int kv = w.head / a.share, db = a.D * ES;
+    Frag<E> q[NS], g[NS];
+    const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
+    const char* gp = a.g.ptr + w.head * a.g.head + (int64_t)row * a.g.row + 8 * h * ES;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const bool ok = row < a.Tq && 16 * s + 8 * h < a.D;
+        q[s] = global_frag<E>(qp + 16 * s * ES, ok);
+        g[s] = global_frag<E>(gp + 16 * s * ES, ok);
+    }
     const OwnRows own(a, row0, wave_row, !SPLIT, lane);
 
     const int tiles = (own.all_hi - own.all_lo + PART - 1) / PART;
@@ -486,15 +495,6 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a)
     };
     const Tiles<E, DP, SPLIT, decltype(request)> ts(lds, wave, SPLIT ? (tiles - wave + 3) >> 2 : tiles, request);
 
-    Frag<E> q[NS], g[NS];
-    const char* qp = a.q.ptr + w.head * a.q.head + (int64_t)row * a.q.row + 8 * h * ES;
-    const char* gp = a.g.ptr + w.head * a.g.head + (int64_t)row * a.g.row + 8 * h * ES;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        const bool ok = row < a.Tq && 16 * s + 8 * h < a.D;
-        q[s] = global_frag<E>(qp + 16 * s * ES, ok);
-        g[s] = global_frag<E>(gp + 16 * s * ES, ok);
-    }
     const float slope = MODE & kBias ? a.slopes[w.head] * kLog2e / a.sc.unit : 0.f;
     const int at = row + a.off;
     float delta = 0.f, lse2 = INFINITY;
