@@ -154,8 +154,8 @@ noble_status noble_kv_append(const noble_rope_desc* desc,
  * reach the rows that see them and no other (such rows, and those beside
  * them, are slow). */
 typedef struct noble_attn_desc {
-    int64_t Tq, Tk;       /* rows of q, and of k and v: up to 2^31 - 4096 */
-    int64_t offset;       /* key index of query row 0, |offset| < 2^31 - 4096 */
+    int64_t Tq, Tk;       /* rows of q, and of k and v: up to 2^30 - 4096 */
+    int64_t offset;       /* key index of query row 0, |offset| <= 2^30 - 4096 */
     int32_t heads, kv_heads, head_dim;
     int32_t dtype;        /* noble_dtype */
     int32_t causal;

@@ -18,6 +18,7 @@ using namespace noble;
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 4096;
+constexpr int64_t kMaxAttnRows = (int64_t(1) << 30) - 4096;   // and offsets: the kernels' row and key numbers are 32 bits
 constexpr int64_t kMaxRowStride = int64_t(1) << 22;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 constexpr int64_t kMaxGroups256 = (int64_t)UINT32_MAX / 256;   // workgroups of 256 that one dispatch holds
@@ -126,8 +127,8 @@ int rope_bwd_groups(const noble_rope_desc* d) {
 noble_status check_attn(const noble_attn_desc* d) {
     if (!d) return NOBLE_ERR_NULL_ARG;
     if (!dtype_ok(d->dtype)) return NOBLE_ERR_BAD_DTYPE;
-    if (d->reserved != 0 || d->Tq < 0 || d->Tq > kMaxRows || d->Tk < 0 || d->Tk > kMaxRows) return NOBLE_ERR_BAD_SHAPE;
-    if (d->offset <= -kMaxRows || d->offset >= kMaxRows) return NOBLE_ERR_BAD_SHAPE;
+    if (d->reserved != 0 || d->Tq < 0 || d->Tq > kMaxAttnRows || d->Tk < 0 || d->Tk > kMaxAttnRows) return NOBLE_ERR_BAD_SHAPE;
+    if (d->offset < -kMaxAttnRows || d->offset > kMaxAttnRows) return NOBLE_ERR_BAD_SHAPE;
     if (d->heads < 1 || d->heads > kMaxHeads || d->kv_heads < 1 || d->heads % d->kv_heads) return NOBLE_ERR_BAD_SHAPE;
     if (!head_dim_ok(d->head_dim)) return NOBLE_ERR_BAD_SHAPE;
     if (!(d->scale > 0.f) || !std::isfinite(d->scale) || !(d->softcap >= 0.f) || !std::isfinite(d->softcap))

@@ -7,7 +7,9 @@
 // The 16 rows are the columns of 16x16x32 MFMAs, so one read of a key serves every query head that shares it.
 // Pieces of one sequence are joined by attn_join_kernel, in their order.
 //
-// What bounds it: reading the cache, once.
+// What bounds it: reading the cache, once.  64 sequences of 16384 to 32768 tokens, 16 heads of 128 over 4 key heads: 3.2 GB
+// in 506 us, 6.4 TB/s; 16 sequences of 130 to 8192 tokens, 16 key heads: 0.55 GB in 108 us, 5.0 TB/s.  One token over 1000
+// keys takes 6 us and 3 for the join: the latencies of lengths, page table, cache and partial results in a row.
 #pragma once
 
 #include "noble_attn_common.hpp"
