@@ -198,8 +198,7 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
  * outside the cache is not seen; nor is, for a row of a token before the
  * first, anything, which gives zeros.  Scores as in noble_attn_fwd.  Slots
  * past a sequence's tokens, and before every row's window, may hold anything;
- * an infinite or NaN value of a new token may also reach the sequence's new
- * tokens before it. */
+ * infinite and NaN values reach the rows that see them, and no others. */
 typedef struct noble_paged_desc {
     int64_t B;
     int64_t table_row;    /* entries of one sequence's page table */

@@ -204,7 +204,9 @@ AttnArgs attn_args(const noble_attn_desc* d, const int32_t* lo, const int32_t* h
 // workgroups of 128 rows are too few for the 256 CUs.  Split and not split (us), bf16, 8 heads over all keys, forward and
 // backward: heads of 128, 64 workgroups (1024 rows) 15.9 + 43 and 25.7 + 90, 128 workgroups 47.6 + 130 and 47.1 + 167, 192
 // workgroups 91.7 + 259 and 66.5 + 231; heads of 64, 128 workgroups 22.3 + 65 and 35.4 + 107, 192 workgroups 53.6 + 141 and
-// 51.2 + 142, 256 workgroups 71.7 + 205 and 66.1 + 197.
+// 51.2 + 142, 256 workgroups 71.7 + 205 and 66.1 + 197.  Float32, the same way and with the same tiles of 32 rows for
+// both: heads of 64, 8 x 2048 rows 94 + 291 and 165 + 505, 8 x 4096 rows 347 + 1101 and 319 + 1002, 16 x 4096 rows 691 +
+// 2195 and 534 + 1771; heads of 128, 8 x 4096 rows 617 + 2196 and 658 + 2288, 24 x 5516 rows 3496 + 12661 and 3781 + 16351.
 template <typename E, int DP>
 bool split_rows(int64_t rows, int64_t heads) {
     return sizeof(E) == 4 || cdiv(rows, kOwn) * heads < (DP == 64 ? 192 : 128);
@@ -554,8 +556,8 @@ noble_status noble_attn_paged(const noble_paged_desc* desc, const noble_heads* q
     const hipStream_t st = (hipStream_t)stream;
     return with_shape(desc->dtype, desc->head_dim, [&]<typename E, int DP>() {
         NOBLE_TRY(with_mode(desc->softcap > 0.f, slopes != nullptr, [&]<int MODE>() {
-            return launch(attn_paged_kernel<E, DP, MODE>, dim3((unsigned)plan.groups),
-                          dim3(64 * PagedShape<E, DP>::WAVES), st, a);
+            return launch(a.fresh > 1 ? attn_paged_kernel<E, DP, MODE, true> : attn_paged_kernel<E, DP, MODE, false>,
+                          dim3((unsigned)plan.groups), dim3(64 * PagedShape<E, DP>::WAVES), st, a);
         }));
         if (plan.pieces == 1) return NOBLE_OK;
         const JoinArgs j{a, rows * desc->heads};

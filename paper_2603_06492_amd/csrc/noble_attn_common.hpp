@@ -52,6 +52,32 @@ __device__ __forceinline__ void mma16x16(f32x4& c, const Frag<float>& a, const F
                                                  c, 0, 0, 0);
 }
 
+// Whether any element is infinite or NaN: its exponent's bits are all ones.
+__device__ __forceinline__ bool not_finite(const Frag<uint16_t>& f) {
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) odd |= (f.v[j] & 0x7f800000u) == 0x7f800000u || (f.v[j] & 0x7f80u) == 0x7f80u;
+    return odd;
+}
+__device__ __forceinline__ bool not_finite(const Frag<float>& f) {
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) odd |= (f.v[j >> 2][j & 3] & 0x7f800000u) == 0x7f800000u;
+    return odd;
+}
+// The elements whose bits are set; the others as zeros.
+__device__ __forceinline__ Frag<uint16_t> only(Frag<uint16_t> f, uint32_t set) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        f.v[j] &= (set >> (2 * j) & 1u ? 0xffffu : 0u) | (set >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+    return f;
+}
+__device__ __forceinline__ Frag<float> only(Frag<float> f, uint32_t set) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = set >> j & 1u ? f.v[j >> 2][j & 3] : 0u;
+    return f;
+}
+
 // Two float32 values as bf16 in one register, rounded to nearest even.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -414,6 +414,35 @@ def test_paged_window_leaves_older_slots_alone():
     check("o", o, want["o"], BF)
 
 
+@pytest.mark.parametrize("dt,D", [(BF, 64), (BF, 128), (F32, 96)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_paged_nan_reaches_the_tokens_that_see_it(dt, D, window):
+    """Several new tokens in one tile of rows, and tokens at their windows' starts: each token's result is that of the
+    tokens it sees, as a call without the others gives it."""
+    print(f"[paged] nan {dt} {D} {window}", flush=True)
+    g = _gen(11)
+    page, n, new, H, K = 16, 150, 6, 4, 2
+    cache = _rand(g, (12, 2, K, page, D), dt)
+    table = torch.arange(10, dtype=torch.int32, device="cuda")[None] + 1
+    q = _rand(g, (new, H, D), dt)
+    slot = lambda t: (int(table[0, t // page]), t % page)  # noqa: E731
+    marks = [(n - 2, 1, math.nan), (n - 4, 0, math.inf)] + ([(n - new - window + 3, 1, -math.inf)] if window else [])
+    for t, i, x in marks:
+        cache[slot(t)[0], i, 0, slot(t)[1], 5] = x
+    o = na.noble_attn_paged(q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), window=window)
+    t = torch.arange(n, device="cuda")
+    held = [cache[table[0].long()[t // page], i, :, t % page] for i in (0, 1)]
+    for r in range(new):
+        first, end = max(n - new + r - window + 1, 0) if window else 0, n - new + r + 1
+        ref, mag = attention(q[r:r + 1], *(x[first:end] for x in held), torch.ones(1, end - first, dtype=torch.bool))["o"]
+        assert bool((torch.isfinite(o[r, H // K:].cpu())).all())   # the second key head has no marks
+        if any(first <= t < end for t, _, _ in marks):
+            assert bool((torch.isfinite(o[r].cpu()) | ~torch.isfinite(ref[0])).all())
+        else:
+            check("o", o[r:r + 1], (ref, mag), dt)
+    assert not bool(o[new - 1].isfinite().all())
+
+
 def test_paged_pages_outside_the_cache_are_not_seen():
     g = _gen(8)
     cache = _rand(g, (4, 2, 1, 8, 64), BF)
