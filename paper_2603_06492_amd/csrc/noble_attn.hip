@@ -212,9 +212,32 @@ bool split_rows(int64_t rows, int64_t heads) {
     return sizeof(E) == 4 || cdiv(rows, kOwn) * heads < (DP == 64 ? 192 : 128);
 }
 
-// The backward's scratch: lse in units of log2 and delta [heads, Tq padded to tiles], the rows' intervals [Tq], their spans.
+// Whether the dk/dv launch runs split workgroups.
+bool split_keys(const noble_attn_desc* d) {
+    return d->dtype == NOBLE_F32 || (d->head_dim <= 64 ? split_rows<uint16_t, 64>(d->Tk, d->kv_heads)
+                                                       : split_rows<uint16_t, 128>(d->Tk, d->kv_heads));
+}
+
+// The query heads that share a key head are dealt to parts in the dk/dv launch, each with workgroups and sums of its own,
+// which attn_dkv_join_kernel adds: the fewest parts that give as many workgroups as run at once, one a CU (split) or two,
+// or fewer than twice as many that are of one size.  dk/dv of one part, and of these with the join (us, bf16): 8 heads of
+// 96 over 1, 7 x 4357 rows of documents 1083 and 341 (four parts); 16 heads of 128 over 2, 8 x 2048 causal 674 and 397;
+// 4 heads of 64 over 1, 8 x 379 rows 60 and 29; 8 heads of 128 over 2, 2 x 1001 50 and 36; over 1, 200 x 150 causal 137
+// and 123.  Where documents are that short and heads small the sums cost more than they give: 8 heads of 64 over 2,
+// 200 x 150 62 and 86.  Twice as many parts: 302, 418, 30, 36, 172.
+int64_t dkv_parts(const noble_attn_desc* d) {
+    const bool split = split_keys(d);
+    const int64_t share = d->heads / d->kv_heads, groups = cdiv(d->Tk, split ? 32 : kOwn) * d->kv_heads;
+    const int64_t least = std::clamp<int64_t>(groups > 0 ? cdiv(split ? 256 : 512, groups) : 1, 1, share);
+    for (int64_t parts = least; parts < 2 * least && parts <= share; ++parts)
+        if (share % parts == 0) return parts;
+    return least;
+}
+
+// The backward's scratch: lse in units of log2 and delta [heads, Tq padded to tiles], the rows' intervals [Tq], their
+// spans, and the parts' sums.
 struct BwdScratch {
-    size_t lse2, delta, lo, keys, span, bytes;
+    size_t lse2, delta, lo, keys, span, part, bytes;
     static int64_t pad(int64_t rows) { return (rows + kPart - 1) / kPart * kPart; }
     explicit BwdScratch(const noble_attn_desc* d) {
         const size_t per_head = up256((size_t)d->heads * pad(d->Tq) * 4), per_row = up256((size_t)d->Tq * 4);
@@ -223,7 +246,9 @@ struct BwdScratch {
         lo = delta + per_head;
         keys = lo + per_row;
         span = keys + per_row;
-        bytes = span + up256((size_t)((d->Tq + kPart - 1) / kPart) * sizeof(int4));
+        part = span + up256((size_t)((d->Tq + kPart - 1) / kPart) * sizeof(int4));
+        const int64_t parts = dkv_parts(d);
+        bytes = part + (parts > 1 ? (size_t)parts * 2 * d->kv_heads * d->Tk * d->head_dim * 4 : 0);
     }
 };
 
@@ -488,6 +513,8 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
     a.row_lo = reinterpret_cast<int*>(s + ws.lo);
     a.row_keys = reinterpret_cast<int*>(s + ws.keys);
     a.span = reinterpret_cast<int4*>(s + ws.span);
+    a.part = reinterpret_cast<float*>(s + ws.part);
+    a.parts = (int)dkv_parts(desc);
     const hipStream_t st = (hipStream_t)stream;
     return with_shape(desc->dtype, D, [&]<typename E, int DP>() {
         return with_mode(desc->softcap > 0.f, slopes != nullptr, [&]<int MODE>() {
@@ -498,10 +525,17 @@ noble_status noble_attn_bwd(const noble_attn_desc* desc, const noble_heads* grad
                                  dim3((unsigned)HeadOrder::grid(desc->kv_heads, tiles * a.share)), dim3(256), st, a));
             }
             if (desc->Tk > 0) {
-                const bool split = split_rows<E, DP>(desc->Tk, desc->kv_heads);
+                const bool split = split_keys(desc);
                 const int64_t tiles = cdiv(desc->Tk, split ? 32 : kOwn);
-                NOBLE_TRY(launch(split ? attn_dkv_kernel<E, DP, MODE, true> : attn_dkv_kernel<E, DP, MODE, sizeof(E) == 4>,
-                                 dim3((unsigned)HeadOrder::grid(desc->kv_heads, tiles)), dim3(256), st, a));
+                const auto kernel = [&]<bool PARTS>() {
+                    return split ? attn_dkv_kernel<E, DP, MODE, true, PARTS>
+                                 : attn_dkv_kernel<E, DP, MODE, sizeof(E) == 4, PARTS>;
+                };
+                NOBLE_TRY(launch(a.parts > 1 ? kernel.template operator()<true>() : kernel.template operator()<false>(),
+                                 dim3((unsigned)HeadOrder::grid(desc->kv_heads, tiles * a.parts)), dim3(256), st, a));
+                if (a.parts > 1)
+                    NOBLE_TRY(launch(attn_dkv_join_kernel<E>,
+                                     dim3((unsigned)cdiv(desc->kv_heads * desc->Tk * (D / 4), 256), 2), dim3(256), st, a));
             }
             return NOBLE_OK;
         });

@@ -59,7 +59,8 @@ struct PagedShape {
 };
 
 // SEVERAL: more than one new token a sequence, whose rows may see different keys of a tile.  Calls of single tokens do
-// without: with the general kernel 16 sequences of 130 to 8192 tokens, cap, take 114 us and not 109, one of 1000 6.7 and not 6.4.
+// without: with the general kernel 16 sequences of 130 to 8192 tokens, cap, take 114 us and not 109, one of 1000 6.7 and
+// not 6.4.
 template <typename E, int DP, int MODE, bool SEVERAL>
 __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_kernel(PagedArgs a) {
     using T = Tile<E, DP>;

@@ -26,6 +26,8 @@ struct AttnArgs {
     int* row_lo;                 // backward: the rows' first keys and numbers of keys, and of each 64 rows the bounds
     int* row_keys;
     int4* span;
+    float* part;                 // backward, parts > 1: dk and dv of each part, [parts][2][key heads][Tk][D]
+    int parts;                   // that the query heads of a key head are dealt to
     int Tq, Tk, heads, share, D;   // share: query heads of a key head
     int Tpad;                      // Tq rounded up to a tile: rows past the end have probability zero in lse2
     int causal, off;               // key index of row 0
@@ -649,24 +651,30 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a)
     }
 }
 
-// The 64-row tiles of queries that see a workgroup's keys, in order, over the query heads that share the key head.
+// The query heads [at, end) of a key head's that part p of them has.
+struct HeadPart {
+    int at, end;
+    __device__ __forceinline__ HeadPart(int share, int p, int parts) : at(share * p / parts), end(share * (p + 1) / parts) {}
+};
+
+// The 64-row tiles of queries that see a workgroup's keys, in order, over query heads that share the key head.
 // 64 tiles are looked at together, one a lane.
 struct Partners {
-    int share, tiles;
+    int end, tiles;
     const int4* span;
     int k0, k1, w0, w1;      // the workgroup's keys, and the wave's
-    int head = 0, base = -64, lane;
+    int head, base = -64, lane;
     uint64_t any = 0, mine = 0, full = 0;
-    __device__ __forceinline__ Partners(const AttnArgs& a, int key0, int keys, int wave_key, int wave_keys, int lane_)
-        : share(a.share), tiles((a.Tq + kPart - 1) / kPart), span(a.span), k0(key0), k1(min(key0 + keys, a.Tk)),
-          w0(wave_key), w1(min(wave_key + wave_keys, a.Tk)), lane(lane_) {}
+    __device__ __forceinline__ Partners(const AttnArgs& a, HeadPart heads, int key0, int keys, int wave_key, int wave_keys, int lane_)
+        : end(heads.end), tiles((a.Tq + kPart - 1) / kPart), span(a.span), k0(key0), k1(min(key0 + keys, a.Tk)),
+          w0(wave_key), w1(min(wave_key + wave_keys, a.Tk)), head(heads.at), lane(lane_) {}
     // The next (head, tile), and whether the wave's keys are seen by any or by all of its rows; false at the end.
     __device__ __forceinline__ bool next(int& hd, int& tile, bool& seen, bool& whole) {
         while (!any) {
             base += 64;
             if (base >= tiles) {
                 base = 0;
-                if (++head >= share) return false;
+                if (++head >= end) return false;
             }
             int4 s = {0, 0, 0, 0};
             if (base + lane < tiles) s = span[base + lane];
@@ -699,7 +707,18 @@ struct DkvShape {
     static constexpr int REQUESTS = 2 * TB / 1024 + 4;   // of a split wave and stage
 };
 
-template <typename E, int DP, int MODE, bool SPLIT>
+// Where a part's sums for dk (which 0) or dv (1) go.
+__device__ __forceinline__ HeadRows part_rows(const AttnArgs& a, int part, int which) {
+    HeadRows r;
+    r.row = (int64_t)a.D * 4;
+    r.head = a.Tk * r.row;
+    r.ptr = reinterpret_cast<char*>(a.part) + (2 * part + which) * (a.heads / a.share) * r.head;
+    return r;
+}
+
+// PARTS: more than one part; with the choice made inside one kernel, forward and backward of 128 images of
+// 12 heads of 64 took 246 us and not 225.
+template <typename E, int DP, int MODE, bool SPLIT, bool PARTS>
 __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
     using S = DkvShape<E, DP, SPLIT>;
@@ -707,11 +726,15 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     int kv = 0, key_tile = 0;   // the first keys (which the most rows see under a causal mask) first
-    if (!HeadOrder{a.heads / a.share, (a.Tk + S::OWN - 1) / S::OWN}.place(blockIdx.x, kv, key_tile)) return;
+    const int parts = PARTS ? a.parts : 1;
+    if (!HeadOrder{a.heads / a.share, (a.Tk + S::OWN - 1) / S::OWN * parts}.place(blockIdx.x, kv, key_tile)) return;
+    const int part_of = key_tile % parts;
+    key_tile /= parts;
+    const HeadPart heads(a.share, part_of, parts);
     const int key0 = key_tile * S::OWN, wkey = SPLIT ? key0 : key0 + 32 * wave, key = wkey + (lane & 31), db = a.D * ES;
 
     // Tiles of ROWS rows: of all waves, or every fourth one (`turn`) for each
-    Partners it(a, key0, S::OWN, wkey, 32, lane);
+    Partners it(a, heads, key0, S::OWN, wkey, 32, lane);
     char* stages = SPLIT ? lds + wave * S::STAGES * STAGE : lds;
     int gi = 0, tile = 0, sub = 0, turn = -1;   // sub: the part of ROWS rows of a 64-row tile
     bool seen = false, whole = false, more = it.next(gi, tile, seen, whole);
@@ -863,19 +886,22 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
     }
 
     uint32_t again = rows_of(key < a.Tk && !(zero_of(dv, zero_of(dk, 0.f)) == 0.f));
+    // the outputs, or this part's sums of float32
+    using Out = std::conditional_t<PARTS, float, E>;
+    const HeadRows to_dk = PARTS ? part_rows(a, part_of, 0) : a.dk, to_dv = PARTS ? part_rows(a, part_of, 1) : a.dv;
     if constexpr (!SPLIT) {
         if (key < a.Tk && !((again >> (lane & 31)) & 1u)) {
-            char* okp = a.dk.ptr + kv * a.dk.head + (int64_t)key * a.dk.row;
-            char* ovp = a.dv.ptr + kv * a.dv.head + (int64_t)key * a.dv.row;
+            char* okp = to_dk.ptr + kv * to_dk.head + (int64_t)key * to_dk.row;
+            char* ovp = to_dv.ptr + kv * to_dv.head + (int64_t)key * to_dv.row;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int e = 32 * d + 8 * i + 4 * h;
+                    const int e = 32 * d + 8 * i + 4 * h, at = e * (int)sizeof(Out);
                     if (e < a.D) {
-                        store4<E>(okp + e * ES, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale,
-                                  dk[d][4 * i + 2] * a.scale, dk[d][4 * i + 3] * a.scale);
-                        store4<E>(ovp + e * ES, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+                        store4<Out>(okp + at, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale,
+                                    dk[d][4 * i + 2] * a.scale, dk[d][4 * i + 3] * a.scale);
+                        store4<Out>(ovp + at, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
                     }
                 }
         }
@@ -885,7 +911,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
         uint32_t* flags = reinterpret_cast<uint32_t*>(lds + Meeting<DP>::BYTES);
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            const HeadRows& to = which ? a.dv : a.dk;
+            const HeadRows& to = which ? to_dv : to_dk;
             const float scale = which ? 1.f : a.scale;
             __syncthreads();   // the stages, and then dk's sums, have been read
             meet.put(which ? dv : dk, 0.f, 0.f);
@@ -898,8 +924,8 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
 #pragma unroll
                 for (int x = 0; x < 4; ++x) v += *reinterpret_cast<const f32x4*>(meet.get(x, r) + d);
                 if (d < a.D && key0 + r < a.Tk && !((again >> r) & 1u))
-                    store4<E>(to.ptr + kv * to.head + (int64_t)(key0 + r) * to.row + d * ES, v[0] * scale, v[1] * scale,
-                              v[2] * scale, v[3] * scale);
+                    store4<Out>(to.ptr + kv * to.head + (int64_t)(key0 + r) * to.row + d * (int)sizeof(Out), v[0] * scale,
+                                v[1] * scale, v[2] * scale, v[3] * scale);
             }
         }
         again &= 0x11111111u << wave;   // a quarter of the keys for each wave
@@ -908,7 +934,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
         const int j = wkey + __builtin_ctz(again);
         const Pair kj = load_pair<E>(a.k, kv, j, a.D, lane), vj = load_pair<E>(a.v, kv, j, a.D, lane);
         Pair sk, sv;
-        for (int head = kv * a.share; head < (kv + 1) * a.share; ++head) {
+        for (int head = kv * a.share + heads.at; head < kv * a.share + heads.end; ++head) {
             const float slope = MODE & kBias ? a.slopes[head] * kLog2e / a.sc.unit : 0.f;
             for (int i = 0; i < a.Tq; ++i) {
                 if ((uint32_t)(j - a.row_lo[i]) >= (uint32_t)a.row_keys[i]) continue;
@@ -923,9 +949,23 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dkv_kernel(AttnArgs a
                 sk.y += dz * q.y;
             }
         }
-        store_pair<E>(a.dk, kv, j, a.D, lane, sk.x, sk.y);
-        store_pair<E>(a.dv, kv, j, a.D, lane, sv.x, sv.y);
+        store_pair<Out>(to_dk, kv, j, a.D, lane, sk.x, sk.y);
+        store_pair<Out>(to_dv, kv, j, a.D, lane, sv.x, sv.y);
     }
+}
+
+// dk and dv from the parts' sums, in their order: four elements a thread.
+template <typename E>
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(AttnArgs a) {
+    const int quads = a.D / 4, which = blockIdx.y;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)(a.heads / a.share) * a.Tk;
+    if (i >= rows * quads) return;
+    const float* p = a.part + which * rows * a.D + 4 * i;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(p);
+    for (int n = 1; n < a.parts; ++n) sum += *reinterpret_cast<const f32x4*>(p + 2 * n * rows * a.D);
+    const int64_t row = i / quads;
+    const HeadRows& to = which ? a.dv : a.dk;
+    store4<E>(to.ptr + row / a.Tk * to.head + row % a.Tk * to.row + i % quads * 4 * (int)sizeof(E), sum[0], sum[1], sum[2], sum[3]);
 }
 
 }  // namespace noble

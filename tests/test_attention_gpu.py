@@ -172,6 +172,33 @@ def test_repeated_backward_is_bitwise_equal(H, K):
         assert all(bool((a[n] == b[n]).all()) for n in a)
 
 
+@pytest.mark.parametrize("dt,H,K,D,T", [(BF, 96, 48, 128, 300), (BF, 192, 64, 64, 260), (BF, 8, 1, 128, 200),
+                                        (BF, 12, 2, 40, 131), (F32, 6, 1, 72, 97), (F32, 24, 8, 64, 150)])
+def test_heads_dealt_to_parts(dt, H, K, D, T):
+    """Few key heads with several query heads each: their gradients are summed over parts of the query heads.  Twice the
+    same bits, and an infinite value in one row reaches the keys that the row sees."""
+    print(f"[attn] parts {dt} {H} {K} {D} {T}", flush=True)
+    g = _gen(T + H)
+    q, k, v, do = (_rand(g, (T, n, D), dt) for n in (H, K, K, H))
+    lo, hi = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in zip(*[(0, 60) if i < 60 else (60, T) for i in range(T)]))
+    slopes = _slopes(H)
+    got = _run(q, k, v, do, lo, hi, slopes, causal=True, offset=0)
+    seen = dense_mask(T, T, lo.cpu(), hi.cpu(), causal=True)
+    want = attention(q, k, v, seen, slopes=slopes, do=do)
+    for name in ("o", "lse", "dq", "dk", "dv"):
+        check(name, got[name], want[name], dt)
+    for name, x in _run(q, k, v, do, lo, hi, slopes, causal=True, offset=0).items():
+        assert torch.equal(x, got[name]), name
+    do[80, H - 1, 3] = math.inf
+    bad = _run(q, k, v, do, lo, hi, slopes, causal=True, offset=0)
+    rest = torch.ones(T, dtype=torch.bool)
+    rest[60:81] = False
+    for name in ("dk", "dv"):
+        assert torch.equal(bad[name][:, :K - 1], got[name][:, :K - 1])   # the other key heads
+        check(name, bad[name].cpu()[rest], [t[rest] for t in want[name]], dt)
+    assert not bad["dv"][60:81, K - 1, 3].isfinite().any()
+
+
 def test_large_scores():
     """Scores of some hundreds: the softmax stays in range and rows take one key nearly alone."""
     T, H, D = 200, 2, 64
