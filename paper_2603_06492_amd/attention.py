@@ -3,8 +3,8 @@ the O layer of a transformer block.
 
 The functions keep the C names and take torch tensors: ``noble_qk_rope_fwd`` / ``_bwd``, ``noble_kv_append``,
 ``noble_attn_fwd`` / ``_bwd``, ``noble_attn_paged``, ``noble_rope_table``, ``noble_mask_rows``.  They check their
-arguments, allocate the outputs that are not given and the scratch, and enqueue on ``stream`` (default: torch's current
-stream).  ``QKRope``, ``Attention`` and ``RopeAttention`` are the ``torch.autograd.Function`` forms, ``PagedCache``
+arguments, allocate the outputs that are not given and the scratch, and enqueue all their work on ``stream`` (default:
+torch's current stream), where the inputs have to be ready.  ``QKRope``, ``Attention`` and ``RopeAttention`` are the ``torch.autograd.Function`` forms, ``PagedCache``
 keeps the pages of a batch of sequences, and ``NobleSelfAttention`` is the block's attention from x to the O layer's
 output, for training, prompts and single tokens.
 
@@ -13,6 +13,7 @@ There is no fallback: without the built library or a gfx950 device, calls raise.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.util
 import os
@@ -185,18 +186,31 @@ def _gpu(t, name) -> torch.device:
     return t.device
 
 
-def _used_on(stream, *tensors) -> None:
-    """Tensors allocated here for a call on another stream than the current one: kept until that stream is past it."""
-    if stream is not None:
+@contextlib.contextmanager
+def _work(device, stream):
+    """Makes ``device`` and, where one is given, ``stream`` current: what a call allocates, fills or copies inside is in that
+    stream's order, as its kernels are.  Yields the stream's handle, and a function for the tensors that the call returns:
+    new ones come from the stream's memory and are used on the caller's own, given ones the other way round, and either's
+    memory is kept for both."""
+    handle = _stream(stream, device)
+    if stream is None:
+        with _on(device):
+            yield handle, lambda *tensors: None
+        return
+    home = torch.cuda.current_stream(device)
+
+    def shared(*tensors):
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
+                t.record_stream(home)
+
+    with torch.cuda.stream(stream):
+        yield handle, shared
 
 
-def _scratch(n, device, stream):
-    s = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
-    _used_on(stream, s)
-    return s
+def _scratch(n, device):
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
 
 
 # ------------------------------------------------------- norm and rotation --
@@ -212,12 +226,11 @@ def noble_rope_table(length: int, rot: int, *, base: float = 10000.0, scaling: s
     dev = torch.empty(0, device=device).device
     if dev.type != "cuda":
         raise ValueError(f"the tables live on the GPU (got {dev})")
-    cos, sin = (torch.empty((max(length, 0), max(rot, 0) // 2), device=dev) for _ in range(2))
     s = noble_rope_scaling(SCALINGS[scaling], 0, base, factor, trained, fast, slow, gain)
-    with _on(dev):
-        _call("noble_rope_table", ctypes.byref(s), length, rot, cos.data_ptr() or None, sin.data_ptr() or None,
-              _stream(stream, dev))
-    _used_on(stream, cos, sin)
+    with _work(dev, stream) as (st, shared):
+        cos, sin = (torch.empty((max(length, 0), max(rot, 0) // 2), device=dev) for _ in range(2))
+        _call("noble_rope_table", ctypes.byref(s), length, rot, cos.data_ptr() or None, sin.data_ptr() or None, st)
+        shared(cos, sin)
     return cos, sin
 
 
@@ -256,12 +269,12 @@ def noble_qk_rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, *, heads: in
             return out
     dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
     T, D = d.T, d.head_dim
-    q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
-    k = torch.empty((T, kv_heads, D), dtype=qkv.dtype, device=dev) if k is None else k
-    out = [_tensor(q, "q", qkv.dtype, (T, heads, D), dev), _tensor(k, "k", qkv.dtype, (T, kv_heads, D), dev)]
-    with _on(dev):
-        _call("noble_qk_rope_fwd", ctypes.byref(d), *args, *out, _stream(stream, dev))
-    _used_on(stream, q, k)
+    with _work(dev, stream) as (st, shared):
+        q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
+        k = torch.empty((T, kv_heads, D), dtype=qkv.dtype, device=dev) if k is None else k
+        out = [_tensor(q, "q", qkv.dtype, (T, heads, D), dev), _tensor(k, "k", qkv.dtype, (T, kv_heads, D), dev)]
+        _call("noble_qk_rope_fwd", ctypes.byref(d), *args, *out, st)
+        shared(q, k)
     return q, k
 
 
@@ -277,24 +290,23 @@ def noble_qk_rope_bwd(dq, dk, qkv, q_weight, k_weight, cos, sin, positions, *, h
     dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
     T, D = d.T, d.head_dim
     grads = [_tensor(dq, "dq", qkv.dtype, (T, heads, D), dev), _tensor(dk, "dk", qkv.dtype, (T, kv_heads, D), dev)]
-    if dqkv is None:
-        dqkv = torch.zeros_like(qkv, memory_format=torch.contiguous_format)
-    if dqkv.device != dev or dqkv.dtype != qkv.dtype or dqkv.shape != qkv.shape:
-        raise ValueError("dqkv must have qkv's shape, dtype and device")
-    if T > 1 and _rows(dqkv, "dqkv", qkv.shape[1]) != d.x_row:
-        qkv = qkv.contiguous() if dqkv.is_contiguous() else qkv
-        if _rows(qkv, "qkv", None) != dqkv.stride(0):
-            raise ValueError("dqkv must have qkv's row stride, or be contiguous")
-        d.x_row, args[0] = dqkv.stride(0), qkv.data_ptr()
-    w = [None, None] if q_weight is None else [torch.empty(D, device=dev) for _ in range(2)]
-    n = _sz(0)
-    _call("noble_qk_rope_scratch_size", ctypes.byref(d), ctypes.byref(n))
-    scratch = _scratch(n.value if q_weight is not None else 0, dev, stream)
-    with _on(dev):
+    with _work(dev, stream) as (st, shared):
+        if dqkv is None:
+            dqkv = torch.zeros_like(qkv, memory_format=torch.contiguous_format)
+        if dqkv.device != dev or dqkv.dtype != qkv.dtype or dqkv.shape != qkv.shape:
+            raise ValueError("dqkv must have qkv's shape, dtype and device")
+        if T > 1 and _rows(dqkv, "dqkv", qkv.shape[1]) != d.x_row:
+            qkv = qkv.contiguous() if dqkv.is_contiguous() else qkv
+            if _rows(qkv, "qkv", None) != dqkv.stride(0):
+                raise ValueError("dqkv must have qkv's row stride, or be contiguous")
+            d.x_row, args[0] = dqkv.stride(0), qkv.data_ptr()
+        w = [None, None] if q_weight is None else [torch.empty(D, device=dev) for _ in range(2)]
+        n = _sz(0)
+        _call("noble_qk_rope_scratch_size", ctypes.byref(d), ctypes.byref(n))
+        scratch = _scratch(n.value if q_weight is not None else 0, dev)
         _call("noble_qk_rope_bwd", ctypes.byref(d), *grads, *args, dqkv.data_ptr() or None,
-              *[None if t is None else t.data_ptr() for t in w], scratch.data_ptr(), scratch.numel(),
-              _stream(stream, dev))
-    _used_on(stream, dqkv, *w)
+              *[None if t is None else t.data_ptr() for t in w], scratch.data_ptr(), scratch.numel(), st)
+        shared(dqkv, *w)
     return dqkv, w[0], w[1]
 
 
@@ -318,12 +330,12 @@ def noble_kv_append(qkv, q_weight, k_weight, cos, sin, positions, slots, cache, 
     dev, d, args = _rope_args(qkv, q_weight, k_weight, cos, sin, positions, heads, kv_heads, eps, interleaved)
     T, D = d.T, d.head_dim
     pages, page, pc = _cache_shape(cache, kv_heads, D, qkv.dtype, dev)
-    q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
     c = noble_cache_desc(pages, page, 0)
-    rest = [_tensor(slots, "slots", torch.int64, (T,), dev), _tensor(q, "q", qkv.dtype, (T, heads, D), dev), pc]
-    with _on(dev):
-        _call("noble_kv_append", ctypes.byref(d), ctypes.byref(c), *args, *rest, _stream(stream, dev))
-    _used_on(stream, q)
+    with _work(dev, stream) as (st, shared):
+        q = torch.empty((T, heads, D), dtype=qkv.dtype, device=dev) if q is None else q
+        rest = [_tensor(slots, "slots", torch.int64, (T,), dev), _tensor(q, "q", qkv.dtype, (T, heads, D), dev), pc]
+        _call("noble_kv_append", ctypes.byref(d), ctypes.byref(c), *args, *rest, st)
+        shared(q)
     return q
 
 
@@ -337,12 +349,12 @@ def noble_mask_rows(starts, T: int, *, prefix=None, causal: bool = True, window:
     if starts.dim() != 1 or starts.shape[0] < 1:
         raise ValueError("starts must be int32 [documents + 1]")
     n = starts.shape[0] - 1
-    out = [torch.empty(max(T, 0), dtype=torch.int32, device=dev) for _ in range(3)]
-    with _on(dev):
+    with _work(dev, stream) as (st, shared):
+        out = [torch.empty(max(T, 0), dtype=torch.int32, device=dev) for _ in range(3)]
         _call("noble_mask_rows", T, n, _tensor(starts, "starts", torch.int32, (n + 1,), dev),
               _tensor(prefix, "prefix", torch.int32, (n,), dev), int(causal), window,
-              *[t.data_ptr() or None for t in out], _stream(stream, dev))
-    _used_on(stream, *out)
+              *[t.data_ptr() or None for t in out], st)
+        shared(*out)
     return tuple(out)
 
 
@@ -375,13 +387,12 @@ def noble_attn_fwd(q, k, v, key_lo=None, key_hi=None, slopes=None, *, causal: bo
             return out
     dev, d, heads, mask = _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap)
     shape = tuple(q.shape)
-    o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
-    lse = torch.empty(shape[1::-1], device=dev) if lse is None else lse
-    with _on(dev):
+    with _work(dev, stream) as (st, shared):
+        o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
+        lse = torch.empty(shape[1::-1], device=dev) if lse is None else lse
         _call("noble_attn_fwd", ctypes.byref(d), *map(ctypes.byref, heads), *mask,
-              ctypes.byref(_heads(o, "o", q.dtype, dev, shape)), _tensor(lse, "lse", torch.float32, shape[1::-1], dev),
-              _stream(stream, dev))
-    _used_on(stream, o, lse)
+              ctypes.byref(_heads(o, "o", q.dtype, dev, shape)), _tensor(lse, "lse", torch.float32, shape[1::-1], dev), st)
+        shared(o, lse)
     return o, lse
 
 
@@ -395,17 +406,17 @@ def noble_attn_bwd(do, q, k, v, o, lse, key_lo=None, key_hi=None, slopes=None, *
             return out
     dev, d, heads, mask = _attn_args(q, k, v, key_lo, key_hi, slopes, causal, offset, scale, softcap)
     dt, sq, sk = q.dtype, tuple(q.shape), tuple(k.shape)
-    dq, dk, dv = (torch.empty(s, dtype=dt, device=dev) if t is None else t for t, s in ((dq, sq), (dk, sk), (dv, sk)))
     g, oo = _heads(do, "do", dt, dev, sq), _heads(o, "o", dt, dev, sq)
-    outs = [_heads(t, n, dt, dev, s) for t, n, s in ((dq, "dq", sq), (dk, "dk", sk), (dv, "dv", sk))]
     n = _sz(0)
     _call("noble_attn_bwd_scratch_size", ctypes.byref(d), ctypes.byref(n))
-    scratch = _scratch(n.value, dev, stream)
-    with _on(dev):
+    with _work(dev, stream) as (st, shared):
+        dq, dk, dv = (torch.empty(s, dtype=dt, device=dev) if t is None else t for t, s in ((dq, sq), (dk, sk), (dv, sk)))
+        outs = [_heads(t, n, dt, dev, s) for t, n, s in ((dq, "dq", sq), (dk, "dk", sk), (dv, "dv", sk))]
+        scratch = _scratch(n.value, dev)
         _call("noble_attn_bwd", ctypes.byref(d), ctypes.byref(g), *map(ctypes.byref, heads), ctypes.byref(oo),
               _tensor(lse, "lse", torch.float32, sq[1::-1], dev), *mask, *map(ctypes.byref, outs), scratch.data_ptr(),
-              scratch.numel(), _stream(stream, dev))
-    _used_on(stream, dq, dk, dv)
+              scratch.numel(), st)
+        shared(dq, dk, dv)
     return dq, dk, dv
 
 
@@ -427,20 +438,20 @@ def noble_attn_paged(q, cache, page_table, lengths, slopes=None, *, scale: Optio
         raise ValueError(f"{rows} rows of q are not the same number for each of {B} sequences")
     K = cache.shape[2] if isinstance(cache, torch.Tensor) and cache.dim() == 5 else 0
     pages, page, pc = _cache_shape(cache, K, D, q.dtype, dev)
-    o = torch.empty((rows, H, D), dtype=q.dtype, device=dev) if o is None else o
     i32 = torch.int32
     d = noble_paged_desc(B, per, pages, page, rows // B, window, H, K, D, _dtype_code(q),
                          D ** -0.5 if scale is None else scale, softcap, 0)
     n = _sz(0)
     _call("noble_attn_paged_scratch_size", ctypes.byref(d), ctypes.byref(n))
-    scratch = _scratch(n.value, dev, stream) if n.value else None
-    with _on(dev):
+    with _work(dev, stream) as (st, shared):
+        o = torch.empty((rows, H, D), dtype=q.dtype, device=dev) if o is None else o
+        scratch = _scratch(n.value, dev) if n.value else None
         _call("noble_attn_paged", ctypes.byref(d), ctypes.byref(_heads(q, "q", q.dtype, dev)), pc,
               _tensor(page_table, "page_table", i32, (B, per), dev), _tensor(lengths, "lengths", i32, (B,), dev),
               _tensor(slopes, "slopes", torch.float32, (H,), dev),
               ctypes.byref(_heads(o, "o", q.dtype, dev, (rows, H, D))),
-              None if scratch is None else scratch.data_ptr(), n.value, _stream(stream, dev))
-    _used_on(stream, o)
+              None if scratch is None else scratch.data_ptr(), n.value, st)
+        shared(o)
     return o
 
 

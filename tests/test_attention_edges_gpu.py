@@ -1,0 +1,80 @@
+"""The attention operators at the edges of their arguments: other streams, windows, infinities, caps, one row, second
+derivatives, lengths."""
+
+import math
+
+import pytest
+import torch
+
+from _attention import attention, check, dense_mask
+from paper_2603_06492_amd import attention as na
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _rand(g, shape, dt=F32, std=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(dt)
+
+
+# ---------------------------------------------------------------- streams --
+
+def test_calls_on_another_stream_while_the_current_one_is_busy():
+    """Every call on a stream of its own, its inputs ready, while the current stream has work queued on tensors that have
+    been freed since: the results are those of the current stream, bit for bit, and the queued work is not disturbed."""
+    T, H, K, D = 200, 4, 2, 64
+    g = _gen(21)
+    wide = _rand(g, (T, (H + 2 * K) * D + 64), BF)
+    qkv = wide[:, :(H + 2 * K) * D]
+    w = 1 + _rand(g, (D,), F32, 0.1)
+    dq, dk, do = _rand(g, (T, H, D), BF), _rand(g, (T, K, D), BF), _rand(g, (T, H, D), BF)
+    starts = torch.tensor([0, 70, 71, 190], dtype=torch.int32, device="cuda")
+    slots = torch.arange(T, device="cuda") + 8
+    table = torch.arange(1, 27, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([T], dtype=torch.int32, device="cuda")
+    caches = [torch.zeros((27, 2, K, 8, D), dtype=BF, device="cuda") for _ in range(2)]
+    given = [torch.full((T, (H + 2 * K) * D), 5.0, dtype=BF, device="cuda") for _ in range(2)]
+    how = dict(heads=H, kv_heads=K)
+
+    def everything(cache, into, **on):
+        cos, sin = na.noble_rope_table(256, 32, **on)
+        lo, hi, pos = na.noble_mask_rows(starts, T, **on)
+        rope = (qkv, w, w, cos, sin, pos)
+        q, k = na.noble_qk_rope_fwd(*rope, **how, **on)
+        v = qkv[:, (H + K) * D:].view(T, K, D)
+        o, lse = na.noble_attn_fwd(q, k, v, lo, hi, **on)
+        grads = na.noble_attn_bwd(do, q, k, v, o, lse, lo, hi, **on)
+        zeroed = na.noble_qk_rope_bwd(dq, dk, *rope, **how, **on)                # its gradient's tensor is zeroed inside
+        copied = na.noble_qk_rope_bwd(dq, dk, *rope, dqkv=into, **how, **on)     # its rows are copied inside
+        qa = na.noble_kv_append(*rope, slots, cache, **how, **on)
+        op = na.noble_attn_paged(qa[-3:], cache, table, lens, **on)
+        return [cos, sin, lo, hi, pos, q, k, o, lse, *grads, *zeroed, *copied, qa, op]
+
+    want = everything(caches[0], given[0])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.randn(2048, 2048, device="cuda", generator=g)
+    for _ in range(2):   # the second time with blocks that the first one's tensors left
+        caches[1].zero_()
+        given[1].fill_(5.0)
+        torch.cuda.synchronize()
+        sums = []
+        for n in (16, 4096, T * H * D * 2, T * (H + 2 * K) * D * 2, 1 << 20):   # queued work on blocks that are free at once
+            x = torch.ones(n, dtype=torch.uint8, device="cuda")
+            for _ in range(20):
+                big = torch.tanh(big @ big)
+            sums.append((n, x.sum(dtype=torch.int64) + 0 * big[0, 0].nan_to_num().long()))
+            del x
+        got = everything(caches[1], given[1], stream=side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        for n, s in sums:
+            assert int(s) == n
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), i
+        assert torch.equal(caches[0], caches[1])
+        del got
