@@ -394,7 +394,7 @@ __device__ __forceinline__ void bias16(float* z, float slope, float first) {
 // [0, 1/4] in x^2: relative error 3e-8), above it 1 - 2 / (e^2x + 1), whose absolute error of 1e-7 is relative there.
 // With the caps in use nearly every score is below, and a wave without a larger one runs the polynomial alone: 6
 // multiplications and additions for each score, where exp and reciprocal take as long as 10.  The float32 path
-// takes the library's tanh.  `slope` (given or nullptr): the cap's derivative, 1 - tanh^2.
+// takes the library's tanh.  z may be s.  `slope` (given or nullptr): the cap's derivative, 1 - tanh^2.
 template <typename E, int MODE, int N>
 __device__ __forceinline__ void scores(const ScoreArgs& k, const float* s, float* z, float* slope) {
     if constexpr (!(MODE & kCap)) {
@@ -411,17 +411,20 @@ __device__ __forceinline__ void scores(const ScoreArgs& k, const float* s, float
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(s[i]));
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = s[i] * s[i];
-            z[i] = s[i] * fmaf(fmaf(fmaf(fmaf(k.p[4], y, k.p[3]), y, k.p[2]), y, k.p[1]), y, k.p[0]);
-        }
+        const auto near = [&](float x) {
+            const float y = x * x;
+            return x * fmaf(fmaf(fmaf(fmaf(k.p[4], y, k.p[3]), y, k.p[2]), y, k.p[1]), y, k.p[0]);
+        };
         if (__any(top > k.small)) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[i] * k.cap_e) + 1.f);
-                z[i] = fabsf(s[i]) > k.small ? t * k.cap_out : z[i];
+                const float x = s[i];   // z may be s
+                const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * k.cap_e) + 1.f);
+                z[i] = fabsf(x) > k.small ? t * k.cap_out : near(x);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = near(s[i]);
         }
         if (slope) {
 #pragma unroll

@@ -78,3 +78,57 @@ def test_calls_on_another_stream_while_the_current_one_is_busy():
             assert torch.equal(a, b), i
         assert torch.equal(caches[0], caches[1])
         del got
+
+
+# -------------------------------------------------------------------- caps --
+
+CAP_SIZES = pytest.mark.parametrize("dt,H,K,D", [(BF, 4, 2, 64), (F32, 4, 2, 64), (BF, 96, 96, 64), (BF, 96, 48, 128)],
+                                    ids=["bf16", "f32", "bf16_wide64", "bf16_wide128"])
+
+
+def _slope_slack(q, k, v, do, seen, cap):
+    """1e-6 of what dq and dk would sum without the cap's slope."""
+    (T, H, D), K = q.shape, k.shape[1]
+    q, do = (x.double().cpu().transpose(0, 1) for x in (q, do))
+    k, v = (x.double().cpu().transpose(0, 1).repeat_interleave(H // K, 0) for x in (k, v))
+    p = torch.softmax((cap * torch.tanh(q @ k.transpose(1, 2) * D ** -0.5 / cap)).masked_fill(~seen, -math.inf), -1)
+    m = 1e-6 * D ** -0.5 * p * ((do @ v.transpose(1, 2)).abs() + (do * (p @ v)).sum(-1, keepdim=True).abs())
+    return (m @ k.abs()).transpose(0, 1), (m.transpose(1, 2) @ q.abs()).view(K, H // K, T, D).sum(1).transpose(0, 1)
+
+
+@CAP_SIZES
+@pytest.mark.parametrize("cap", [0.5, 1.0, 4.0])
+def test_scores_up_to_many_times_the_cap(dt, H, K, D, cap):
+    """Scores of standard deviation 1 to 3 under caps of half to four: below, near and far above the cap, in one tile and in
+    one lane.  1 - tanh^2 is a float32 difference of numbers up to 1: 1e-6 of what the score gradients would be
+    without it joins their bounds."""
+    print(f"[attn] capped {dt} {H} {K} {D} {cap}", flush=True)
+    T = 150
+    g = _gen(75)
+    q, k, v, do = (_rand(g, s, dt) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
+    q *= torch.linspace(0.2, 3.0, T, device="cuda")[:, None, None].to(dt)
+    o, lse = na.noble_attn_fwd(q, k, v, causal=True, softcap=cap)
+    dq, dk, dv = na.noble_attn_bwd(do, q, k, v, o, lse, causal=True, softcap=cap)
+    seen = dense_mask(T, T, causal=True)
+    want = attention(q, k, v, seen, softcap=cap, do=do)
+    slack_q, slack_k = _slope_slack(q, k, v, do, seen, cap)
+    for n, t in dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        ref, mag = want[n]
+        u = 2.0 ** -8 if dt == BF else 2e-5
+        check(n, t, (ref, mag + {"dq": slack_q / u, "dk": slack_k / u}.get(n, 0.0)), dt)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("cap", [0.5, 2.0])
+@pytest.mark.parametrize("new", [1, 3])
+def test_paged_scores_up_to_many_times_the_cap(dt, cap, new):
+    print(f"[paged] capped {dt} {cap} {new}", flush=True)
+    n, H, K, D, page = 333, 8, 2, 64, 16
+    g = _gen(76)
+    cache = _rand(g, (22, 2, K, page, D), dt)
+    table = torch.arange(22, dtype=torch.int32, device="cuda")[None]
+    q = _rand(g, (new, H, D), dt) * torch.linspace(0.3, 3.0, H, device="cuda")[:, None].to(dt)
+    o = na.noble_attn_paged(q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), softcap=cap)
+    t = torch.arange(n, device="cuda")
+    k, v = (cache[t // page, i, :, t % page] for i in (0, 1))
+    check("o", o, attention(q, k, v, dense_mask(new, n, causal=True), softcap=cap)["o"], dt)
