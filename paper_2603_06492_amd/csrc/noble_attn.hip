@@ -165,20 +165,31 @@ noble_status check_mask(const noble_attn_desc* d, const int32_t* lo, const int32
     return need_array(slopes, false, 4);
 }
 
-// Scores from raw products, in units of log2 (float32 from double; a cap of 0 is none).
-ScoreArgs score_args(float scale, float cap) {
+// Scores from raw products, in units of log2 (float32 from double; a cap of 0 is none).  Caps below 1e-18 and above 1e18 are
+// taken as these: scores under the first are alike to a float32 exponential, and scores of up to 1e14 are within 3e-9 of
+// themselves under the second.
+ScoreArgs score_args(float scale, float softcap) {
     ScoreArgs k{};
-    const double log2e = 1.4426950408889634, x = cap > 0.f ? (double)scale / cap : 0.0;
-    k.unit = cap > 0.f ? 1.f : (float)(scale * log2e);
-    if (cap > 0.f) {
+    const double log2e = 1.4426950408889634, cap = softcap > 0.f ? std::clamp((double)softcap, 1e-18, 1e18) : 0.0;
+    k.unit = cap > 0.0 ? 1.f : (float)(scale * log2e);
+    if (cap > 0.0) {
+        const double x = scale / cap;
         k.cap_in = (float)x;
         k.cap_e = (float)(2.0 * x * log2e);
         k.cap_out = (float)(cap * log2e);
         k.inv2 = (float)(1.0 / (cap * log2e * cap * log2e));
-        k.small = (float)(0.5 / x);
-        // tanh(x) / x as a polynomial in x^2 on [0, 1/4]
+        // tanh(x) / x as a polynomial in x^2 on [0, 1/4].  From the first coefficient on that no normal float32 holds, the
+        // scale being that far from the cap, the terms are left out, and the polynomial ends where they would be 3e-8.
         const double fit[5] = {1.0, -0.3333307206630707, 0.13324828445911407, -0.05298924073576927, 0.017141319811344147};
-        for (int i = 0; i < 5; ++i) k.p[i] = (float)(fit[i] * scale * log2e * std::pow(x, 2 * i));
+        double end = 0.5;
+        for (int i = 0; i < 5; ++i) {
+            k.p[i] = (float)(fit[i] * scale * log2e * std::pow(x, 2 * i));
+            if (i > 0 && !std::isnormal(k.p[i])) {
+                end = std::pow(3e-8 / std::fabs(fit[i]), 0.5 / i);
+                for (; i < 5; ++i) k.p[i] = 0.f;
+            }
+        }
+        k.small = (float)(end / x);
     }
     return k;
 }

@@ -373,7 +373,7 @@ struct ScoreArgs {
     float cap_e;      // 2 scale log2 e / cap: exp2 of it is e^2x
     float cap_out;    // cap log2 e
     float inv2;       // 1 / cap_out^2
-    float small;      // |s| up to which x = s scale / cap is at most 1/2
+    float small;      // |s| up to which the polynomial is taken: x = s scale / cap up to 1/2, or less (score_args)
     float p[5];       // there: score = s (p0 + p1 s^2 + .. + p4 s^8)
 };
 

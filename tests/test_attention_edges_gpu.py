@@ -132,3 +132,35 @@ def test_paged_scores_up_to_many_times_the_cap(dt, cap, new):
     t = torch.arange(n, device="cuda")
     k, v = (cache[t // page, i, :, t % page] for i in (0, 1))
     check("o", o, attention(q, k, v, dense_mask(new, n, causal=True), softcap=cap)["o"], dt)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("cap", [1e-30, 1e-12, 1e-6, 1e30])
+def test_caps_of_any_size(dt, cap):
+    """A cap far below the scores leaves them all alike, one far above leaves them as they are.  There 1 - tanh^2 is 0 in
+    float64 and up to a float32 rounding here, 1e-6 of the uncapped score gradients, themselves below 10."""
+    print(f"[attn] cap {dt} {cap}", flush=True)
+    T, H, K, D = 70, 4, 2, 64
+    g = _gen(71)
+    q, k, v, do = (_rand(g, s, dt) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
+    o, lse = na.noble_attn_fwd(q, k, v, causal=True, softcap=cap)
+    dq, dk, dv = na.noble_attn_bwd(do, q, k, v, o, lse, causal=True, softcap=cap)
+    want = attention(q, k, v, dense_mask(T, T, causal=True), softcap=cap, do=do)
+    names = ("o", "lse", "dv") + (("dq", "dk") if cap > 1 else ())
+    for n in names:
+        check(n, dict(o=o, lse=lse, dv=dv, dq=dq, dk=dk)[n], want[n], dt)
+    if cap < 1:
+        assert float(dq.float().abs().max()) <= 1e-4 and float(dk.float().abs().max()) <= 1e-4
+
+
+def test_large_caps_near_their_scores():
+    """A cap of 1e6 and scores of 0.02 to 0.9 times it, one key a row: lse is the score, within the tanh's error (1e-7 below
+    1, relative 3e-8 up to 1/2) and four float32 roundings, 6e-7."""
+    T, D = 44, 64
+    x = torch.linspace(0.02, 0.9, T)
+    q = torch.full((T, 1, D), 125.0, dtype=BF, device="cuda")
+    k = (x * 1e6 / D / 125.0)[:, None, None].expand(T, 1, D).to(BF).cuda().contiguous()
+    i = torch.arange(T, dtype=torch.int32, device="cuda")
+    _, lse = na.noble_attn_fwd(q, k, k, i, i + 1, scale=1.0, softcap=1e6)
+    want = 1e6 * torch.tanh(D * 125.0 * k[:, 0, 0].double().cpu() / 1e6)
+    assert float((lse[0].double().cpu() / want - 1).abs().max()) <= 6e-7 + 1e-7 / 0.5
