@@ -27,6 +27,9 @@ struct PagedArgs {
     int page, shift, fresh, window, heads, kv_heads, share, D;
     int row_tiles, pieces;
     ScoreArgs sc;
+    // The first token that the row of token `at` sees.  A row before the first token sees none, and its number, down to
+    // -2^20, would take the window's difference past 32 bits.
+    __device__ __forceinline__ int oldest(int at) const { return window > 0 ? max(max(at, -1) - window + 1, 0) : 0; }
 };
 
 constexpr int kChunk = 32;       // keys of a wave's step
@@ -43,7 +46,7 @@ struct Chunks {
         at0 = len - a.fresh + row_tile * kRows16 / a.share;
         at1 = len - a.fresh + r1 / a.share;
         end = max(at1 + 1, 0);
-        start = a.window > 0 ? max(at0 - a.window + 1, 0) : 0;
+        start = a.oldest(at0);
         first = start / kChunk;
         count = end > start ? (end + kChunk - 1) / kChunk - first : 0;
         pieces = max(1, min(a.pieces, count / waves));
@@ -176,13 +179,13 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
                     z[i] = fmaf(-slope, fabsf((float)(k0 + 4 * g4 - at) + (float)(16 * (i >> 2) + (i & 3))), z[i]);
             }
             // keys that some of the rows do not see
-            const bool edge = k0 + kChunk > ck.at0 + 1 || (a.window > 0 && k0 <= ck.at1 - a.window);
+            const bool edge = k0 + kChunk > ck.at0 + 1 || k0 < a.oldest(ck.at1);
             if (edge || bads[s]) {
-                const int from = a.window > 0 ? at - a.window : -1;
+                const int from = a.oldest(at);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int o = 16 * (i >> 2) + 4 * g4 + (i & 3), j = k0 + o;
-                    z[i] = j <= at && j > from && !((bads[s] >> o) & 1u) ? z[i] : -INFINITY;
+                    z[i] = j <= at && j >= from && !((bads[s] >> o) & 1u) ? z[i] : -INFINITY;
                 }
             }
             float top = z[0];
@@ -218,7 +221,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int j = k0 + 16 * (i >> 2) + 4 * g4 + (i & 3);
-                        seen |= (uint32_t)(j <= t && (a.window == 0 || j > t - a.window)) << i;
+                        seen |= (uint32_t)(j <= t && j >= a.oldest(t)) << i;
                     }
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {

@@ -164,3 +164,25 @@ def test_large_caps_near_their_scores():
     _, lse = na.noble_attn_fwd(q, k, k, i, i + 1, scale=1.0, softcap=1e6)
     want = 1e6 * torch.tanh(D * 125.0 * k[:, 0, 0].double().cpu() / 1e6)
     assert float((lse[0].double().cpu() / want - 1).abs().max()) <= 6e-7 + 1e-7 / 0.5
+
+
+# ----------------------------------------------------------------- windows --
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 5, 1 << 30, 64, 40])
+@pytest.mark.parametrize("lengths,new", [([3, 40, 0], 7), ([2, 64], 1)])
+def test_paged_windows_up_to_the_largest(lengths, new, window):
+    """Windows that hide nothing, up to the largest number, and sequences that hold fewer tokens than are new: the rows
+    of tokens before the first see nothing, the others what they see without a window."""
+    print(f"[paged] window {window} {lengths} {new}", flush=True)
+    H, K, D, page = 4, 2, 64, 16
+    g = _gen(31)
+    cache = _rand(g, (20, 2, K, page, D), BF)
+    table = torch.randperm(20, generator=g, device="cuda")[:len(lengths) * 4].view(-1, 4).to(torch.int32)
+    q = _rand(g, (len(lengths) * new, H, D), BF)
+    o = na.noble_attn_paged(q, cache, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), window=window)
+    for b, n in enumerate(lengths):
+        t = torch.arange(n, device="cuda")
+        k, v = (cache[table[b].long()[t // page], i, :, t % page] for i in (0, 1))
+        at = torch.arange(n - new, n)
+        rows = slice(b * new, (b + 1) * new)
+        check("o", o[rows], attention(q[rows], k, v, dense_mask(new, n, (at - window + 1).clamp(min=0), at + 1))["o"], BF)
