@@ -84,14 +84,16 @@ struct Angles {
             }
         }
     }
-    // The elements turned forward (dir 1) or back (dir -1), in place.
+    // The elements turned forward (dir 1) or back (dir -1), in place.  Those past the rotated ones are kept, not turned by
+    // nothing: an infinite one would become NaN, or make its neighbour that.
     __device__ __forceinline__ void turn(float* x, int rot, int chunk, float dir) const {
+        const bool turned = 8 * chunk < rot;
         if constexpr (INTER) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float p = x[2 * i], q = x[2 * i + 1], t = dir * s[i];
-                x[2 * i] = p * c[i] - q * t;
-                x[2 * i + 1] = q * c[i] + p * t;
+                x[2 * i] = turned ? p * c[i] - q * t : p;
+                x[2 * i + 1] = turned ? q * c[i] + p * t : q;
             }
         } else {
             // the pair's other element: rot / 16 lanes on for the first half, back for the second
@@ -102,7 +104,7 @@ struct Angles {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float other = __shfl(x[i], from);
-                x[i] = x[i] * c[i] + other * (sign * s[i]);
+                x[i] = turned ? x[i] * c[i] + other * (sign * s[i]) : x[i];
             }
         }
     }

@@ -186,3 +186,32 @@ def test_paged_windows_up_to_the_largest(lengths, new, window):
         at = torch.arange(n - new, n)
         rows = slice(b * new, (b + 1) * new)
         check("o", o[rows], attention(q[rows], k, v, dense_mask(new, n, (at - window + 1).clamp(min=0), at + 1))["o"], BF)
+
+
+# ------------------------------------------------- elements not rotated --
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("D,rot", [(64, 16), (128, 64), (72, 32)])
+def test_infinities_past_the_rotated_elements_stay_alone(dt, inter, D, rot):
+    """Without a norm the elements past the rotated ones come out as they went in, infinite ones too, and reach no other
+    element; so do their gradients."""
+    print(f"[rope] inf {dt} {inter} {D} {rot}", flush=True)
+    T, H, K = 11, 3, 2
+    g = _gen(41)
+    qkv, dq, dk = (_rand(g, s, dt) for s in ((T, (H + 2 * K) * D), (T, H, D), (T, K, D)))
+    cos, sin = na.noble_rope_table(T, rot)
+    heads = lambda x, a, b: x[:, a * D:b * D].view(T, b - a, D)  # noqa: E731
+
+    def run():
+        q, k = na.noble_qk_rope_fwd(qkv, None, None, cos, sin, None, heads=H, kv_heads=K, interleaved=inter)
+        d, _, _ = na.noble_qk_rope_bwd(dq, dk, qkv, None, None, cos, sin, None, heads=H, kv_heads=K, interleaved=inter)
+        return [q, k, heads(d, 0, H), heads(d, H, H + K)]
+
+    clean = run()
+    ins = [heads(qkv, 0, H), heads(qkv, H, H + K), dq, dk]
+    for x in ins:
+        x[3, 0, rot], x[5, 1, rot + 5], x[7, :, D - 1] = math.inf, -math.inf, math.inf
+    for x, was, now in zip(ins, clean, run()):
+        assert torch.equal(now[..., rot:], x[..., rot:])
+        assert torch.equal(now[..., :rot], was[..., :rot])
