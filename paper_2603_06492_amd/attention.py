@@ -295,7 +295,7 @@ def noble_qk_rope_bwd(dq, dk, qkv, q_weight, k_weight, cos, sin, positions, *, h
             dqkv = torch.zeros_like(qkv, memory_format=torch.contiguous_format)
         if dqkv.device != dev or dqkv.dtype != qkv.dtype or dqkv.shape != qkv.shape:
             raise ValueError("dqkv must have qkv's shape, dtype and device")
-        if T > 1 and _rows(dqkv, "dqkv", qkv.shape[1]) != d.x_row:
+        if _rows(dqkv, "dqkv", qkv.shape[1]) != d.x_row and T > 1:
             qkv = qkv.contiguous() if dqkv.is_contiguous() else qkv
             if _rows(qkv, "qkv", None) != dqkv.stride(0):
                 raise ValueError("dqkv must have qkv's row stride, or be contiguous")

@@ -215,3 +215,23 @@ def test_infinities_past_the_rotated_elements_stay_alone(dt, inter, D, rot):
     for x, was, now in zip(ins, clean, run()):
         assert torch.equal(now[..., rot:], x[..., rot:])
         assert torch.equal(now[..., :rot], was[..., :rot])
+
+
+# ----------------------------------------------------------------- one row --
+
+@pytest.mark.parametrize("T", [1, 2])
+def test_gradient_rows_need_adjacent_columns(T):
+    """A given gradient of the Q/K/V rows with spread columns is refused whatever the number of rows; columns of a wider
+    buffer are not."""
+    H, K, D = 2, 1, 16
+    C = (H + 2 * K) * D
+    g = _gen(51)
+    qkv, dq, dk = _rand(g, (T, 2 * C), BF)[:, :C], _rand(g, (T, H, D), BF), _rand(g, (T, K, D), BF)
+    wide = torch.full((T, 2 * C), 7.0, dtype=BF, device="cuda")
+    with pytest.raises(ValueError, match="adjacent columns"):
+        na.noble_qk_rope_bwd(dq, dk, qkv, None, None, None, None, None, heads=H, kv_heads=K, dqkv=wide[:, ::2])
+    assert bool((wide == 7.0).all())
+    into = wide[:, 16:16 + C]
+    na.noble_qk_rope_bwd(dq, dk, qkv, None, None, None, None, None, heads=H, kv_heads=K, dqkv=into)
+    assert torch.equal(into[:, :H * D], dq.view(T, -1)) and torch.equal(into[:, H * D:(H + K) * D], dk.view(T, -1))
+    assert bool((wide[:, :16] == 7.0).all()) and bool((wide[:, 16 + (H + K) * D:] == 7.0).all())
