@@ -146,7 +146,8 @@ noble_status noble_kv_append(const noble_rope_desc* desc,
 /* Row i of query head h sees the keys j in [key_lo[i], key_hi[i]) (int32
  * [Tq], both or none; none: [0, Tk)), with `causal` only j <= i + offset.
  * Intervals are cut to [0, Tk); a row that sees no key gives o = 0,
- * lse = -inf and no gradient.  With z = scale q_i.k_j:
+ * lse = -inf and no gradient (one that sees keys, all with scores of -inf, gives
+ * NaN, as the formula does).  With z = scale q_i.k_j:
  *   s = softcap tanh(z / softcap) (softcap 0: z) - slope[h] |i + offset - j|
  *   o_i = sum_j exp(s_j - lse_i) v_j,   lse_i = log sum_j exp(s_j)
  * (slopes float32 [heads], NULL: no bias; constants, without a gradient).

@@ -30,6 +30,16 @@ struct PagedArgs {
     // The first token that the row of token `at` sees.  A row before the first token sees none, and its number, down to
     // -2^20, would take the window's difference past 32 bits.
     __device__ __forceinline__ int oldest(int at) const { return window > 0 ? max(max(at, -1) - window + 1, 0) : 0; }
+    // What a row's sum of products is multiplied by.  A sum of probabilities of zero: the row sees no key in the cache, or its
+    // scores are all minus infinity, and 0 / 0 is not a number.
+    __device__ float inverse(float total, int b, int at) const {
+        if (total != 0.f) return 1.f / total;
+        for (int j = oldest(at); j <= at; j = (j | (page - 1)) + 1) {
+            const int n = table[b * table_row + (j >> shift)];
+            if (n >= 0 && n < pages) return NAN;
+        }
+        return 0.f;
+    }
 };
 
 constexpr int kChunk = 32;       // keys of a wave's step
@@ -270,7 +280,7 @@ __global__ __launch_bounds__((64 * PagedShape<E, DP>::WAVES)) void attn_paged_ke
         }
         if (ck.pieces == 1) {
             const int rr = rt * kRows16 + row;
-            const float inv = total == 0.f ? 0.f : 1.f / total;
+            const float inv = a.inverse(total, b, ck.len - a.fresh + rr / a.share);
             if (d < a.D)
                 store4<E>(a.o.ptr + (int64_t)(kv * a.share + rr % a.share) * a.o.head +
                               ((int64_t)b * a.fresh + rr / a.share) * a.o.row + d * ES,
@@ -331,7 +341,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs j) {
             total += l[n] * f;
         }
     }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float inv = a.inverse(total, b, ck.len - a.fresh + row / a.share);
     if (d < a.D)
         store4<E>(a.o.ptr + (int64_t)(kv * a.share + row % a.share) * a.o.head +
                       ((int64_t)b * a.fresh + row / a.share) * a.o.row + d * ES,

@@ -21,7 +21,7 @@ struct AttnArgs {
     const int* hi;
     const float* slopes;         // [heads], with the bias
     float* lse;                  // [heads, Tq], natural logarithm
-    float* lse2;                 // backward: lse log2 e, +inf for a row that sees nothing, and delta: [heads, Tpad]
+    float* lse2;                 // backward: lse log2 e, +inf for a row that sees no key, and delta: [heads, Tpad]
     float* delta;
     int* row_lo;                 // backward: the rows' first keys and numbers of keys, and of each 64 rows the bounds
     int* row_keys;
@@ -362,8 +362,9 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
     l = sum_halves(l);
     const bool ok = zero_of(acc, 0.f) == 0.f;
     uint32_t again = rows_of(row < a.Tq && !ok);
+    // A sum of zero: a row that sees no key, or one whose scores are all minus infinity, and 0 / 0 is not a number.
     if constexpr (!SPLIT) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = l != 0.f ? 1.f / l : own.lo < own.hi ? NAN : 0.f;
         if (row < a.Tq && !((again >> (lane & 31)) & 1u)) {
             char* op = a.o.ptr + w.head * a.o.head + (int64_t)row * a.o.row;
 #pragma unroll
@@ -385,6 +386,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
         if (lane == 0) flags[wave] = again;
         __syncthreads();
         again = flags[0] | flags[1] | flags[2] | flags[3];
+        const uint32_t sees = rows_of(own.lo < own.hi);
         // every lane's statistics of its row, over the waves
         float top = -INFINITY, total = 0.f, f[4];
 #pragma unroll
@@ -407,7 +409,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int x = 0; x < 4; ++x) v += *reinterpret_cast<const f32x4*>(meet.get(x, r) + d) * f[x];
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float inv = sum != 0.f ? 1.f / sum : (sees >> r) & 1u ? NAN : 0.f;
             if (d < a.D && row0 + r < a.Tq && !((again >> r) & 1u))
                 store4<E>(a.o.ptr + w.head * a.o.head + (int64_t)(row0 + r) * a.o.row + d * ES, v[0] * inv, v[1] * inv,
                           v[2] * inv, v[3] * inv);
@@ -513,6 +515,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a)
         delta = sum_halves(delta);
         const float lse = row < a.Tq ? a.lse[(int64_t)w.head * a.Tq + row] : -INFINITY;
         if (lse != -INFINITY) lse2 = lse * kLog2e;
+        else if (own.lo < own.hi) lse2 = NAN;   // its scores are all minus infinity
         if (h == 0 && row < a.Tpad && (!SPLIT || wave == 0)) a.lse2[(int64_t)w.head * a.Tpad + row] = lse2;
     }
     if (w.head == 0 && row0 % kPart == 0 && wave < (S::OWN + kPart - 1) / kPart) write_spans(a, row0 / kPart + wave, lane);

@@ -235,3 +235,60 @@ def test_gradient_rows_need_adjacent_columns(T):
     na.noble_qk_rope_bwd(dq, dk, qkv, None, None, None, None, None, heads=H, kv_heads=K, dqkv=into)
     assert torch.equal(into[:, :H * D], dq.view(T, -1)) and torch.equal(into[:, H * D:(H + K) * D], dk.view(T, -1))
     assert bool((wide[:, :16] == 7.0).all()) and bool((wide[:, 16 + (H + K) * D:] == 7.0).all())
+
+
+# ------------------------------------------- scores of minus infinity alone --
+
+@pytest.mark.parametrize("dt,H,K,D", [(BF, 4, 2, 64), (F32, 4, 2, 64), (BF, 96, 96, 64), (BF, 96, 48, 128)],
+                         ids=["bf16", "f32", "bf16_wide64", "bf16_wide128"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_rows_that_see_only_scores_of_minus_infinity(dt, H, K, D, bias):
+    """One document's keys are minus infinity before positive queries: its rows' exponentials are all 0 / 0.  Its results
+    are not numbers, the other documents' those of clean inputs, an empty row's zeros."""
+    print(f"[attn] -inf {dt} {H} {K} {D} {bias}", flush=True)
+    T, a, z = 150, 61, 70
+    g = _gen(61)
+    starts = torch.tensor([0, a, z, 140], dtype=torch.int32, device="cuda")
+    lo, hi, _ = na.noble_mask_rows(starts, T)
+    q, k, v, do = (_rand(g, s, dt) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
+    q = q.abs() + 0.125
+    slopes = torch.linspace(0.1, 1.0, H, device="cuda") if bias else None
+    want = attention(q, k, v, dense_mask(T, T, lo.cpu(), hi.cpu()), slopes=slopes, do=do)
+    k[a:z] = -math.inf
+    o, lse = na.noble_attn_fwd(q, k, v, lo, hi, slopes)
+    grads = na.noble_attn_bwd(do, q, k, v, o, lse, lo, hi, slopes)
+    ok = torch.ones(T, dtype=torch.bool)
+    ok[a:z] = False
+    for n, t in zip(("o", "dq", "dk", "dv"), (o, *grads)):
+        assert bool(t[a:z].isnan().all()), n
+        check(n, t.cpu()[ok], tuple(x[ok] for x in want[n]), dt)
+        assert n == "o" or bool((t[140:] == 0).all())
+    assert bool((o[140:] == 0).all()) and bool((lse[:, a:z] == -math.inf).all())
+    check("lse", lse.cpu()[:, ok], tuple(x[:, ok] for x in want["lse"]), dt)
+    k[a] = 0.5   # one of them is an ordinary score: it takes the rows alone
+    o, _ = na.noble_attn_fwd(q, k, v, lo, hi, slopes)
+    one = v[a].repeat_interleave(H // K, 0).float().cpu()
+    for i in range(a, z):
+        assert float((o[i].float().cpu() - one).abs().max()) <= 2.0 ** -7 * float(one.abs().max())
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("n,window", [(1, 0), (9, 0), (3000, 0), (3000, 40)])
+@pytest.mark.parametrize("new", [1, 2])
+def test_paged_rows_that_see_only_scores_of_minus_infinity(dt, n, window, new):
+    """Over the cache: not numbers, and zeros for a row that sees nothing, its pages outside the cache or its token before
+    the first."""
+    print(f"[paged] -inf {dt} {n} {window} {new}", flush=True)
+    H, K, D, page = 4, 2, 64, 16
+    per = -(-n // page)
+    g = _gen(62)
+    cache = _rand(g, (per + 1, 2, K, page, D), dt)
+    cache[:, 0] = -math.inf
+    table = torch.stack([torch.randperm(per + 1, generator=g, device="cuda")[:per], torch.full((per,), -1, device="cuda"),
+                         torch.zeros(per, dtype=torch.int64, device="cuda")]).to(torch.int32)
+    q = _rand(g, (3 * new, H, D), dt).abs() + 0.125
+    lens = torch.tensor([n, n, 0], dtype=torch.int32, device="cuda")
+    o = na.noble_attn_paged(q, cache, table, lens, window=window).view(3, new, H, D)
+    assert bool((o[1:] == 0).all())
+    for t in range(new):
+        assert bool(o[0, t].isnan().all()) if n - new + t >= 0 else bool((o[0, t] == 0).all())
