@@ -153,7 +153,7 @@ noble_status noble_kv_append(const noble_rope_desc* desc,
  * (slopes float32 [heads], NULL: no bias; constants, without a gradient).
  * Query head h uses key head h / (heads / kv_heads).  Infinite and NaN values
  * reach the rows that see them and no other (such rows, and those beside
- * them, are slow). */
+ * them, are slow, up to a key at a time, until they are all NaN). */
 typedef struct noble_attn_desc {
     int64_t Tq, Tk;       /* rows of q, and of k and v: up to 2^30 - 4096 */
     int64_t offset;       /* key index of query row 0, |offset| <= 2^30 - 4096 */

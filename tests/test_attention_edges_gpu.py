@@ -292,3 +292,64 @@ def test_paged_rows_that_see_only_scores_of_minus_infinity(dt, n, window, new):
     assert bool((o[1:] == 0).all())
     for t in range(new):
         assert bool(o[0, t].isnan().all()) if n - new + t >= 0 else bool((o[0, t] == 0).all())
+
+
+# ----------------------------------------------------- what not-a-number costs --
+
+def _ms(f, n=3):
+    f()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    for _ in range(n):
+        f()
+    b.record()
+    torch.cuda.synchronize()
+    return a.elapsed_time(b) / n
+
+
+@pytest.mark.parametrize("what", ["do", "v", "q"])
+def test_a_step_of_nan_takes_milliseconds(what):
+    """A training step whose values or upstream gradient have all turned into NaN: a row or key whose sums are NaN already
+    is done.  About 64 rows a wave, a few microseconds each: ten times the clean step and a millisecond leave room."""
+    print(f"[attn] cost {what}", flush=True)
+    T, H, K, D = 2048, 8, 8, 128
+    g = _gen(81)
+    x = dict(q=_rand(g, (T, H, D), BF), k=_rand(g, (T, K, D), BF), v=_rand(g, (T, K, D), BF), do=_rand(g, (T, H, D), BF))
+
+    def step():
+        o, lse = na.noble_attn_fwd(x["q"], x["k"], x["v"])
+        return na.noble_attn_bwd(x["do"], x["q"], x["k"], x["v"], o, lse)
+
+    clean = _ms(step)
+    x[what].fill_(math.nan)
+    bad = _ms(step)
+    print(f"clean {clean:.3f} ms, {what} NaN {bad:.3f} ms", flush=True)
+    assert bad <= 10 * clean + 1.0
+    dq, dk, dv = step()
+    assert bool(dk.isnan().all()) and bool(dq.isnan().all())
+    assert bool(dv.isnan().all()) == (what != "v")
+
+
+@pytest.mark.parametrize("dt,H,K,D", [(BF, 4, 2, 64), (F32, 4, 2, 64), (BF, 96, 96, 128), (BF, 8, 1, 96)])
+def test_infinite_gradients_over_many_documents(dt, H, K, D):
+    """Infinite upstream gradients in one row of every third document: the keys that the row sees, in their documents and
+    between their tiles, and no other."""
+    print(f"[attn] inf documents {dt} {H} {K} {D}", flush=True)
+    T = 450
+    g = _gen(82)
+    starts = torch.cat([torch.arange(0, T, 50), torch.tensor([T])]).to(torch.int32).cuda()
+    lo, hi, _ = na.noble_mask_rows(starts, T)
+    q, k, v, do = (_rand(g, s, dt) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
+    want = attention(q, k, v, dense_mask(T, T, lo.cpu(), hi.cpu()), do=do)
+    hit = torch.zeros(T, dtype=torch.bool)
+    for a in range(0, T, 150):
+        do[a + 20, 0, 3] = math.inf
+        hit[a:a + 21] = True
+    o, lse = na.noble_attn_fwd(q, k, v, lo, hi)
+    dq, dk, dv = na.noble_attn_bwd(do, q, k, v, o, lse, lo, hi)
+    for n, t in (("dk", dk), ("dv", dv)):
+        check(n, t.cpu()[~hit], tuple(x[~hit] for x in want[n]), dt)
+    assert bool((dv[hit.cuda(), 0, 3] == math.inf).all()) and not bool(dk[hit.cuda(), 0].isfinite().any())
+    rest = torch.arange(D) != 3   # the value's other elements
+    check("dv", dv.cpu()[hit][..., rest], tuple(x[hit][..., rest] for x in want["dv"]), dt)
