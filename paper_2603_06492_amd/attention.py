@@ -20,6 +20,7 @@ import os
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import noble
 from .noble import NobleError, _dtype_code, _on, _stream
@@ -468,6 +469,7 @@ class QKRope(torch.autograd.Function):
         return noble_qk_rope_fwd(qkv, q_weight, k_weight, cos, sin, positions, **ctx.how)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         dqkv, dqw, dkw = noble_qk_rope_bwd(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, **ctx.how)
         return (dqkv, dqw, dkw) + (None,) * 7
@@ -485,6 +487,7 @@ class Attention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         return noble_attn_bwd(do.contiguous(), *ctx.saved_tensors, **ctx.how) + (None,) * 6
 
@@ -505,6 +508,7 @@ class RopeAttention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         qkv, q_weight, k_weight, cos, sin, positions, q, k, o, lse, *mask = ctx.saved_tensors
         dqkv = torch.empty_like(qkv)

@@ -353,3 +353,29 @@ def test_infinite_gradients_over_many_documents(dt, H, K, D):
     assert bool((dv[hit.cuda(), 0, 3] == math.inf).all()) and not bool(dk[hit.cuda(), 0].isfinite().any())
     rest = torch.arange(D) != 3   # the value's other elements
     check("dv", dv.cpu()[hit][..., rest], tuple(x[hit][..., rest] for x in want["dv"]), dt)
+
+
+# ------------------------------------------------------ second derivatives --
+
+def test_second_derivatives_are_refused():
+    """The backwards are not differentiable: a penalty on a gradient raises, it is not taken for a constant."""
+    T, H, K, D = 20, 2, 1, 32
+    g = _gen(91)
+    qkv = _rand(g, (T, (H + 2 * K) * D)).requires_grad_(True)
+    w = torch.ones(D, device="cuda", requires_grad=True)
+    cos, sin = na.noble_rope_table(T, 32)
+
+    def whole():
+        return na.RopeAttention.apply(qkv, w, w, cos, sin, None, None, None, None, H, K)
+
+    def rope():
+        return torch.cat(na.QKRope.apply(qkv, w, w, cos, sin, None, H, K), 1)
+
+    def attn():
+        q, k, v = (qkv[:, a * D:b * D].reshape(T, b - a, D) for a, b in ((0, H), (H, H + K), (H + K, H + 2 * K)))
+        return na.Attention.apply(q, k, v)
+
+    for f in (whole, rope, attn):
+        first, = torch.autograd.grad(f().square().sum(), qkv, create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiate twice"):
+            (qkv.sum() + first.square().sum()).backward()
