@@ -564,6 +564,11 @@ class PagedCache:
         return (torch.tensor(positions, dtype=torch.int32, device=dev),
                 torch.tensor(slots, dtype=torch.int64, device=dev))
 
+    @property
+    def held(self) -> int:
+        """Tokens of the sequence that holds the most."""
+        return max(self._held, default=0)
+
     def release(self, sequence: int) -> None:
         """Gives a sequence's pages back; it holds no tokens then."""
         self._free += reversed(self._table[sequence])
@@ -579,7 +584,9 @@ class NobleSelfAttention(torch.nn.Module):
     widths allow it), norm and rotation of the heads, attention, and a NOBLE layer for O.  Parameters and initialisation
     of the two layers are NobleLinear's; the norms' weights are float32 ones.
 
-    ``forward`` takes packed rows or a batch and trains; ``step`` serves prompts and single tokens from a PagedCache."""
+    ``forward`` takes packed rows or a batch and trains; ``step`` serves prompts and single tokens from a PagedCache.
+    Positions are rotated up to ``longest`` tokens; longer sequences are refused (in packed rows, whose lengths only the
+    device knows, their later tokens come out as NaN)."""
 
     def __init__(self, d: int, heads: int, r: int, *, kv_heads: Optional[int] = None, head_dim: Optional[int] = None,
                  rot: Optional[int] = None, base: float = 10000.0, longest: int = 2048, scaling: Optional[dict] = None,
@@ -607,6 +614,10 @@ class NobleSelfAttention(torch.nn.Module):
         """The mask of packed rows, for every layer and step over them: noble_mask_rows."""
         return noble_mask_rows(starts, T, prefix=prefix, causal=causal, window=window)
 
+    def _fits(self, tokens: int) -> None:
+        if self.cos is not None and tokens > self.longest:
+            raise ValueError(f"a sequence of {tokens} tokens, the positions' tables hold longest={self.longest}")
+
     def forward(self, x, mask=None, causal: bool = True):
         """x [T, d] (one sequence, or packed documents with their ``mask``) or [B, S, d]."""
         shape = x.shape
@@ -614,6 +625,7 @@ class NobleSelfAttention(torch.nn.Module):
         T = x.shape[0]
         if mask is None:
             S = shape[-2]
+            self._fits(S)
             mask = self.mask(torch.arange(0, T + 1, max(S, 1), dtype=torch.int32, device=x.device), T, causal=causal)
         key_lo, key_hi, positions = mask
         o = RopeAttention.apply(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, key_lo, key_hi,
@@ -626,6 +638,7 @@ class NobleSelfAttention(torch.nn.Module):
         """The newest tokens of every sequence, x [sequences * new, d], with the positions and slots that
         ``cache.extend(new)`` gave: their keys and values go into the cache, their attention runs over it.  A whole prompt
         is a step too."""
+        self._fits(cache.held)
         q = noble_kv_append(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, slots,
                             cache.data[layer], **self.how)
         o = noble_attn_paged(q, cache.data[layer], cache.page_table, cache.lengths, self.slopes, softcap=self.softcap)

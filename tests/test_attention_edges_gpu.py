@@ -379,3 +379,24 @@ def test_second_derivatives_are_refused():
         first, = torch.autograd.grad(f().square().sum(), qkv, create_graph=True)
         with pytest.raises(RuntimeError, match="differentiate twice"):
             (qkv.sum() + first.square().sum()).backward()
+
+
+# ------------------------------------------------------------------ module --
+
+def test_lengths_past_the_tables_are_refused():
+    """Sequences longer than the module's positions: refused where the host knows the length, in a batch, one sequence and a
+    cache; a module that rotates nothing takes them."""
+    m = na.NobleSelfAttention(64, 2, 8, longest=16)
+    x = torch.randn(2, 17, 64, device="cuda", generator=_gen(95)).to(BF)
+    for y in (x, x[0]):
+        with pytest.raises(ValueError, match="longest"):
+            m(y)
+    assert bool(m(x[:, :16]).isfinite().all())
+    cache = na.PagedCache(2, 40, 12, kv_heads=2, head_dim=32, page=8)
+    assert cache.held == 0
+    assert bool(m.step(x[:, :16].reshape(-1, 64), cache, *cache.extend(16)).isfinite().all()) and cache.held == 16
+    with pytest.raises(ValueError, match="longest"):
+        m.step(x[:, 16].contiguous(), cache, *cache.extend(1))
+    still = na.NobleSelfAttention(64, 2, 8, longest=16, rot=0)
+    assert bool(still(x).isfinite().all())
+    assert bool(still.step(x[:, 16].contiguous(), cache, *cache.extend(1)).isfinite().all())
