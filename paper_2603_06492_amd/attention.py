@@ -634,14 +634,16 @@ class NobleSelfAttention(torch.nn.Module):
         return self.out(o.reshape(T, -1)).reshape(shape)
 
     @torch.no_grad()
-    def step(self, x, cache: PagedCache, positions, slots, layer: int = 0):
+    def step(self, x, cache: PagedCache, positions, slots, layer: int = 0, window: int = 0):
         """The newest tokens of every sequence, x [sequences * new, d], with the positions and slots that
         ``cache.extend(new)`` gave: their keys and values go into the cache, their attention runs over it.  A whole prompt
-        is a step too."""
+        is a step too.  A token sees those up to itself, with a ``window`` (the one that ``mask`` took for training) only
+        that many; a mask with a prefix or without ``causal`` has no such form: feed its tokens to ``forward``."""
         self._fits(cache.held)
         q = noble_kv_append(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, slots,
                             cache.data[layer], **self.how)
-        o = noble_attn_paged(q, cache.data[layer], cache.page_table, cache.lengths, self.slopes, softcap=self.softcap)
+        o = noble_attn_paged(q, cache.data[layer], cache.page_table, cache.lengths, self.slopes, softcap=self.softcap,
+                             window=window)
         return self.out(o.reshape(x.shape[0], -1))
 
     def param_groups(self, lr):

@@ -400,3 +400,22 @@ def test_lengths_past_the_tables_are_refused():
     still = na.NobleSelfAttention(64, 2, 8, longest=16, rot=0)
     assert bool(still(x).isfinite().all())
     assert bool(still.step(x[:, 16].contiguous(), cache, *cache.extend(1)).isfinite().all())
+
+
+@pytest.mark.parametrize("window", [7, 20])
+def test_module_decodes_with_the_window_that_it_trains_with(window):
+    """A forward with a window, and a prompt and single tokens with the same: the same sums in another order, 1% of the
+    output's norm."""
+    B, S, d = 2, 33, 128
+    m = na.NobleSelfAttention(d, 4, 16, kv_heads=2, longest=64, seed=4)
+    x = torch.randn(B, S, d, device="cuda", generator=_gen(101)).to(BF)
+    starts = torch.arange(0, B * S + 1, S, dtype=torch.int32, device="cuda")
+    with torch.no_grad():
+        whole = m(x, m.mask(starts, B * S, window=window))
+        assert float((whole - m(x)).norm() / whole.norm()) > 0.05   # the window matters here
+    cache = na.PagedCache(B, 64, 40, kv_heads=2, head_dim=m.head_dim, page=8)
+    outs = [m.step(x[:, :20].reshape(-1, d), cache, *cache.extend(20), window=window).view(B, 20, d)]
+    for t in range(20, S):
+        outs.append(m.step(x[:, t].contiguous(), cache, *cache.extend(1), window=window)[:, None])
+    off = torch.cat(outs, 1).float() - whole.float()
+    assert float(off.norm() / whole.float().norm()) <= 1e-2
