@@ -544,6 +544,8 @@ class PagedCache:
         """Room for ``new`` more tokens of every sequence: (positions int32, slots int64), both [sequences * new], a
         sequence's tokens in a row.  Raises MemoryError when the pages run out and ValueError past ``longest``; nothing has
         changed then."""
+        if new < 0:
+            raise ValueError(f"{new} new tokens")
         if max(self._held) + new > self.longest:
             raise ValueError(f"sequences of up to {self.longest} tokens: {max(self._held)} held, {new} more")
         need = [-(-(n + new) // self.page) - len(t) for n, t in zip(self._held, self._table)]
