@@ -21,11 +21,13 @@ BINDINGS = [("noble_torch.cpp", BINDING), ("noble_attn_torch.cpp", os.path.join(
 SOURCES = ["noble_api.hip", "noble_attn.hip"]
 HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_binding.h", "noble_torch.cpp", "noble_attn_torch.cpp"]
 
+# of the library; its objects are compiled with all but -shared
 HIP_FLAGS = [
     "-O3",
     "-std=c++20",
     "--offload-arch=gfx950",
     "-fPIC",
+    "-shared",
     "-munsafe-fp-atomics",
     # no packed-FP32 instructions in device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -41,7 +43,7 @@ def hipcc() -> str:
 
 
 def _hipcc(args, verbose: bool) -> None:
-    cmd = [hipcc(), *HIP_FLAGS, *args]
+    cmd = [hipcc(), *[f for f in HIP_FLAGS if f != "-shared" or "-c" not in args], *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -57,7 +59,7 @@ def build(verbose: bool = False) -> str:
         # the sources side by side, then one link
         list(pool.map(lambda so: _hipcc(["-c", "-I", INCLUDE, "-I", CSRC, os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
                       zip(SOURCES, objs)))
-        _hipcc(["-shared", *objs, "-o", tmp], verbose)
+        _hipcc([*objs, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     build_binding(verbose)
     return LIB
