@@ -419,3 +419,45 @@ def test_module_decodes_with_the_window_that_it_trains_with(window):
         outs.append(m.step(x[:, t].contiguous(), cache, *cache.extend(1), window=window)[:, None])
     off = torch.cat(outs, 1).float() - whole.float()
     assert float(off.norm() / whole.float().norm()) <= 1e-2
+
+
+# --------------------------------------------------------------- long rows --
+
+@pytest.mark.parametrize("dt,T,H,K,D,kind", [(BF, 2100, 8, 2, 128, "causal"), (BF, 2100, 8, 8, 64, "documents"),
+                                             (F32, 1300, 2, 1, 64, "causal")])
+def test_rows_of_thousands_of_keys(dt, T, H, K, D, kind):
+    """Enough rows of few heads for workgroups of 128 rows, and many tiles in each; bounds as at every size."""
+    print(f"[attn] long {dt} {T} {H} {K} {D} {kind}", flush=True)
+    g = _gen(111)
+    q, k, v, do = (_rand(g, s, dt) for s in ((T, H, D), (T, K, D), (T, K, D), (T, H, D)))
+    lo = hi = None
+    if kind == "documents":   # of 1000, 1 and 1088 rows, the last 11 in none
+        lo, hi, _ = na.noble_mask_rows(torch.tensor([0, 1000, 1001, 2089], dtype=torch.int32, device="cuda"), T)
+    causal = kind == "causal"
+    o, lse = na.noble_attn_fwd(q, k, v, lo, hi, causal=causal, softcap=3.0)
+    dq, dk, dv = na.noble_attn_bwd(do, q, k, v, o, lse, lo, hi, causal=causal, softcap=3.0)
+    seen = dense_mask(T, T, *((None, None) if lo is None else (lo.cpu(), hi.cpu())), causal)
+    want = attention(q, k, v, seen, softcap=3.0, do=do)
+    for n, t in dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        check(n, t, want[n], dt)
+
+
+@pytest.mark.parametrize("dt,H,K,D,page,window", [(BF, 16, 2, 128, 16, 0), (BF, 4, 4, 64, 64, 150), (F32, 4, 1, 96, 8, 0)])
+def test_prompts_over_the_cache(dt, H, K, D, page, window):
+    """Hundreds of new tokens a sequence, a whole prompt and a chunk of a longer one."""
+    print(f"[paged] prompt {dt} {H} {K} {D} {page} {window}", flush=True)
+    lengths, new = [300, 777], 300
+    g = _gen(112)
+    per = -(-max(lengths) // page)
+    cache = _rand(g, (2 * per + 1, 2, K, page, D), dt)
+    table = torch.randperm(2 * per + 1, generator=g, device="cuda")[:2 * per].view(2, per).to(torch.int32)
+    q = _rand(g, (2 * new, H, D), dt)
+    o = na.noble_attn_paged(q, cache, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), window=window,
+                            softcap=3.0)
+    for b, n in enumerate(lengths):
+        t = torch.arange(n, device="cuda")
+        k, v = (cache[table[b].long()[t // page], i, :, t % page] for i in (0, 1))
+        at = torch.arange(n - new, n)
+        lo = (at - window + 1).clamp(min=0) if window else torch.zeros_like(at)
+        rows = slice(b * new, (b + 1) * new)
+        check("o", o[rows], attention(q[rows], k, v, dense_mask(new, n, lo, at + 1), softcap=3.0)["o"], dt)
