@@ -218,6 +218,8 @@ AttnArgs attn_args(const noble_attn_desc* d, const int32_t* lo, const int32_t* h
 // 51.2 + 142, 256 workgroups 71.7 + 205 and 66.1 + 197.  Float32, the same way and with the same tiles of 32 rows for
 // both: heads of 64, 8 x 2048 rows 94 + 291 and 165 + 505, 8 x 4096 rows 347 + 1101 and 319 + 1002, 16 x 4096 rows 691 +
 // 2195 and 534 + 1771; heads of 128, 8 x 4096 rows 617 + 2196 and 658 + 2288, 24 x 5516 rows 3496 + 12661 and 3781 + 16351.
+// So float32 heads of up to 64 over 8 x 4096 rows and more would take 8 to 23% less time unsplit: another set of float32
+// kernels for those calls alone, which is not built.
 template <typename E, int DP>
 bool split_rows(int64_t rows, int64_t heads) {
     return sizeof(E) == 4 || cdiv(rows, kOwn) * heads < (DP == 64 ? 192 : 128);

@@ -8,8 +8,9 @@
 // Pieces of one sequence are joined by attn_join_kernel, in their order.
 //
 // What bounds it: reading the cache, once.  64 sequences of 16384 to 32768 tokens, 16 heads of 128 over 4 key heads: 3.2 GB
-// in 506 us, 6.4 TB/s; 16 sequences of 130 to 8192 tokens, 16 key heads: 0.55 GB in 108 us, 5.0 TB/s.  One token over 1000
-// keys takes 6 us and 3 for the join: the latencies of lengths, page table, cache and partial results in a row.
+// in 514 us, 6.3 TB/s; 16 sequences of 130 to 8192 tokens, 16 key heads: 0.55 GB in 109 us, 5.0 TB/s.  One token over 1000
+// keys takes 6 us and 3 for the join: the latencies of lengths, page table, cache and partial results in a row.  It is made for
+// few new tokens: a prompt reads its keys once for every 16 rows (4096 tokens, 16 heads over 4: 0.65 ms, attn_fwd_kernel 0.10).
 #pragma once
 
 #include "noble_attn_common.hpp"
@@ -22,7 +23,7 @@ struct PagedArgs {
     const int* table;
     const int* lengths;
     const float* slopes;
-    float* part;          // [workgroup][16][DP + 2] float32: product, maximum, sum
+    float* part;          // [workgroup][16][DP + 4] float32: product, maximum, sum
     int64_t table_row, pages, page_bytes;   // page_bytes: of one page, keys and values of all heads
     int page, shift, fresh, window, heads, kv_heads, share, D;
     int row_tiles, pieces;

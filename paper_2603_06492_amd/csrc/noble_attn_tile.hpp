@@ -259,9 +259,9 @@ __device__ __forceinline__ float one_probability(const AttnArgs& a, const Pair& 
 
 // Forward.  What bounds it at long rows: the issue slots that a score's 5 to 12 vector operations take (its exponential
 // counts for four) beside the matrix cores, at the clock that both together leave: a prompt of 16384 tokens, 16 heads of
-// 128 over 4 key heads, prefix mask and bias, 1.25 ms, 0.97 PFLOP/s; a large library product reaches 1.25 on this card.
+// 128 over 4 key heads, prefix mask and bias, 1.26 ms, 0.97 PFLOP/s; a large library product reaches 1.25 on this card.
 // Packed short rows are bound by the steps that follow each other in one workgroup: 8 x 1024 tokens, 8 heads of 128,
-// causal, 32.5 us (0.53 PFLOP/s of seen pairs), 128 images of 197 tokens, 12 heads of 64, 55 us (2.8 TB/s).
+// causal, 32.6 us (0.53 PFLOP/s of seen pairs), 128 images of 197 tokens, 12 heads of 64, 53 us (2.9 TB/s).
 template <typename E, int DP, int MODE, bool SPLIT>
 __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_fwd_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
@@ -478,7 +478,7 @@ __device__ __forceinline__ void write_spans(const AttnArgs& a, int tile, int lan
 // dq, and what the dk/dv launch after it reads: delta (do is here already, o is read once for it), lse in units of log2,
 // the rows' intervals and what 64 of them span.  delta is do.o of the rounded o, plus what is left of sum p (dp - delta)
 // after the row's keys, which an exact one would make zero: so dk does not carry o's rounding.
-// Three products a tile where the forward has two: 8 x 1024 tokens 47 us, the images 75 us.
+// Three products a tile where the forward has two: 8 x 1024 tokens 48 us, the images 71 us.
 template <typename E, int DP, int MODE, bool SPLIT>
 __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
     using T = Tile<E, DP>;
@@ -706,7 +706,7 @@ struct Partners {
 // bf16 heads of 128: the two sums (128 registers), the keys (32), S and dP (32) and the operands read ahead leave no room
 // for the values in the 256 registers that a wave has when two share a SIMD, so the values are read from LDS for every
 // tile, and tiles are 32 rows, so that two workgroups fit a CU's LDS.  With the values in registers and one wave a SIMD
-// 8 x 1024 tokens took 104 us, with 64 keys a wave 94, this way 65; 128 images of 12 heads of 64 take 93.
+// 8 x 1024 tokens took 104 us, with 64 keys a wave 94, this way 65 to 67; 128 images of 12 heads of 64 take 89.
 template <typename E, int DP, bool SPLIT>
 struct DkvShape {
     static constexpr bool VALUES_IN_LDS = !SPLIT && sizeof(E) == 2 && DP == 128;

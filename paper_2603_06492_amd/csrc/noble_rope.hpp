@@ -3,8 +3,8 @@
 // One pass over the Q/K/V layer's rows.  Sixteen lanes (eight for D <= 64) hold a head, eight elements each: the
 // head's mean square is four (three) lane exchanges away, a half-layout pair's other element one.  A lane group stays
 // at one token and steps over its heads, so the token's cosines and sines are read once.  Bound by memory: 32768 tokens of
-// 16 + 16 heads of 128 in bf16, forward 95 us (5.6 TB/s), backward 170 us (4.7 TB/s) and 5 us for the weights' sums;
-// 3108 prompt tokens of 16 + 4 heads into the cache 10 us, 16 single tokens 4 us, which is a launch.
+// 16 + 16 heads of 128 in bf16, forward 95 us (5.6 TB/s), backward 167 to 182 us (4.4 to 4.8 TB/s) and 5 us for the weights' sums;
+// 3108 prompt tokens of 16 + 4 heads into the cache 11 us, 16 single tokens 4 us, which is a launch.
 #pragma once
 
 #include "noble_attn_common.hpp"
