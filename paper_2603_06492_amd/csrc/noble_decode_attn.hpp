@@ -1,0 +1,536 @@
+// Attention of each sequence's newest tokens over the paged cache where a row does not simply see every token before it:
+// a tree of drafted tokens (kTree), pages that were selected for each row and key head (kBlocks), and the plain order with
+// the scores kept, from which the weight of every cached token is formed (kWeigh).
+//
+// As in attn_paged_kernel, a workgroup takes rows (new tokens x query heads that share a key head) of one sequence and key
+// head and one piece of its keys; its waves take turns at chunks of 32 keys, which come to LDS without passing through
+// registers, through a ring of each wave's own, and their results meet in LDS.  Here a workgroup has R groups of 16 rows,
+// the columns of R sets of 16x16x32 MFMAs that share every operand read from LDS: a tree of 16 tokens with four heads to
+// a key head reads its cache once, not four times.
+#pragma once
+
+#include "noble_attn_common.hpp"
+
+namespace noble {
+
+enum { kTree = 0, kBlocks = 1, kWeigh = 2 };
+
+struct DecodeArgs {
+    HeadRows q, o;
+    const char* cache;
+    const int* table;
+    const int* lengths;
+    const float* slopes;
+    float* part;          // [workgroup][16 R][DP + 4] float32: product, maximum, sum, (first piece) number of pieces
+    int64_t table_row, pages, page_bytes;   // page_bytes: of one page, keys and values of all heads
+    int page, shift, fresh, heads, kv_heads, share, D;
+    int row_tiles, pieces;
+    ScoreArgs sc;
+    const uint32_t* seen;   // kTree: [B, fresh, words]
+    const int* depths;      // [B, fresh]
+    int words;
+    int count;              // kBlocks: entries of a list
+    const int* chosen;      // [B fresh, kv_heads, count]
+    float* z;               // kWeigh: scores [B, kv_heads, fresh share, z_row], times log2 e
+    float2* stats;          // [B, kv_heads, fresh share]: maximum, 1 / sum
+    int64_t z_row;
+
+    __device__ __forceinline__ int held(int b) const {
+        return (int)min((int64_t)max(lengths[b], 0), table_row * page);
+    }
+    __device__ __forceinline__ bool there(int b, int block) const {
+        const int n = table[b * table_row + block];
+        return n >= 0 && n < pages;
+    }
+    __device__ __forceinline__ const uint32_t* line(int b, int tok) const {
+        return seen + ((int64_t)b * fresh + tok) * words;
+    }
+    __device__ __forceinline__ const int* list(int b, int tok, int kv) const {
+        return chosen + (((int64_t)b * fresh + tok) * kv_heads + kv) * count;
+    }
+};
+
+// Bits c .. c + 31 of a node's line; places before the tree are all seen.
+__device__ __forceinline__ uint32_t line_bits(const uint32_t* line, int words, int c) {
+    if (c <= -32) return ~0u;
+    if (c < 0) return (line[0] << -c) | ((1u << -c) - 1u);
+    const int i = c >> 5, s = c & 31;
+    const uint32_t lo = i < words ? line[i] : 0u, hi = i + 1 < words ? line[i + 1] : 0u;
+    return s ? (lo >> s) | (hi << (32 - s)) : lo;
+}
+__device__ __forceinline__ bool line_holds(const uint32_t* line, int c) { return line[c >> 5] >> (c & 31) & 1u; }
+
+constexpr int kKeys = 32;        // keys of a wave's step
+constexpr int kGroup = 16;       // rows of a group
+
+// Entries of a row's list up to the first that is not larger than the one before it, negative or past the row's own block.
+__device__ __forceinline__ int list_length(const int* list, int count, int last, int lane) {
+    int n = 0;
+    for (int i0 = 0; i0 < count; i0 += 64) {
+        const int i = i0 + lane;
+        const bool in = i < count;
+        const int e = in ? list[i] : -1, before = in && i > 0 ? list[i - 1] : -1;
+        const uint64_t end = ~__ballot(in && e > before && e <= last);
+        const int run = end ? __builtin_ctzll(end) : 64;
+        n += run;
+        if (run < 64) break;
+    }
+    return n;
+}
+
+// What a row's sum of products is multiplied by where its sum of probabilities is zero: it sees no key in the cache (0), or its
+// scores are all minus infinity, and 0 / 0 is not a number.
+template <int FORM>
+__device__ float decode_empty(const DecodeArgs& a, int b, int kv, int tok) {
+    const int first = a.held(b) - a.fresh, at = first + tok;
+    if constexpr (FORM == kBlocks) {
+        const int* list = a.list(b, tok, kv);
+        const int last = at >= 0 ? at >> a.shift : -1;
+        for (int i = 0, before = -1; i < a.count && list[i] > before && list[i] <= last; ++i) {
+            before = list[i];
+            if (a.there(b, before)) return NAN;
+        }
+        return 0.f;
+    } else {
+        const int end = FORM == kTree ? first : at + 1;
+        for (int j = 0; j < end; j += a.page)
+            if (a.there(b, j >> a.shift)) return NAN;
+        if constexpr (FORM == kTree) {
+            const uint32_t* line = a.line(b, tok);
+            for (int c = max(-first, 0); c <= tok; ++c)
+                if (line_holds(line, c) && a.there(b, (first + c) >> a.shift)) return NAN;
+        }
+        return 0.f;
+    }
+}
+
+// Four elements of a row of o from the row's sums.
+template <typename E, int FORM>
+__device__ __forceinline__ void decode_store(const DecodeArgs& a, int b, int kv, int tok, int in_tok, int d, f32x4 sum,
+                                             float total) {
+    const float inv = total != 0.f ? 1.f / total : decode_empty<FORM>(a, b, kv, tok);
+    if (FORM == kTree && !line_holds(a.line(b, tok), tok)) sum = f32x4{0.f, 0.f, 0.f, 0.f};   // no node, whatever it met
+    else sum *= inv;
+    if (d < a.D)
+        store4<E>(a.o.ptr + (int64_t)(kv * a.share + in_tok) * a.o.head + ((int64_t)b * a.fresh + tok) * a.o.row +
+                      d * (int)sizeof(E),
+                  sum[0], sum[1], sum[2], sum[3]);
+}
+
+template <typename E, int DP>
+struct DecodeShape {
+    static constexpr int WAVES = sizeof(E) * DP > 256 ? 2 : 4;
+    static constexpr int STAGE = 2 * kKeys * DP * (int)sizeof(E);             // keys and values of a chunk
+    static constexpr int STAGES = 128 * 1024 / (WAVES * STAGE);
+};
+
+template <typename E, int DP, int FORM, int MODE, int R>
+__global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_kernel(DecodeArgs a) {
+    using T = Tile<E, DP>;
+    using S = DecodeShape<E, DP>;
+    constexpr int ES = T::ES, NS = DP / 32, ND = DP / 16, W = S::WAVES, NST = S::STAGES;
+    constexpr int RPI = 1024 / T::RB, PER = kKeys / RPI;   // rows of a request, requests of a chunk's keys
+    __shared__ __attribute__((aligned(1024))) char lds[W * NST * S::STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g4 = lane >> 4;
+    // pieces of one (sequence, key head) apart, key heads of a sequence side by side: their pages are the same
+    int w = blockIdx.x;
+    const int kv = w % a.kv_heads;
+    w /= a.kv_heads;
+    const int rt = w % a.row_tiles;
+    w /= a.row_tiles;
+    const int piece = w % a.pieces, b = w / a.pieces, db = a.D * ES;
+
+    // this lane's row of each group.  kBlocks: a tile's rows are one token's; else tokens x heads, one after the other
+    const int per_tok = FORM == kBlocks ? (a.share + kGroup - 1) / kGroup : 1;
+    const int rows = FORM == kBlocks ? a.share : a.fresh * a.share;
+    const int row0 = (FORM == kBlocks ? rt % per_tok : rt * R) * kGroup;
+    const int tok0 = FORM == kBlocks ? rt / per_tok : row0 / a.share;
+    const int tok1 = FORM == kBlocks ? tok0 : (min(rows, row0 + R * kGroup) - 1) / a.share;
+    bool live[R];
+    int tok[R], head[R];
+    Frag<E> q[R][NS];
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+        const int r = row0 + g * kGroup + n16;
+        live[g] = r < rows;
+        tok[g] = FORM == kBlocks ? tok0 : live[g] ? r / a.share : tok1;
+        head[g] = live[g] ? kv * a.share + r - (FORM == kBlocks ? 0 : tok[g] * a.share) : 0;
+        const char* qp = a.q.ptr + (int64_t)head[g] * a.q.head + ((int64_t)b * a.fresh + tok[g]) * a.q.row;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int d = 32 * s + 8 * g4;
+            q[g][s] = global_frag<E>(qp + d * ES, live[g] && d < a.D);
+        }
+    }
+    const int len = a.held(b), first = len - a.fresh;   // first: place of the first new token
+    const int* list = FORM == kBlocks ? a.list(b, tok0, kv) : nullptr;
+    // the keys are [0, end): tokens of the sequence, or (kBlocks) of the listed pages in a row
+    int end, listed = 0;
+    if constexpr (FORM == kBlocks) {
+        const int at = first + tok0;
+        listed = __builtin_amdgcn_readfirstlane(list_length(list, a.count, at >= 0 ? at >> a.shift : -1, lane));
+        end = listed > 0 ? (listed - 1) * a.page + min(a.page, at + 1 - list[listed - 1] * a.page) : 0;
+        end = __builtin_amdgcn_readfirstlane(end);
+    } else {
+        end = max(first + tok1 + 1, 0);
+    }
+    const int chunks = (end + kKeys - 1) / kKeys;
+    const int pieces = max(1, min(a.pieces, chunks / W));
+    if (piece >= pieces) return;
+    const int c0 = (int)((int64_t)chunks * piece / pieces) + wave, c1 = (int)((int64_t)chunks * (piece + 1) / pieces);
+    float slope[R];
+    int at[R];   // a row's position, which the bias goes by
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+        slope[g] = a.slopes ? a.slopes[head[g]] * kLog2e / a.sc.unit : 0.f;
+        at[g] = first + (FORM == kTree ? a.depths[(int64_t)b * a.fresh + tok[g]] : tok[g]);
+    }
+
+    char* ring = lds + wave * NST * S::STAGE;
+    typedef const __attribute__((address_space(4))) int* table_ptr;
+    const table_ptr table = (table_ptr)(a.table + b * a.table_row);
+    const table_ptr blocks = (table_ptr)list;
+    uint32_t bad = 0;   // keys of the next chunk without a page in the cache
+    uint32_t bads[NST];
+    const auto request = [&](int c, int stage) {
+        const int k0 = c * kKeys;
+        char* dst = ring + stage * S::STAGE;
+        const int in_page = k0 & (a.page - 1);
+        const char* base = a.cache + (int64_t)kv * a.page * db + (int64_t)in_page * db;
+        int page = -1;
+        bad = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int key = k0 + i * RPI, left = max(min(end - key, RPI), 0);
+            // a new page starts here, or the chunk does; pages hold at least a request's rows
+            if (i == 0 || ((in_page + i * RPI) & (a.page - 1)) == 0) {
+                page = -1;
+                if (left > 0) page = table[FORM == kBlocks ? blocks[key >> a.shift] : key >> a.shift];
+                if (i > 0) base = a.cache + (int64_t)kv * a.page * db - (int64_t)i * RPI * db;
+            }
+            const bool ok = page >= 0 && page < a.pages;
+            if (!ok) bad |= ((1u << RPI) - 1u) << (i * RPI);
+            const char* src = base + (int64_t)(ok ? page : 0) * a.page_bytes + (int64_t)i * RPI * db;
+            const int row = i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(row);
+            const uint32_t vo = 16 * ch < db ? (uint32_t)((lane / T::NC) * db + 16 * ch) : kOOB;
+            const int64_t bytes = ok ? (int64_t)left * db : 0;
+            dma16(wave_desc(src, bytes), dst + i * 1024, vo, 0);
+            dma16(wave_desc(src + (int64_t)a.kv_heads * a.page * db, bytes), dst + S::STAGE / 2 + i * 1024, vo, 0);
+        }
+    };
+    // Which of this lane's eight keys of the chunk at k0 (places 16 (i / 4) + 4 g4 + i % 4) the row of a token sees.
+    const auto sees = [&](int t, int k0) {
+        uint32_t mask;
+        if constexpr (FORM == kTree) {
+            mask = line_bits(a.line(b, t), a.words, k0 - first);
+        } else {
+            const int n = (FORM == kBlocks ? end : first + t + 1) - k0;   // keys up to the token
+            mask = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+        }
+        return mask;
+    };
+    const auto mine = [&](uint32_t mask) { return (mask >> (4 * g4) & 15u) | (mask >> (16 + 4 * g4) & 15u) << 4; };
+
+    f32x4 acc[R][ND];
+    float m[R], l[R];
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+        m[g] = -INFINITY;
+        l[g] = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    operands_here();
+    int ahead = c0;   // next chunk to request
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s) {
+        if (ahead < c1) request(ahead, s);
+        bads[s] = bad;
+        ahead += W;
+    }
+    bads[NST - 1] = 0;
+    for (int c = c0; c < c1; c += NST * W) {
+#pragma unroll
+        for (int s = 0; s < NST; ++s) {
+            const int ch = c + s * W;
+            if (ch >= c1) break;
+            // the stage of the step before is free: its reads have been waited for
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (ahead < c1) {
+                request(ahead, (s + NST - 1) % NST);
+                bads[(s + NST - 1) % NST] = bad;
+                wait_vmcnt<2 * PER * (NST - 1)>();
+            } else {
+                wait_vmcnt<0>();
+            }
+            asm volatile("" ::: "memory");
+            ahead += W;
+            const int k0 = ch * kKeys;
+            const char* kt = ring + s * S::STAGE;
+            const char* vt = kt + S::STAGE / 2;
+            float z[R][8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f32x4 sv[R];
+#pragma unroll
+                for (int g = 0; g < R; ++g) sv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < NS; ++x) {
+                    const Frag<E> kf = T::along(kt, 16 * u + n16, 4 * x + g4);
+#pragma unroll
+                    for (int g = 0; g < R; ++g) mma16x16(sv[g], kf, q[g][x]);
+                }
+#pragma unroll
+                for (int g = 0; g < R; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[g][4 * u + i] = sv[g][i];
+            }
+            // keys that some of the rows do not see
+            const bool edge = FORM == kTree ? k0 + kKeys > first : FORM == kWeigh ? k0 + kKeys > first + tok0 + 1 : k0 + kKeys > end;
+            int block[4];   // kBlocks: the chunk's pages, whose places the bias goes by
+            if (FORM == kBlocks && a.slopes) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) block[x] = blocks[min((k0 + 8 * x) >> a.shift, listed - 1)] << a.shift;
+            }
+            Frag<E> p[R];
+#pragma unroll
+            for (int g = 0; g < R; ++g) {
+                scores<E, MODE, 8>(a.sc, z[g], z[g], nullptr);
+                if (a.slopes) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int o = 16 * (i >> 2) + 4 * g4 + (i & 3);
+                        int pos = k0 + o;
+                        if constexpr (FORM == kBlocks) {
+                            const int x = o >> 3;
+                            pos = (x == 0 ? block[0] : x == 1 ? block[1] : x == 2 ? block[2] : block[3]) + (pos & (a.page - 1));
+                        } else if (FORM == kTree && pos >= first) {
+                            const int node = pos - first;
+                            pos = node < a.fresh ? first + a.depths[(int64_t)b * a.fresh + node] : pos;
+                        }
+                        z[g][i] = fmaf(-slope[g], fabsf((float)(pos - at[g])), z[g][i]);
+                    }
+                }
+                if (edge || bads[s]) {
+                    const uint32_t mask = mine(sees(tok[g], k0) & ~bads[s]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[g][i] = mask >> i & 1u ? z[g][i] : -INFINITY;
+                }
+                if constexpr (FORM == kWeigh) {
+                    if (live[g]) {
+                        const int r = row0 + g * kGroup + n16;
+                        const float unit = MODE & kCap ? 1.f : a.sc.unit;
+                        float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + r) * a.z_row + k0 + 4 * g4;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            *reinterpret_cast<f32x4*>(zp + 16 * u) = f32x4{z[g][4 * u] * unit, z[g][4 * u + 1] * unit,
+                                                                           z[g][4 * u + 2] * unit, z[g][4 * u + 3] * unit};
+                    }
+                }
+                float top = z[g][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, z[g][i]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32)) * (MODE & kCap ? 1.f : a.sc.unit);
+                if (__any(top > m[g] + 8.f)) {   // see attn_fwd_kernel
+                    const float to = fmaxf(m[g], top);
+                    const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[g] - to);
+                    m[g] = to;
+                    l[g] *= f;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) acc[g][d] *= f;
+                }
+                const float base = m[g] == -INFINITY ? 0.f : m[g];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    z[g][i] = exp_score<MODE>(a.sc, z[g][i], base);
+                    l[g] += z[g][i];
+                }
+                p[g] = to_frag<E>(z[g]);
+            }
+            // a value that a row does not see meets a probability of zero, which an infinite or NaN one would outlive: then
+            // each token's rows are multiplied by the values that this token sees, with zeros for the others
+            bool odd = false;
+            if (FORM != kBlocks && edge && a.fresh > 1) {
+#pragma unroll
+                for (int d = 0; d < ND; ++d) odd |= not_finite(T::across16(vt, d, lane));
+            }
+            if (FORM != kBlocks && __any(odd)) {
+                for (int t = tok0; t <= tok1; ++t) {
+                    const uint32_t mask = mine(sees(t, k0));
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const Frag<E> vf = only(T::across16(vt, d, lane), mask);
+#pragma unroll
+                        for (int g = 0; g < R; ++g) {
+                            f32x4 sum = acc[g][d];
+                            mma16x16(sum, vf, p[g]);
+                            acc[g][d] = tok[g] == t ? sum : acc[g][d];
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const Frag<E> vf = T::across16(vt, d, lane);
+#pragma unroll
+                    for (int g = 0; g < R; ++g) mma16x16(acc[g][d], vf, p[g]);
+                }
+            }
+        }
+    }
+
+    // the waves' results meet, a group at a time: [wave][16 rows][DP + 4] float32
+    constexpr int LD = DP + 4;
+    static_assert(W * kGroup * LD * 4 <= W * NST * S::STAGE, "fits the ring");
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+        l[g] += __shfl_xor(l[g], 16);
+        l[g] += __shfl_xor(l[g], 32);
+        __syncthreads();
+        float* dst = reinterpret_cast<float*>(lds) + (wave * kGroup + n16) * LD;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(dst + 16 * d + 4 * g4) = acc[g][d];
+        if (g4 == 0) {
+            dst[DP] = m[g];
+            dst[DP + 1] = l[g];
+        }
+        __syncthreads();
+        const int take = min(rows - row0 - g * kGroup, kGroup);
+        for (int e = threadIdx.x; e < take * (DP / 4); e += 64 * W) {
+            const int row = e / (DP / 4), d = e % (DP / 4) * 4;
+            const float* src = reinterpret_cast<const float*>(lds) + row * LD;
+            float top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < W; ++x) top = fmaxf(top, src[x * kGroup * LD + DP]);
+            const float base = top == -INFINITY ? 0.f : top;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            float total = 0.f;
+#pragma unroll
+            for (int x = 0; x < W; ++x) {
+                const float* p = src + x * kGroup * LD;
+                const float f = __builtin_amdgcn_exp2f(p[DP] - base);
+                sum += *reinterpret_cast<const f32x4*>(p + d) * f;
+                total += p[DP + 1] * f;
+            }
+            if (a.pieces > 1 || FORM == kWeigh) {
+                float* out = a.part + (((int64_t)blockIdx.x * R + g) * kGroup + row) * LD;
+                *reinterpret_cast<f32x4*>(out + d) = sum;
+                if (d == 0) {
+                    out[DP] = top;
+                    out[DP + 1] = total;
+                    out[DP + 2] = (float)pieces;
+                }
+            } else {
+                const int rr = row0 + g * kGroup + row, t = FORM == kBlocks ? tok0 : rr / a.share;
+                decode_store<E, FORM>(a, b, kv, t, rr - (FORM == kBlocks ? 0 : t * a.share), d, sum, total);
+            }
+        }
+    }
+}
+
+// Joins the pieces of every row, in their order.  A row's DP / 4 lanes each take four elements.  kWeigh: and keeps the rows'
+// maxima and sums for weigh_kernel.
+struct DecodeJoinArgs {
+    DecodeArgs a;
+    int64_t items;   // rows of all heads
+    int groups;      // R
+};
+template <typename E, int DP, int FORM>
+__global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
+    const DecodeArgs& a = j.a;
+    constexpr int LANES = DP / 4, LD = DP + 4;
+    const int64_t item = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (item >= j.items) return;
+    const int d = threadIdx.x % LANES * 4, rows = a.fresh * a.share;
+    const int row = (int)(item % rows), kv = (int)(item / rows % a.kv_heads), b = (int)(item / rows / a.kv_heads);
+    const int tok = row / a.share, in_tok = row - tok * a.share;
+    int rt, slot;   // the row's tile and place in it
+    if constexpr (FORM == kBlocks) {
+        rt = tok * ((a.share + kGroup - 1) / kGroup) + in_tok / kGroup;
+        slot = in_tok % kGroup;
+    } else {
+        rt = row / (kGroup * j.groups);
+        slot = row % (kGroup * j.groups);
+    }
+    const int64_t tile = (int64_t)j.groups * kGroup * LD, step = (int64_t)a.row_tiles * a.kv_heads * tile;   // from piece to piece
+    const float* p = a.part + (((int64_t)b * a.pieces * a.row_tiles + rt) * a.kv_heads + kv) * tile + (int64_t)slot * LD;
+    const int pieces = (int)p[DP + 2];
+    if (FORM != kWeigh && a.pieces == 1) return;
+    // eight pieces at a time, their loads all in flight
+    constexpr int N = 8;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f, top = -INFINITY;
+    for (int x0 = 0; x0 < pieces; x0 += N) {
+        f32x4 v[N];
+        float m[N], l[N], next = top;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float* q = p + min(x0 + n, pieces - 1) * step;
+            v[n] = *reinterpret_cast<const f32x4*>(q + d);
+            m[n] = x0 + n < pieces ? q[DP] : -INFINITY;
+            l[n] = q[DP + 1];
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) next = fmaxf(next, m[n]);
+        const float base = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - base);
+        sum *= keep;
+        total *= keep;
+        top = next;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (x0 + n >= pieces) break;
+            const float f = __builtin_amdgcn_exp2f(m[n] - base);
+            sum += v[n] * f;
+            total += l[n] * f;
+        }
+    }
+    if (FORM == kWeigh && d == 0) a.stats[item] = make_float2(top, 1.f / total);
+    decode_store<E, FORM>(a, b, kv, tok, in_tok, d, sum, total);
+}
+
+// The weight that every token received: of the rows that see it, exp2(score - maximum) / sum, added in the rows' order.  A
+// workgroup takes 1024 tokens of one sequence and key head, a thread four of them.
+struct WeighArgs {
+    DecodeArgs a;
+    const float* in;   // [B, kv_heads, table_row page], nullptr: nothing
+    float* out;
+    int parts;         // workgroups of one (sequence, key head)
+};
+__global__ __launch_bounds__(256) void weigh_kernel(WeighArgs w) {
+    const DecodeArgs& a = w.a;
+    const int head = blockIdx.x / w.parts, b = head / a.kv_heads;   // (sequence, key head)
+    const int len = a.held(b), first = len - a.fresh, rows = a.fresh * a.share;
+    const int j0 = (int)(blockIdx.x % w.parts) * 1024 + threadIdx.x;
+    if (j0 - (int)threadIdx.x >= len) return;
+    const float2* stats = a.stats + (int64_t)head * rows;
+    const float* z = a.z + (int64_t)head * rows * a.z_row;
+    bool ok[4];
+    float sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = j0 + 256 * i;
+        ok[i] = j < len && a.there(b, j >> a.shift);
+        sum[i] = 0.f;
+    }
+    for (int r = 0; r < rows; ++r) {
+        const float2 st = stats[r];
+        const int at = first + r / a.share;
+        const float* zr = z + (int64_t)r * a.z_row;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + 256 * i;
+            if (ok[i] && j <= at) sum[i] += __builtin_amdgcn_exp2f(zr[j] - st.x) * st.y;
+        }
+    }
+    const int64_t base = (int64_t)head * a.table_row * a.page;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = j0 + 256 * i;
+        if (j < len) w.out[base + j] = (w.in && j < first ? w.in[base + j] : 0.f) + sum[i];
+    }
+}
+
+}  // namespace noble

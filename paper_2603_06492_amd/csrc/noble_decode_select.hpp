@@ -1,0 +1,425 @@
+// The operators around attention over a cache that is not read, or not kept, as a whole: rows of a tree, means of pages,
+// selection of pages and of tokens, and the move of the tokens that stay.
+#pragma once
+
+#include <type_traits>
+
+#include "noble_attn_common.hpp"
+
+namespace noble {
+
+// ------------------------------------------------------------------- tree --
+
+struct TreeArgs {
+    const int* parents;
+    const int* lengths;
+    uint32_t* seen;
+    int* depths;
+    int* positions;
+    int n, words;
+};
+
+// One workgroup a tree, one thread a node.  A node's line is its own bit and its parent's line: after round k a node has the
+// bits of the nodes up to 2^k steps above it and the place 2^k steps above it (-1: the root, -2: no node), so a tree of n
+// nodes takes log2 n rounds, however deep it is.
+constexpr int kTreeMost = 256, kTreeWords = kTreeMost / 32;
+__global__ __launch_bounds__(kTreeMost) void tree_rows_kernel(TreeArgs a) {
+    __shared__ uint32_t bits[2][kTreeMost][kTreeWords + 1];
+    __shared__ int up[2][kTreeMost];
+    const int i = threadIdx.x;
+    const int64_t b = blockIdx.x;
+    if (i < a.n) {
+        const int p = a.parents[b * a.n + i];
+        up[0][i] = p >= -1 && p < i ? p : -2;
+        for (int w = 0; w < a.words; ++w) bits[0][i][w] = w == i >> 5 ? 1u << (i & 31) : 0u;
+    }
+    int cur = 0;
+    for (int step = 1; step < a.n; step *= 2) {
+        __syncthreads();
+        if (i < a.n) {
+            const int u = up[cur][i];
+            up[cur ^ 1][i] = u < 0 ? u : up[cur][u];
+            for (int w = 0; w < a.words; ++w) bits[cur ^ 1][i][w] = bits[cur][i][w] | (u < 0 ? 0u : bits[cur][u][w]);
+        }
+        cur ^= 1;
+    }
+    if (i >= a.n) return;
+    // n rounds' steps of at least n - 1 reach the root or none
+    const bool node = up[cur][i] == -1;
+    int depth = -1;
+    for (int w = 0; w < a.words; ++w) {
+        const uint32_t v = node ? bits[cur][i][w] : 0u;
+        depth += __popc(v);
+        a.seen[(b * a.n + i) * a.words + w] = v;
+    }
+    a.depths[b * a.n + i] = depth;
+    if (a.positions) a.positions[b * a.n + i] = node ? max(max(a.lengths[b], 0) - a.n + depth, 0) : 0;
+}
+
+// ------------------------------------------------------------------ pages --
+
+struct PageArgs {
+    const char* cache;
+    const int* table;
+    const int* lengths;
+    char* means;
+    int64_t table_row, pages, fresh;
+    int page, shift, kv_heads, D, touched;   // touched: workgroups of one (sequence, key head)
+    __device__ __forceinline__ int64_t held(int b) const { return min((int64_t)max(lengths[b], 0), table_row * page); }
+};
+
+template <typename E>
+__device__ __forceinline__ float element(const char* p) {
+    if constexpr (sizeof(E) == 2) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+    else return *reinterpret_cast<const float*>(p);
+}
+// Eight consecutive elements.
+template <typename E>
+__device__ __forceinline__ void elements8(const char* p, float* x) {
+    const Frag<E> f = global_frag<E>(p, true);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(E) == 2) x[i] = __uint_as_float(i & 1 ? f.v[i >> 1] & 0xffff0000u : f.v[i >> 1] << 16);
+        else x[i] = __uint_as_float(f.v[i >> 2][i & 3]);
+    }
+}
+
+// A float64 value rounded once to bf16, to nearest even: the float32 in between takes the side of the value where it
+// would be a tie.
+__device__ __forceinline__ uint16_t double_to_bf16(double x) {
+    const float f = (float)x;
+    uint32_t u = __float_as_uint(f);
+    if ((u & 0xffffu) == 0x8000u && x == x) u += fabs(x) > fabs((double)f) ? 1 : fabs(x) < fabs((double)f) ? -1 : 0;
+    return (uint16_t)(pack_bf16(__uint_as_float(u), 0.f) & 0xffffu);
+}
+
+// The mean of one page's keys of one head.  Eight elements a lane, D / 8 lanes a token, the workgroup's other lanes on other
+// tokens; float64 sums, so that the mean, rounded once, is the same in whatever order it is formed.
+template <typename E>
+__global__ __launch_bounds__(256) void page_means_kernel(PageArgs a) {
+    __shared__ double sums[256][9];
+    const int per = a.D / 8, groups = 256 / per;
+    int w = blockIdx.x;
+    const int kv = w % a.kv_heads;
+    w /= a.kv_heads;
+    const int t = w % a.touched, b = w / a.touched;
+    const int64_t len = a.held(b), from = max(len - a.fresh, (int64_t)0);
+    const int64_t block = from / a.page + t;
+    if (block * a.page >= len) return;
+    const int page = a.table[b * a.table_row + block];
+    if (page < 0 || page >= a.pages) return;
+    const int n = (int)min(len - block * a.page, (int64_t)a.page), ES = (int)sizeof(E);
+    const char* k = a.cache + ((int64_t)page * 2 * a.kv_heads + kv) * a.page * a.D * ES;
+    const int g = threadIdx.x / per, x = threadIdx.x % per;
+    double s[8] = {};
+    if (g < groups)
+        for (int r = g; r < n; r += groups) {
+            float v[8];
+            elements8<E>(k + ((int64_t)r * a.D + 8 * x) * ES, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] += (double)v[i];
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = s[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.D; e += 256) {
+        double total = 0.0;
+        for (int r = 0; r < min(groups, n); ++r) total += sums[r * per + e / 8][e % 8];
+        total /= n;
+        char* out = a.means + (((int64_t)page * a.kv_heads + kv) * a.D + e) * ES;
+        if constexpr (sizeof(E) == 2) *reinterpret_cast<uint16_t*>(out) = double_to_bf16(total);
+        else *reinterpret_cast<float*>(out) = (float)total;
+    }
+}
+
+// -------------------------------------------------------------- selection --
+
+// Whole numbers in the order of the values, NaN above all, -0 with 0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    if (x != x) return ~0u;
+    const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t ordered(double x) {
+    if (x != x) return ~0ull;
+    const uint64_t u = (uint64_t)__double_as_longlong(x == 0.0 ? 0.0 : x);
+    return u >> 63 ? ~u : u | 1ull << 63;
+}
+
+// The `need` largest of the keys key(lo) .. key(hi - 1), of equal ones the first, between places that are taken in any case:
+// out(i, j) for the i-th of all taken places j of [0, n), in their order.  The least key taken is found from its highest byte
+// down, by counting the keys that agree with it so far; places are then counted off by waves that each own a range.
+template <typename K, int THREADS>
+struct Pick {
+    static constexpr int WAVES = THREADS / 64;
+    uint32_t hist[WAVES][257];
+    uint32_t above[WAVES], equal[WAVES];
+    K prefix, mask;
+    uint32_t left, done;
+
+    template <typename Key, typename Out>
+    __device__ int run(int n, int lo, int hi, int need, Key key, Out out) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        K pre = 0, msk = 0;
+        uint32_t want = (uint32_t)need;
+        for (int shift = 8 * (int)sizeof(K) - 8; shift >= 0 && want > 0; shift -= 8) {
+            for (int i = lane; i < 256; i += 64) hist[wave][i] = 0;
+            __syncthreads();
+            for (int j = lo + tid; j < hi; j += THREADS) {
+                const K k = key(j);
+                if ((k & msk) == pre) atomicAdd(&hist[wave][(uint32_t)(k >> shift) & 255u], 1u);
+            }
+            __syncthreads();
+            if (wave == 0) {
+                // lane l has the bins 255 - 4 l down to 252 - 4 l
+                uint32_t c[4], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    c[i] = 0;
+                    for (int x = 0; x < WAVES; ++x) c[i] += hist[x][255 - 4 * lane - i];
+                    sum += c[i];
+                }
+                uint32_t upto = sum;   // of this lane's bins and the larger ones
+#pragma unroll
+                for (int o = 1; o < 64; o *= 2) {
+                    const uint32_t v = __shfl_up(upto, o);
+                    if (lane >= o) upto += v;
+                }
+                uint32_t before = upto - sum;
+                if (before < want && upto >= want) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (before < want && before + c[i] >= want) {
+                            prefix = pre | (K)(255 - 4 * lane - i) << shift;
+                            mask = msk | (K)255 << shift;
+                            left = want - before;
+                            done = c[i] == want - before;   // the whole bin is taken
+                            break;
+                        }
+                        before += c[i];
+                    }
+                }
+            }
+            __syncthreads();
+            pre = prefix;
+            msk = mask;
+            want = left;
+            if (done) break;
+            __syncthreads();
+        }
+        // places in order: those above the least key or taken in any case, and the first `want` of the least
+        const int span = ((n + THREADS - 1) / THREADS) * 64, j0 = min(wave * span, n), j1 = min(j0 + span, n);
+        const auto state = [&](int j, bool& is_above, bool& is_equal) {
+            is_above = j < j1 && (j < lo || j >= hi);
+            is_equal = false;
+            if (j < j1 && !is_above && need > 0) {
+                const K k = key(j) & msk;
+                is_above = k > pre;
+                is_equal = k == pre;
+            }
+        };
+        uint32_t na = 0, ne = 0;
+        for (int j = j0; j < j1; j += 64) {
+            bool u, e;
+            state(j + lane, u, e);
+            na += __popcll(__ballot(u));
+            ne += __popcll(__ballot(e));
+        }
+        if (lane == 0) {
+            above[wave] = na;
+            equal[wave] = ne;
+        }
+        __syncthreads();
+        uint32_t at = 0, same = 0, all = 0, every = 0;
+        for (int x = 0; x < WAVES; ++x) {
+            if (x < wave) {
+                at += above[x];
+                same += equal[x];
+            }
+            all += above[x];
+            every += equal[x];
+        }
+        const uint64_t below = (1ull << lane) - 1;
+        for (int j = j0; j < j1; j += 64) {
+            bool u, e;
+            state(j + lane, u, e);
+            const uint64_t bu = __ballot(u), be = __ballot(e);
+            const uint32_t ae = same + __popcll(be & below);   // equal ones before this place
+            if (u || (e && ae < want)) out((int)(at + __popcll(bu & below) + min(ae, want)), j + lane);
+            at += __popcll(bu);
+            same += __popcll(be);
+        }
+        return (int)(all + min(every, want));
+    }
+};
+
+struct EvictArgs {
+    const float* weights;
+    const int* lengths;
+    int* kept;
+    float* kept_weights;
+    int64_t row;
+    int heads, keep, sink, recent;
+};
+
+// One workgroup a sequence and key head.  LDS holds the weights of up to N tokens; longer rows are read again each time.
+template <int N>
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
+    __shared__ uint32_t keys[N];
+    __shared__ Pick<uint32_t, 1024> pick;
+    const int b = blockIdx.x / a.heads;
+    const int n = (int)min((int64_t)max(a.lengths[b], 0), a.row);
+    const float* w = a.weights + (int64_t)blockIdx.x * a.row;
+    int* kept = a.kept + (int64_t)blockIdx.x * a.keep;
+    float* kw = a.kept_weights ? a.kept_weights + (int64_t)blockIdx.x * a.keep : nullptr;
+    const auto out = [&](int i, int j) {
+        kept[i] = j;
+        if (kw) kw[i] = w[j];
+    };
+    int total = n;
+    if (n <= a.keep) {
+        for (int j = threadIdx.x; j < n; j += 1024) out(j, j);
+    } else {
+        const int lo = a.sink, hi = n - a.recent, need = a.keep - a.sink - a.recent;
+        if (n <= N) {
+            for (int j = threadIdx.x; j < n; j += 1024) keys[j] = ordered(w[j]);
+            __syncthreads();
+            total = pick.run(n, lo, hi, need, [&](int j) { return keys[j]; }, out);
+        } else {
+            total = pick.run(n, lo, hi, need, [&](int j) { return ordered(w[j]); }, out);
+        }
+    }
+    for (int i = total + threadIdx.x; i < a.keep; i += 1024) {
+        kept[i] = -1;
+        if (kw) kw[i] = 0.f;
+    }
+}
+
+struct SelectArgs {
+    HeadRows q;
+    const char* means;
+    const int* table;
+    const int* lengths;
+    int* chosen;
+    uint64_t* keys;     // [B fresh, kv_heads, table_row] where LDS does not hold them
+    int64_t table_row, pages;
+    int page, shift, fresh, kv_heads, share, D, count, sink, local;
+};
+
+// One workgroup a row and key head: the scores of the row's blocks, eight elements a lane, then the selection.  LDS holds the
+// scores of up to N blocks; those of longer sequences lie in global memory.
+template <typename E, int N, int THREADS>
+__global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
+    __shared__ uint64_t local_keys[N];
+    __shared__ Pick<uint64_t, THREADS> pick;
+    const int ES = (int)sizeof(E), lanes = a.D <= 64 ? 8 : 16;
+    const int kv = blockIdx.x % a.kv_heads, row = blockIdx.x / a.kv_heads, b = row / a.fresh;
+    const int64_t held = min((int64_t)max(a.lengths[b], 0), a.table_row * a.page);
+    const int64_t at = held - a.fresh + row % a.fresh;
+    const int n = at >= 0 ? (int)(at >> a.shift) + 1 : 0;   // blocks up to the row's own
+    int* chosen = a.chosen + (int64_t)blockIdx.x * a.count;
+    const auto out = [&](int i, int j) { chosen[i] = j; };
+    int total = n;
+    if (n <= a.count) {
+        for (int j = threadIdx.x; j < n; j += THREADS) out(j, j);
+    } else {
+        const int lo = a.sink, hi = n - a.local, need = a.count - a.sink - a.local;
+        uint64_t* keys = n <= N ? local_keys : a.keys + (int64_t)blockIdx.x * a.table_row;
+        if (need > 0) {
+            const int x = threadIdx.x % lanes, g = threadIdx.x / lanes;
+            const bool in = 8 * x < a.D;
+            double q[8] = {};
+            const char* qp = a.q.ptr + (int64_t)row * a.q.row + (int64_t)kv * a.share * a.q.head + 8 * x * ES;
+            if (in)
+                for (int h = 0; h < a.share; ++h) {
+                    float v[8];
+                    elements8<E>(qp + h * a.q.head, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[i] += (double)v[i];
+                }
+            for (int j = lo + g; j < hi; j += THREADS / lanes) {
+                const int page = a.table[b * a.table_row + j];
+                const bool ok = page >= 0 && page < a.pages;
+                double s = 0.0;
+                if (ok && in) {
+                    float v[8];
+                    elements8<E>(a.means + (((int64_t)page * a.kv_heads + kv) * a.D + 8 * x) * ES, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s = fma(q[i], (double)v[i], s);
+                }
+                for (int o = 1; o < lanes; o *= 2) s += __shfl_xor(s, o);
+                if (x == 0) keys[j] = ordered(ok ? s : -(double)INFINITY);
+            }
+            __syncthreads();
+        }
+        // two copies, so that the one over LDS is compiled for it
+        if (n <= N) total = pick.run(n, lo, hi, need, [&](int j) { return local_keys[j]; }, out);
+        else total = pick.run(n, lo, hi, need, [&](int j) { return keys[j]; }, out);
+    }
+    for (int i = total + threadIdx.x; i < a.count; i += THREADS) chosen[i] = -1;
+}
+
+// ------------------------------------------------------------------- move --
+
+struct KeepArgs {
+    char* cache;
+    const int* table;
+    const int* kept;
+    const int* start;
+    int64_t table_row, pages, most;
+    int page, shift, kv_heads, kept_heads;
+    int bytes, slices, lanes;   // of a token's head; shares of it that workgroups take; lanes of a share
+};
+
+// One workgroup moves a share of one sequence's and key head's keys (or values), tokens in ascending order, a tile of them
+// through registers at a time.  A token never moves up, so what a tile writes no later tile reads; what it writes and an
+// earlier lane of the same tile reads, the barrier keeps.
+__global__ __launch_bounds__(256) void cache_keep_kernel(KeepArgs a) {
+    constexpr int U = 8;
+    int w = blockIdx.x;
+    const int slice = w % a.slices;
+    w /= a.slices;
+    const int half = w & 1;   // keys or values
+    w >>= 1;
+    const int kv = w % a.kv_heads, b = w / a.kv_heads;
+    const int per = 256 / a.lanes, r = threadIdx.x / a.lanes;
+    const int byte = 16 * (slice * a.lanes + threadIdx.x % a.lanes);
+    const bool in = r < per && byte < a.bytes;
+    const int* kept = a.kept + ((int64_t)b * a.kept_heads + (a.kept_heads > 1 ? kv : 0)) * a.most;
+    const int* table = a.table + b * a.table_row;
+    const int64_t start = a.start ? a.start[b] : 0, held = a.table_row * a.page, head = (int64_t)a.page * a.bytes;
+    char* base = a.cache + ((int64_t)half * a.kv_heads + kv) * head + byte;
+    // the token's place in memory, nullptr: none
+    const auto place = [&](int64_t t) -> char* {
+        if (t < 0 || t >= held) return nullptr;
+        const int page = table[t >> a.shift];
+        if (page < 0 || page >= a.pages) return nullptr;
+        return base + (int64_t)page * 2 * a.kv_heads * head + (t & (a.page - 1)) * a.bytes;
+    };
+    for (int64_t i0 = 0; i0 < a.most; i0 += per * U) {
+        u32x4 v[U];
+        char* to[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * per + r;
+            to[u] = nullptr;
+            if (in && i < a.most) {
+                const int k = kept[i];
+                if (k > i) {
+                    const char* from = place(start + k);
+                    to[u] = place(start + i);
+                    if (!from) to[u] = nullptr;
+                    if (to[u]) v[u] = *reinterpret_cast<const u32x4*>(from);
+                }
+            }
+        }
+        // every lane's loads have arrived before any lane stores
+        wait_vmcnt<0>();
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (to[u]) *reinterpret_cast<u32x4*>(to[u]) = v[u];
+    }
+}
+
+}  // namespace noble
