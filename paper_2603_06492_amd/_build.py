@@ -1,5 +1,5 @@
 """Builds libnoble.so (the HIP kernels and the C ABI) in-tree for gfx950, and
-_noble_torch.so and _noble_attn_torch.so, the binding's calls on torch tensors
+_noble_torch.so, _noble_attn_torch.so and _noble_decode_torch.so, the binding's calls on torch tensors
 (host code)."""
 
 from __future__ import annotations
@@ -17,9 +17,10 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libnoble.so")
 BINDING = os.path.join(PKG, "_noble_torch.so")
-BINDINGS = [("noble_torch.cpp", BINDING), ("noble_attn_torch.cpp", os.path.join(PKG, "_noble_attn_torch.so"))]
+BINDINGS = [("noble_torch.cpp", BINDING), ("noble_attn_torch.cpp", os.path.join(PKG, "_noble_attn_torch.so")),
+            ("noble_decode_torch.cpp", os.path.join(PKG, "_noble_decode_torch.so"))]
 SOURCES = ["noble_api.hip", "noble_attn.hip", "noble_decode.hip"]
-HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_host.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_decode_attn.hpp", "noble_decode_select.hpp", "noble_binding.h", "noble_torch.cpp", "noble_attn_torch.cpp"]
+HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_host.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_decode_attn.hpp", "noble_decode_select.hpp", "noble_binding.h", "noble_torch.cpp", "noble_attn_torch.cpp", "noble_decode_torch.cpp", "noble_torch_call.hpp"]
 
 # of the library; its objects are compiled with all but -shared
 HIP_FLAGS = [
@@ -70,7 +71,9 @@ def build_binding(verbose: bool = False) -> str:
     import torch
     root = os.path.dirname(torch.__file__)
     inc = os.path.join(root, "include")
-    for source, target in BINDINGS:
+
+    def one(binding):
+        source, target = binding
         tmp = target + ".tmp"
         cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, "-isystem", inc,
@@ -84,6 +87,9 @@ def build_binding(verbose: bool = False) -> str:
         if res.returncode != 0:
             raise RuntimeError(f"g++ failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
         os.replace(tmp, target)
+
+    with ThreadPoolExecutor() as pool:
+        list(pool.map(one, BINDINGS))
     return BINDING
 
 

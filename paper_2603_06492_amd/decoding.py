@@ -15,12 +15,14 @@ There is no fallback: without the built library or a gfx950 device, calls raise.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import os
 from typing import Optional, Tuple
 
 import torch
 
 from . import noble
-from .attention import (_cache_shape, _gpu, _heads, _P, _scratch, _tensor, _work, noble_heads, noble_paged_desc)
+from .attention import (_cache_shape, _gpu, _heads, _P, _scratch, _served, _tensor, _work, noble_heads, noble_paged_desc)
 from .noble import NobleError, _dtype_code
 
 _vp = ctypes.c_void_p
@@ -73,6 +75,30 @@ def lib() -> ctypes.CDLL:
     return L
 
 
+BINDING_PATH = os.path.join(noble.PKG_DIR, "_noble_decode_torch.so")
+_native_module = None
+
+
+def _native():
+    """The native calls (_noble_decode_torch.so), given the library's entry points.  They serve well-formed calls on ordinary
+    tensors and the current stream and return None for any other, which the Python code then checks and runs."""
+    global _native_module
+    if _native_module is None:
+        L = lib()
+        if not os.path.exists(BINDING_PATH):
+            raise RuntimeError(f"{BINDING_PATH} is missing: build it with __graft_entry__.build() "
+                               "(or python -m paper_2603_06492_amd._build)")
+        spec = importlib.util.spec_from_file_location("_noble_decode_torch", BINDING_PATH)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        m.init(*(ctypes.cast(getattr(L, n), _vp).value for n in (
+            "noble_tree_rows", "noble_attn_tree", "noble_attn_tree_scratch_size", "noble_cache_keep", "noble_page_means",
+            "noble_block_select", "noble_block_select_scratch_size", "noble_attn_blocks", "noble_attn_blocks_scratch_size",
+            "noble_attn_weigh", "noble_attn_weigh_scratch_size", "noble_evict_select")))
+        _native_module = m
+    return _native_module
+
+
 def _call(name, *args) -> None:
     st = getattr(lib(), name)(*args)
     if st != 0:
@@ -89,6 +115,13 @@ def _need(t, name):
     if t is None:
         raise TypeError(f"{name} must be a torch.Tensor")
     return t
+
+
+def _whole(**numbers) -> None:
+    """Whole numbers as the descriptors' 32 bits hold them."""
+    for name, n in numbers.items():
+        if not 0 <= n < 2 ** 31:
+            raise ValueError(f"{name}={n}")
 
 
 def _int32(t, name, shape, device):
@@ -134,6 +167,10 @@ def noble_tree_rows(parents, lengths, *, stream=None) -> Tuple[torch.Tensor, tor
     an earlier node, or -1 (the last token before the tree); any other number: no node, nor what hangs from it.  seen int32
     [B, n, (n + 31) // 32], a bit for each node of the line from the root to the node; depths int32 [B, n] (no node: -1);
     positions int32 [B, n], lengths - n + depth (no node: 0), lengths int32 [B] with the tree's tokens."""
+    if stream is None:
+        out = _native().tree_rows(parents, lengths)
+        if _served(out, "noble_tree_rows"):
+            return out
     dev = _gpu(parents, "parents")
     if parents.dim() != 2:
         raise ValueError(f"parents must be [sequences, nodes], got {tuple(parents.shape)}")
@@ -152,6 +189,10 @@ def noble_attn_tree(q, cache, page_table, lengths, seen, depths, slopes=None, *,
     """Attention of the nodes of each sequence's tree, its last n tokens, over the paged cache, which holds them already: q
     [B n, heads, D]; seen and depths from noble_tree_rows.  A node sees the tokens before the tree, the nodes above it and
     itself; the bias goes by the difference of positions."""
+    if stream is None:
+        out = _native().attn_tree(q, cache, page_table, lengths, seen, depths, slopes, scale, softcap, o)
+        if _served(out, "noble_attn_tree"):
+            return out[0]
     s = _Sequences(q, cache, page_table, lengths, slopes, scale, softcap)
     tree = [_int32(seen, "seen", (s.B, s.n, (s.n + 31) // 32), s.dev), _int32(depths, "depths", (s.B, s.n), s.dev)]
     n = _size("noble_attn_tree_scratch_size", ctypes.byref(s.desc))
@@ -170,6 +211,8 @@ def noble_cache_keep(cache, page_table, kept, start=None, *, stream=None) -> tor
     """Moves keys and values of token start[b] + kept[b, h, i] of key head h to the place of token start[b] + i, and returns
     the cache: kept int32 [B, kv_heads or 1, most], ascending; entries below their own i (-1 at the end) are skipped; start
     int32 [B] (None: 0).  Different sequences' pages are distinct."""
+    if stream is None and _served(_native().keep(cache, page_table, kept, start), "noble_cache_keep"):
+        return cache
     dev = _gpu(cache, "cache")
     if cache.dim() != 5 or cache.shape[1] != 2:
         raise ValueError("cache must be [pages, 2, kv_heads, page, head_dim]")
@@ -195,6 +238,8 @@ def noble_page_means(cache, page_table, lengths, new: int, means=None, *, stream
     """The means of the keys of the pages that hold each sequence's last ``new`` tokens, over the tokens that it holds in
     them, into means [pages, kv_heads, D] (the cache's dtype; None: a new tensor, zeros elsewhere).  ``new`` of the longest
     sequence or more: of all its pages."""
+    if stream is None and _served(_native().page_means(cache, page_table, lengths, new, means), "noble_page_means"):
+        return means
     dev = _gpu(cache, "cache")
     if cache.dim() != 5 or cache.shape[1] != 2:
         raise ValueError("cache must be [pages, 2, kv_heads, page, head_dim]")
@@ -203,6 +248,7 @@ def noble_page_means(cache, page_table, lengths, new: int, means=None, *, stream
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be [sequences, pages]")
     B, per = page_table.shape
+    _whole(new=new)
     d = noble_paged_desc(B, per, pages, page, new, 0, K, K, D, _dtype_code(cache), 1.0, 0.0, 0)
     args = [_int32(page_table, "page_table", (B, per), dev), _int32(lengths, "lengths", (B,), dev)]
     with _work(dev, stream) as (st, shared):
@@ -218,6 +264,10 @@ def noble_block_select(q, means, page_table, lengths, count: int, *, page: int, 
     of those up to the row's own the first ``sink``, the last ``local`` and, of the others, those whose means [pages,
     kv_heads, D] have the largest product with the sum of the queries that share the head.  int32 [B n, kv_heads, count],
     ascending, -1 behind the last."""
+    if stream is None:
+        out = _native().block_select(q, means, page_table, lengths, count, page, sink, local, chosen)
+        if _served(out, "noble_block_select"):
+            return out[0]
     dev = _gpu(q, "q")
     if q.dim() != 3 or not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] < 1:
         raise ValueError("q must be [rows, heads, head_dim] and page_table [sequences, pages]")
@@ -228,6 +278,7 @@ def noble_block_select(q, means, page_table, lengths, count: int, *, page: int, 
     if not isinstance(means, torch.Tensor) or means.dim() != 3:
         raise ValueError("means must be [pages, kv_heads, head_dim]")
     pages, K = means.shape[0], means.shape[1]
+    _whole(count=count, page=page, sink=sink, local=local)
     d = noble_paged_desc(B, per, pages, page, rows // B, 0, H, K, D, _dtype_code(q), 1.0, 0.0, 0)
     e = noble_select_desc(count, sink, local, 0)
     args = [_heads(q, "q", q.dtype, dev), _tensor(means, "means", q.dtype, (pages, K, D), dev),
@@ -247,6 +298,10 @@ def noble_attn_blocks(q, cache, page_table, lengths, chosen, slopes=None, *, sca
     """Attention of each sequence's last tokens, q [B n, heads, D], over the blocks that ``chosen`` int32 [B n, kv_heads,
     count] lists (noble_block_select), up to the row's token.  A list ends before its first entry that is not larger than
     the one before it, negative, or past the row's own block."""
+    if stream is None:
+        out = _native().attn_blocks(q, cache, page_table, lengths, chosen, slopes, scale, softcap, o)
+        if _served(out, "noble_attn_blocks"):
+            return out[0]
     s = _Sequences(q, cache, page_table, lengths, slopes, scale, softcap)
     if not isinstance(chosen, torch.Tensor) or chosen.dim() != 3:
         raise ValueError("chosen must be [rows, kv_heads, blocks]")
@@ -270,6 +325,10 @@ def noble_attn_weigh(q, cache, page_table, lengths, weights=None, slopes=None, *
     every token has received, float32 [B, kv_heads, page_table.shape[1] * page]: what ``weights`` holds for the tokens
     before the new ones (None: nothing) and the sum of the rows' probabilities.  ``out`` may be ``weights`` (None: a new
     tensor, zeros past the sequences' tokens; a given one is left as it is there)."""
+    if stream is None:
+        served = _native().attn_weigh(q, cache, page_table, lengths, weights, slopes, scale, softcap, o, out)
+        if _served(served, "noble_attn_weigh"):
+            return served
     s = _Sequences(q, cache, page_table, lengths, slopes, scale, softcap)
     shape = (s.B, s.K, s.tokens)
     pw = _tensor(weights, "weights", torch.float32, shape, s.dev)
@@ -289,14 +348,17 @@ def noble_evict_select(weights, lengths, keep: int, *, sink: int = 0, recent: in
     """(kept, kept_weights): the ``keep`` tokens of each sequence and key head that stay, int32 [B, heads, keep], ascending,
     -1 behind the last, and their weights (0 there).  All, if there are no more; else the first ``sink``, the last
     ``recent`` and, of the others, those with the most of weights float32 [B, heads, tokens]."""
+    if stream is None:
+        out = _native().evict_select(weights, lengths, keep, sink, recent, kept, kept_weights)
+        if _served(out, "noble_evict_select"):
+            return out
     dev = _gpu(weights, "weights")
     if weights.dim() != 3:
         raise ValueError(f"weights must be [sequences, heads, tokens], got {tuple(weights.shape)}")
     B, H, row = weights.shape
+    _whole(keep=keep, sink=sink, recent=recent)
     d = noble_evict_desc(B, row, H, keep, sink, recent)
     args = [_tensor(weights, "weights", torch.float32, None, dev), _int32(lengths, "lengths", (B,), dev)]
-    if not 1 <= keep < 2 ** 31:
-        raise ValueError(f"keep={keep} tokens")
     with _work(dev, stream) as (st, shared):
         kept = torch.empty((B, H, keep), dtype=torch.int32, device=dev) if kept is None else kept
         kept_weights = torch.empty((B, H, keep), device=dev) if kept_weights is None else kept_weights
