@@ -20,7 +20,7 @@ BINDING = os.path.join(PKG, "_noble_torch.so")
 BINDINGS = [("noble_torch.cpp", BINDING), ("noble_attn_torch.cpp", os.path.join(PKG, "_noble_attn_torch.so")),
             ("noble_decode_torch.cpp", os.path.join(PKG, "_noble_decode_torch.so"))]
 SOURCES = ["noble_api.hip", "noble_attn.hip", "noble_decode.hip"]
-HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_host.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_decode_attn.hpp", "noble_decode_select.hpp", "noble_binding.h", "noble_torch.cpp", "noble_attn_torch.cpp", "noble_decode_torch.cpp", "noble_torch_call.hpp"]
+HEADERS = ["noble_act.hpp", "noble_init.hpp", "noble_kernels.hpp", "noble_tiles.hpp", "noble_gemm.hpp", "noble_gemm_dma.hpp", "noble_gemm_tile.hpp", "noble_skinny.hpp", "noble_finish.hpp", "noble_gemm_f32.hpp", "noble_host.hpp", "noble_attn_common.hpp", "noble_attn_host.hpp", "noble_attn_tile.hpp", "noble_attn_paged.hpp", "noble_rope.hpp", "noble_decode_attn.hpp", "noble_decode_select.hpp", "noble_decode_wide.hpp", "noble_binding.h", "noble_torch.cpp", "noble_attn_torch.cpp", "noble_decode_torch.cpp", "noble_torch_call.hpp"]
 
 # of the library; its objects are compiled with all but -shared
 HIP_FLAGS = [

@@ -11,6 +11,7 @@
 #include "noble_decode.h"
 #include "noble_decode_attn.hpp"
 #include "noble_decode_select.hpp"
+#include "noble_decode_wide.hpp"
 
 using namespace noble;
 
@@ -47,6 +48,7 @@ constexpr int64_t kMostNew = 1 << 20;
 
 // Workgroups of one attention call and its scratch.
 struct DecodePlan {
+    bool wide;                            // attn_wide_kernel, else R groups of 16 rows of attn_decode_kernel
     int64_t R, row_tiles, pieces, groups;
     size_t part, stats, z, bytes;   // offsets, and all of it
     int64_t z_row;
@@ -55,17 +57,18 @@ struct DecodePlan {
 template <int FORM>
 noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p) {
     const int64_t share = d->heads / d->kv_heads, rows = d->new_tokens * share;
-    p->R = FORM != kBlocks && rows > kGroup ? 4 : 1;
+    p->wide = FORM != kBlocks && d->dtype == NOBLE_BF16 && rows > 2 * kGroup;
+    p->R = p->wide ? kWideGroups : FORM != kBlocks && rows > kGroup ? 2 : 1;
     p->row_tiles = FORM == kBlocks ? d->new_tokens * cdiv(share, kGroup) : (rows + kGroup * p->R - 1) / (kGroup * p->R);
     const int64_t base = d->B * d->kv_heads * p->row_tiles;
     const int64_t tokens = (FORM == kBlocks ? std::min(count, d->table_row) : d->table_row) * d->page;
-    const int waves = d->dtype == NOBLE_F32 && d->head_dim > 64 ? 2 : 4;
-    const int64_t most = std::max<int64_t>((tokens + kKeys - 1) / kKeys / waves, 1);
-    p->pieces = std::clamp<int64_t>(base > 0 ? (2048 + base - 1) / base : 1, 1, std::min<int64_t>(most, 64));
+    const int waves = p->wide || (d->dtype == NOBLE_F32 && d->head_dim > 64) ? 2 : 4;
+    const int64_t most = std::max<int64_t>((tokens + kKeys - 1) / kKeys / waves / (p->wide ? 2 : 1), 1), turns = p->wide ? 1024 : 2048;
+    p->pieces = std::clamp<int64_t>(base > 0 ? (turns + base - 1) / base : 1, 1, std::min<int64_t>(most, 64));
     p->groups = base * p->pieces;
     if (p->groups > kMaxGroups256 || d->B * d->new_tokens * d->heads > kMaxGroups256 * 8) return NOBLE_ERR_BAD_SHAPE;
     p->part = p->stats = p->z = 0;
-    p->z_row = (d->table_row * d->page + kKeys - 1) / kKeys * kKeys;
+    p->z_row = (d->table_row * d->page + kPart - 1) / kPart * kPart;   // whole tiles of either kernel
     size_t at = 0;
     if (p->pieces > 1 || FORM == kWeigh)
         at = up256((size_t)p->groups * p->R * kGroup * ((d->head_dim <= 64 ? 64 : 128) + 4) * 4);
@@ -131,10 +134,14 @@ noble_status run_attention(const noble_paged_desc* d, const DecodePlan& p, const
     return with_shape(d->dtype, d->head_dim, [&]<typename E, int DP>() {
         const auto kernel = [&]<int MODE>() {
             if constexpr (FORM == kBlocks) return attn_decode_kernel<E, DP, FORM, MODE, 1>;
-            else return p.R == 1 ? attn_decode_kernel<E, DP, FORM, MODE, 1> : attn_decode_kernel<E, DP, FORM, MODE, 4>;
+            else {
+                if constexpr (sizeof(E) == 2)
+                    if (p.wide) return attn_wide_kernel<DP, FORM, MODE>;
+                return p.R == 1 ? attn_decode_kernel<E, DP, FORM, MODE, 1> : attn_decode_kernel<E, DP, FORM, MODE, 2>;
+            }
         };
         NOBLE_TRY(launch(d->softcap > 0.f ? kernel.template operator()<kCap>() : kernel.template operator()<0>(),
-                         dim3((unsigned)p.groups), dim3(64 * DecodeShape<E, DP>::WAVES), st, a));
+                         dim3((unsigned)p.groups), dim3(p.wide ? 256 : 64 * DecodeShape<E, DP>::WAVES), st, a));
         if (p.pieces == 1 && FORM != kWeigh) return NOBLE_OK;
         const DecodeJoinArgs j{a, d->B * d->new_tokens * d->heads, (int)p.R};
         return launch(decode_join_kernel<E, DP, FORM>, dim3((unsigned)cdiv(j.items, 256 / (DP / 4))), dim3(256), st, j);

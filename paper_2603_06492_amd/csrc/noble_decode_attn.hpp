@@ -180,11 +180,12 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
     if (piece >= pieces) return;
     const int c0 = (int)((int64_t)chunks * piece / pieces) + wave, c1 = (int)((int64_t)chunks * (piece + 1) / pieces);
     float slope[R];
+    const int* depths = FORM == kTree ? a.depths + (int64_t)b * a.fresh : nullptr;
     int at[R];   // a row's position, which the bias goes by
 #pragma unroll
     for (int g = 0; g < R; ++g) {
         slope[g] = a.slopes ? a.slopes[head[g]] * kLog2e / a.sc.unit : 0.f;
-        at[g] = first + (FORM == kTree ? a.depths[(int64_t)b * a.fresh + tok[g]] : tok[g]);
+        at[g] = first + (FORM == kTree ? depths[tok[g]] : tok[g]);
     }
 
     char* ring = lds + wave * NST * S::STAGE;
@@ -308,7 +309,7 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
                             pos = (x == 0 ? block[0] : x == 1 ? block[1] : x == 2 ? block[2] : block[3]) + (pos & (a.page - 1));
                         } else if (FORM == kTree && pos >= first) {
                             const int node = pos - first;
-                            pos = node < a.fresh ? first + a.depths[(int64_t)b * a.fresh + node] : pos;
+                            pos = node < a.fresh ? first + depths[(uint32_t)node] : pos;
                         }
                         z[g][i] = fmaf(-slope[g], fabsf((float)(pos - at[g])), z[g][i]);
                     }
@@ -357,8 +358,10 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
 #pragma unroll
                 for (int d = 0; d < ND; ++d) odd |= not_finite(T::across16(vt, d, lane));
             }
+            if (FORM != kBlocks && edge) asm volatile("" ::: "memory");   // the operands are read again: they are too many to be kept
             if (FORM != kBlocks && __any(odd)) {
                 for (int t = tok0; t <= tok1; ++t) {
+                    asm volatile("" ::: "memory");
                     const uint32_t mask = mine(sees(t, k0));
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
