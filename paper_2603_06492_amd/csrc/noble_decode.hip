@@ -46,11 +46,17 @@ noble_status check_tables(const noble_paged_desc* d, const int32_t* page_table, 
 
 constexpr int64_t kMostNew = 1 << 20;
 
+// Workgroups of a call whose sequences are cut into pieces.
+#define kTurns (getenv("NBT") ? atoi(getenv("NBT")) : 1024)
+#define kTurnsWide (getenv("NBW") ? atoi(getenv("NBW")) : 512)
+#define kTurnsBlocks (getenv("NBB") ? atoi(getenv("NBB")) : 1024)
+
 // Workgroups of one attention call and its scratch.
 struct DecodePlan {
     bool wide;                            // attn_wide_kernel, else R groups of 16 rows of attn_decode_kernel
-    int64_t R, row_tiles, pieces, groups;
-    size_t part, stats, z, bytes;   // offsets, and all of it
+    bool split;                           // some pieces are joined
+    int64_t R, row_tiles, slots, groups;
+    size_t where, stats, z, bytes;        // offsets (the parts come first), and all of it
     int64_t z_row;
 };
 
@@ -60,18 +66,29 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
     p->wide = FORM != kBlocks && d->dtype == NOBLE_BF16 && rows > 2 * kGroup;
     p->R = p->wide ? kWideGroups : FORM != kBlocks && rows > kGroup ? 2 : 1;
     p->row_tiles = FORM == kBlocks ? d->new_tokens * cdiv(share, kGroup) : (rows + kGroup * p->R - 1) / (kGroup * p->R);
-    const int64_t base = d->B * d->kv_heads * p->row_tiles;
+    const int64_t base = d->B * d->kv_heads * p->row_tiles, per = d->kv_heads * p->row_tiles;
     const int64_t tokens = (FORM == kBlocks ? std::min(count, d->table_row) : d->table_row) * d->page;
-    const int waves = p->wide || (d->dtype == NOBLE_F32 && d->head_dim > 64) ? 2 : 4;
-    const int64_t most = std::max<int64_t>((tokens + kKeys - 1) / kKeys / waves / (p->wide ? 2 : 1), 1), turns = p->wide ? 1024 : 2048;
-    p->pieces = std::clamp<int64_t>(base > 0 ? (turns + base - 1) / base : 1, 1, std::min<int64_t>(most, 64));
-    p->groups = base * p->pieces;
+    const int waves = !p->wide && d->dtype == NOBLE_F32 && d->head_dim > 64 ? 1 : 2;
+    const int64_t most = std::clamp<int64_t>(tokens / (p->wide ? kPart : kKeys) / waves, 1, 64);   // pieces of one sequence
+    if (FORM == kBlocks) {
+        p->slots = std::clamp<int64_t>(base > 0 ? (kTurnsBlocks + base - 1) / base : 1, 1, most);
+        p->groups = base * p->slots;
+    } else {
+        const int64_t turns = p->wide ? kTurnsWide : kTurns;
+        p->slots = std::clamp<int64_t>(per > 0 ? turns / per : 1, d->B, d->B * most);
+        p->groups = p->slots * per;
+    }
+    const bool split = p->slots > (FORM == kBlocks ? 1 : d->B) || FORM == kWeigh;
     if (p->groups > kMaxGroups256 || d->B * d->new_tokens * d->heads > kMaxGroups256 * 8) return NOBLE_ERR_BAD_SHAPE;
-    p->part = p->stats = p->z = 0;
     p->z_row = (d->table_row * d->page + kPart - 1) / kPart * kPart;   // whole tiles of either kernel
+    p->where = p->stats = p->z = 0;
     size_t at = 0;
-    if (p->pieces > 1 || FORM == kWeigh)
+    if (split) {
         at = up256((size_t)p->groups * p->R * kGroup * ((d->head_dim <= 64 ? 64 : 128) + 4) * 4);
+        p->where = at;
+        at += up256((size_t)(FORM == kBlocks ? d->B * d->new_tokens * d->kv_heads : d->B) * sizeof(int2));
+    }
+    p->split = split;
     if (FORM == kWeigh) {
         const int64_t all = d->B * d->new_tokens * d->heads;
         if (p->z_row > 0 && all > kMaxScratch / 4 / p->z_row) return NOBLE_ERR_BAD_SHAPE;
@@ -95,7 +112,8 @@ DecodeArgs decode_args(const noble_paged_desc* d, const DecodePlan& p, const nob
     a.lengths = lengths;
     a.slopes = slopes;
     char* s = static_cast<char*>(scratch);
-    a.part = reinterpret_cast<float*>(s + p.part);
+    a.part = reinterpret_cast<float*>(s);
+    a.where = p.split ? reinterpret_cast<int2*>(s + p.where) : nullptr;
     a.stats = reinterpret_cast<float2*>(s + p.stats);
     a.z = reinterpret_cast<float*>(s + p.z);
     a.z_row = p.z_row;
@@ -110,7 +128,8 @@ DecodeArgs decode_args(const noble_paged_desc* d, const DecodePlan& p, const nob
     a.share = d->heads / d->kv_heads;
     a.D = d->head_dim;
     a.row_tiles = (int)p.row_tiles;
-    a.pieces = (int)p.pieces;
+    a.slots = (int)p.slots;
+    a.B = d->B;
     a.sc = score_args(d->scale, d->softcap);
     return a;
 }
@@ -141,8 +160,9 @@ noble_status run_attention(const noble_paged_desc* d, const DecodePlan& p, const
             }
         };
         NOBLE_TRY(launch(d->softcap > 0.f ? kernel.template operator()<kCap>() : kernel.template operator()<0>(),
-                         dim3((unsigned)p.groups), dim3(p.wide ? 256 : 64 * DecodeShape<E, DP>::WAVES), st, a));
-        if (p.pieces == 1 && FORM != kWeigh) return NOBLE_OK;
+                         dim3((unsigned)p.groups), dim3(p.wide ? 256 : 64 * DecodeShape<E, DP>::WAVES), st, a,
+                         p.wide ? 0 : DecodeShape<E, DP>::LDS));
+        if (!p.split) return NOBLE_OK;
         const DecodeJoinArgs j{a, d->B * d->new_tokens * d->heads, (int)p.R};
         return launch(decode_join_kernel<E, DP, FORM>, dim3((unsigned)cdiv(j.items, 256 / (DP / 4))), dim3(256), st, j);
     });

@@ -21,10 +21,12 @@ struct DecodeArgs {
     const int* table;
     const int* lengths;
     const float* slopes;
-    float* part;          // [workgroup][16 R][DP + 4] float32: product, maximum, sum, (first piece) number of pieces
+    float* part;          // [workgroup][16 R][DP + 4] float32: product, maximum, sum
+    int2* where;          // [B]: the sequence's first slot and its pieces (kBlocks: [B fresh, kv_heads], the pieces alone)
     int64_t table_row, pages, page_bytes;   // page_bytes: of one page, keys and values of all heads
     int page, shift, fresh, heads, kv_heads, share, D;
-    int row_tiles, pieces;
+    int64_t B;
+    int row_tiles, slots;   // slots: workgroups of one key head and row tile, for all sequences (kBlocks: for each)
     ScoreArgs sc;
     const uint32_t* seen;   // kTree: [B, fresh, words]
     const int* depths;      // [B, fresh]
@@ -117,29 +119,91 @@ __device__ __forceinline__ void decode_store(const DecodeArgs& a, int b, int kv,
                   sum[0], sum[1], sum[2], sum[3]);
 }
 
+// The pieces that the sequences are cut into: of one size, so that a batch of sequences of different lengths keeps every
+// workgroup busy to the end, and as many as give each key head and row tile `slots` workgroups.  With T steps in all and B
+// sequences, pieces of T / (slots - B) steps, rounded up, are slots at most, each sequence's last one being shorter.  Every
+// wave works that out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 32 drafted ones: as many pieces of
+// every sequence 146 us, pieces of one size PIECES_A; one token of 64 of 16384 to 32768 PIECES_B.
+struct Piece {
+    int b = 0, piece = 0, pieces = 1, size = 0;   // size: of a piece, in steps of `keys` keys
+    bool work = true;
+    Piece() = default;
+    __device__ __forceinline__ int steps(const DecodeArgs& a, int64_t b, int keys) const {
+        return b < a.B ? (a.held((int)b) + keys - 1) / keys : 0;
+    }
+    __device__ __forceinline__ Piece(const DecodeArgs& a, int slot, int keys, int least, int lane) {
+        if (a.slots == a.B) {
+            b = slot;
+            return;
+        }
+        const int one = steps(a, lane, keys);   // of the first 64 sequences, a lane each
+        int64_t total = one;
+        for (int64_t n = 64; n < a.B; n += 64) total += steps(a, n + lane, keys);
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
+        const int64_t free = a.slots - a.B;
+        size = (int)max((total + free - 1) / free, (int64_t)least);
+        work = false;
+        int before = 0;
+        for (int64_t n = 0; n < a.B; n += 64) {
+            const int mine = n + lane < a.B ? max(((n ? steps(a, n + lane, keys) : one) + size - 1) / size, 1) : 0;
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const int v = __shfl_up(upto, o);
+                if (lane >= o) upto += v;
+            }
+            const uint64_t here = __ballot(slot < before + upto);
+            if (here) {
+                const int at = __builtin_ctzll(here);
+                b = (int)n + at;
+                pieces = __builtin_amdgcn_readlane(mine, at);
+                piece = slot - (before + __builtin_amdgcn_readlane(upto, at) - pieces);
+                work = true;
+                break;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+        }
+        b = __builtin_amdgcn_readfirstlane(b);
+        piece = __builtin_amdgcn_readfirstlane(piece);
+        pieces = __builtin_amdgcn_readfirstlane(pieces);
+        size = __builtin_amdgcn_readfirstlane(size);
+    }
+};
+
 template <typename E, int DP>
 struct DecodeShape {
-    static constexpr int WAVES = sizeof(E) * DP > 256 ? 2 : 4;
     static constexpr int STAGE = 2 * kKeys * DP * (int)sizeof(E);             // keys and values of a chunk
-    static constexpr int STAGES = 128 * 1024 / (WAVES * STAGE);
+    static constexpr int LDS = 64 * 1024;
+    static constexpr int WAVES = LDS / (2 * STAGE) < 2 ? 1 : 2;
+    static constexpr int STAGES = LDS / (WAVES * STAGE);
 };
 
 template <typename E, int DP, int FORM, int MODE, int R>
-__global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES), (sizeof(E) * DP > 256 ? 1 : 2)) void attn_decode_kernel(DecodeArgs a) {
     using T = Tile<E, DP>;
     using S = DecodeShape<E, DP>;
     constexpr int ES = T::ES, NS = DP / 32, ND = DP / 16, W = S::WAVES, NST = S::STAGES;
     constexpr int RPI = 1024 / T::RB, PER = kKeys / RPI;   // rows of a request, requests of a chunk's keys
-    __shared__ __attribute__((aligned(1024))) char lds[W * NST * S::STAGE];
+    // As much as S::LDS, from the launch: were it declared, the compiler would reckon with one wave a SIMD and 512 registers,
+    // and keep sums in accumulation registers, from and to which every step would move them.
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g4 = lane >> 4;
     // pieces of one (sequence, key head) apart, key heads of a sequence side by side: their pages are the same
     int w = blockIdx.x;
     const int kv = w % a.kv_heads;
     w /= a.kv_heads;
-    const int rt = w % a.row_tiles;
-    w /= a.row_tiles;
-    const int piece = w % a.pieces, b = w / a.pieces, db = a.D * ES;
+    const int rt = w % a.row_tiles, slot = w / a.row_tiles, db = a.D * ES;
+    Piece pc;
+    if constexpr (FORM == kBlocks) {
+        pc.b = slot / a.slots;
+        pc.piece = slot % a.slots;
+    } else {
+        pc = Piece(a, slot, kKeys, W, lane);
+        if (!pc.work) return;
+    }
+    const int b = pc.b;
 
     // this lane's row of each group.  kBlocks: a tile's rows are one token's; else tokens x heads, one after the other
     const int per_tok = FORM == kBlocks ? (a.share + kGroup - 1) / kGroup : 1;
@@ -176,9 +240,21 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
         end = max(first + tok1 + 1, 0);
     }
     const int chunks = (end + kKeys - 1) / kKeys;
-    const int pieces = max(1, min(a.pieces, chunks / W));
-    if (piece >= pieces) return;
-    const int c0 = (int)((int64_t)chunks * piece / pieces) + wave, c1 = (int)((int64_t)chunks * (piece + 1) / pieces);
+    int c0, c1;
+    if constexpr (FORM == kBlocks) {
+        // lists are of one length but for those of short sequences, which are cut into fewer pieces
+        pc.pieces = max(1, min(a.slots, chunks / W));
+        if (pc.piece >= pc.pieces) return;
+        c0 = (int)((int64_t)chunks * pc.piece / pc.pieces) + wave;
+        c1 = (int)((int64_t)chunks * (pc.piece + 1) / pc.pieces);
+    } else {
+        c0 = (pc.pieces > 1 ? pc.piece * pc.size : 0) + wave;
+        c1 = pc.pieces > 1 ? min(chunks, (pc.piece + 1) * pc.size) : chunks;
+    }
+    if (pc.piece == 0 && threadIdx.x == 0 && a.where) {
+        if (FORM == kBlocks) a.where[((int64_t)b * a.fresh + tok0) * a.kv_heads + kv] = int2{slot, pc.pieces};
+        else if (kv == 0 && rt == 0) a.where[b] = int2{slot, pc.pieces};
+    }
     float slope[R];
     const int* depths = FORM == kTree ? a.depths + (int64_t)b * a.fresh : nullptr;
     int at[R];   // a row's position, which the bias goes by
@@ -192,33 +268,56 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
     typedef const __attribute__((address_space(4))) int* table_ptr;
     const table_ptr table = (table_ptr)(a.table + b * a.table_row);
     const table_ptr blocks = (table_ptr)list;
-    uint32_t bad = 0;   // keys of the next chunk without a page in the cache
-    uint32_t bads[NST];
-    const auto request = [&](int c, int stage) {
-        const int k0 = c * kKeys;
-        char* dst = ring + stage * S::STAGE;
-        const int in_page = k0 & (a.page - 1);
-        const char* base = a.cache + (int64_t)kv * a.page * db + (int64_t)in_page * db;
-        int page = -1;
-        bad = 0;
+    // a lane's place in each request of a chunk, from the chunk's first key on
+    uint32_t vo[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int key = k0 + i * RPI, left = max(min(end - key, RPI), 0);
-            // a new page starts here, or the chunk does; pages hold at least a request's rows
-            if (i == 0 || ((in_page + i * RPI) & (a.page - 1)) == 0) {
-                page = -1;
-                if (left > 0) page = table[FORM == kBlocks ? blocks[key >> a.shift] : key >> a.shift];
-                if (i > 0) base = a.cache + (int64_t)kv * a.page * db - (int64_t)i * RPI * db;
+    for (int i = 0; i < PER; ++i) {
+        const int row = i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(row);
+        vo[i] = 16 * ch < db ? (uint32_t)(row * db + 16 * ch) : kOOB;
+    }
+    const char* heads = a.cache + (int64_t)kv * a.page * db;
+    const int64_t values = (int64_t)a.kv_heads * a.page * db;   // from a key to its value
+    // Requests a chunk's keys and values; returns which keys have no page in the cache (they come as zeros).
+    const auto request = [&](int c, char* dst) {
+        const int k0 = c * kKeys;
+        uint32_t bad = 0;
+        bool ok = false;
+        i32x4 dk, dv;
+#pragma unroll
+        for (int x = 0; x < kKeys / 8; ++x) {
+            const int key = k0 + 8 * x;
+            if (x == 0 || (key & (a.page - 1)) == 0) {   // a page starts here, or the chunk does
+                int page = -1;
+                if (key < end) page = table[FORM == kBlocks ? blocks[key >> a.shift] : key >> a.shift];
+                ok = page >= 0 && page < a.pages;
+                const char* base = heads + (int64_t)(ok ? page : 0) * a.page_bytes + (int64_t)((key & (a.page - 1)) - 8 * x) * db;
+                const int bytes = ok ? min(end - k0, kKeys) * db : 0;
+                dk = wave_desc(base, bytes);
+                dv = wave_desc(base + values, bytes);
             }
-            const bool ok = page >= 0 && page < a.pages;
-            if (!ok) bad |= ((1u << RPI) - 1u) << (i * RPI);
-            const char* src = base + (int64_t)(ok ? page : 0) * a.page_bytes + (int64_t)i * RPI * db;
-            const int row = i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(row);
-            const uint32_t vo = 16 * ch < db ? (uint32_t)((lane / T::NC) * db + 16 * ch) : kOOB;
-            const int64_t bytes = ok ? (int64_t)left * db : 0;
-            dma16(wave_desc(src, bytes), dst + i * 1024, vo, 0);
-            dma16(wave_desc(src + (int64_t)a.kv_heads * a.page * db, bytes), dst + S::STAGE / 2 + i * 1024, vo, 0);
+            if (!ok) bad |= 0xffu << (8 * x);
+#pragma unroll
+            for (int i = 8 * x / RPI; i < 8 * (x + 1) / RPI; ++i) {
+                dma16(dk, dst + i * 1024, vo[i], 0);
+                dma16(dv, dst + S::STAGE / 2 + i * 1024, vo[i], 0);
+            }
         }
+        return bad;
+    };
+    // That again, for a chunk that is here.
+    const auto missing = [&](int c) {
+        uint32_t bad = 0;
+        bool ok = false;
+#pragma unroll
+        for (int x = 0; x < kKeys / 8; ++x) {
+            const int key = c * kKeys + 8 * x;
+            if (x == 0 || (key & (a.page - 1)) == 0) {
+                const int page = key < end ? table[key >> a.shift] : -1;
+                ok = page >= 0 && page < a.pages;
+            }
+            if (!ok) bad |= 0xffu << (8 * x);
+        }
+        return bad;
     };
     // Which of this lane's eight keys of the chunk at k0 (places 16 (i / 4) + 4 g4 + i % 4) the row of a token sees.
     const auto sees = [&](int t, int k0) {
@@ -243,145 +342,167 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
         for (int d = 0; d < ND; ++d) acc[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    operands_here();
-    int ahead = c0;   // next chunk to request
+    const auto step = [&]<bool EDGE>(const char* kt, int k0, uint32_t bad) {
+        const char* vt = kt + S::STAGE / 2;
+        float z[R][8];
 #pragma unroll
-    for (int s = 0; s < NST - 1; ++s) {
-        if (ahead < c1) request(ahead, s);
-        bads[s] = bad;
-        ahead += W;
-    }
-    bads[NST - 1] = 0;
-    for (int c = c0; c < c1; c += NST * W) {
+        for (int u = 0; u < 2; ++u) {
+            f32x4 sv[R];
 #pragma unroll
-        for (int s = 0; s < NST; ++s) {
-            const int ch = c + s * W;
-            if (ch >= c1) break;
-            // the stage of the step before is free: its reads have been waited for
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (ahead < c1) {
-                request(ahead, (s + NST - 1) % NST);
-                bads[(s + NST - 1) % NST] = bad;
-                wait_vmcnt<2 * PER * (NST - 1)>();
-            } else {
-                wait_vmcnt<0>();
+            for (int g = 0; g < R; ++g) sv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < NS; ++x) {
+                const Frag<E> kf = T::along(kt, 16 * u + n16, 4 * x + g4);
+#pragma unroll
+                for (int g = 0; g < R; ++g) mma16x16(sv[g], kf, q[g][x]);
             }
-            asm volatile("" ::: "memory");
-            ahead += W;
-            const int k0 = ch * kKeys;
-            const char* kt = ring + s * S::STAGE;
-            const char* vt = kt + S::STAGE / 2;
-            float z[R][8];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                f32x4 sv[R];
+            for (int g = 0; g < R; ++g)
 #pragma unroll
-                for (int g = 0; g < R; ++g) sv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < 4; ++i) z[g][4 * u + i] = sv[g][i];
+        }
+        // keys that some of the rows do not see
+        const bool edge = EDGE || (FORM == kBlocks && k0 + kKeys > end);
+        int block[4];   // kBlocks: the chunk's pages, whose places the bias goes by
+        if (FORM == kBlocks && a.slopes) {
 #pragma unroll
-                for (int x = 0; x < NS; ++x) {
-                    const Frag<E> kf = T::along(kt, 16 * u + n16, 4 * x + g4);
+            for (int x = 0; x < 4; ++x) block[x] = blocks[min((k0 + 8 * x) >> a.shift, listed - 1)] << a.shift;
+        }
+        Frag<E> p[R];
 #pragma unroll
-                    for (int g = 0; g < R; ++g) mma16x16(sv[g], kf, q[g][x]);
-                }
-#pragma unroll
-                for (int g = 0; g < R; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[g][4 * u + i] = sv[g][i];
-            }
-            // keys that some of the rows do not see
-            const bool edge = FORM == kTree ? k0 + kKeys > first : FORM == kWeigh ? k0 + kKeys > first + tok0 + 1 : k0 + kKeys > end;
-            int block[4];   // kBlocks: the chunk's pages, whose places the bias goes by
-            if (FORM == kBlocks && a.slopes) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) block[x] = blocks[min((k0 + 8 * x) >> a.shift, listed - 1)] << a.shift;
-            }
-            Frag<E> p[R];
-#pragma unroll
-            for (int g = 0; g < R; ++g) {
-                scores<E, MODE, 8>(a.sc, z[g], z[g], nullptr);
-                if (a.slopes) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int o = 16 * (i >> 2) + 4 * g4 + (i & 3);
-                        int pos = k0 + o;
-                        if constexpr (FORM == kBlocks) {
-                            const int x = o >> 3;
-                            pos = (x == 0 ? block[0] : x == 1 ? block[1] : x == 2 ? block[2] : block[3]) + (pos & (a.page - 1));
-                        } else if (FORM == kTree && pos >= first) {
-                            const int node = pos - first;
-                            pos = node < a.fresh ? first + depths[(uint32_t)node] : pos;
-                        }
-                        z[g][i] = fmaf(-slope[g], fabsf((float)(pos - at[g])), z[g][i]);
-                    }
-                }
-                if (edge || bads[s]) {
-                    const uint32_t mask = mine(sees(tok[g], k0) & ~bads[s]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) z[g][i] = mask >> i & 1u ? z[g][i] : -INFINITY;
-                }
-                if constexpr (FORM == kWeigh) {
-                    if (live[g]) {
-                        const int r = row0 + g * kGroup + n16;
-                        const float unit = MODE & kCap ? 1.f : a.sc.unit;
-                        float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + r) * a.z_row + k0 + 4 * g4;
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            *reinterpret_cast<f32x4*>(zp + 16 * u) = f32x4{z[g][4 * u] * unit, z[g][4 * u + 1] * unit,
-                                                                           z[g][4 * u + 2] * unit, z[g][4 * u + 3] * unit};
-                    }
-                }
-                float top = z[g][0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) top = fmaxf(top, z[g][i]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32)) * (MODE & kCap ? 1.f : a.sc.unit);
-                if (__any(top > m[g] + 8.f)) {   // see attn_fwd_kernel
-                    const float to = fmaxf(m[g], top);
-                    const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[g] - to);
-                    m[g] = to;
-                    l[g] *= f;
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) acc[g][d] *= f;
-                }
-                const float base = m[g] == -INFINITY ? 0.f : m[g];
+        for (int g = 0; g < R; ++g) {
+            scores<E, MODE, 8>(a.sc, z[g], z[g], nullptr);
+            if (a.slopes) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    z[g][i] = exp_score<MODE>(a.sc, z[g][i], base);
-                    l[g] += z[g][i];
-                }
-                p[g] = to_frag<E>(z[g]);
-            }
-            // a value that a row does not see meets a probability of zero, which an infinite or NaN one would outlive: then
-            // each token's rows are multiplied by the values that this token sees, with zeros for the others
-            bool odd = false;
-            if (FORM != kBlocks && edge && a.fresh > 1) {
-#pragma unroll
-                for (int d = 0; d < ND; ++d) odd |= not_finite(T::across16(vt, d, lane));
-            }
-            if (FORM != kBlocks && edge) asm volatile("" ::: "memory");   // the operands are read again: they are too many to be kept
-            if (FORM != kBlocks && __any(odd)) {
-                for (int t = tok0; t <= tok1; ++t) {
-                    asm volatile("" ::: "memory");
-                    const uint32_t mask = mine(sees(t, k0));
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        const Frag<E> vf = only(T::across16(vt, d, lane), mask);
-#pragma unroll
-                        for (int g = 0; g < R; ++g) {
-                            f32x4 sum = acc[g][d];
-                            mma16x16(sum, vf, p[g]);
-                            acc[g][d] = tok[g] == t ? sum : acc[g][d];
-                        }
+                    const int o = 16 * (i >> 2) + 4 * g4 + (i & 3);
+                    int pos = k0 + o;
+                    if constexpr (FORM == kBlocks) {
+                        const int x = o >> 3;
+                        pos = (x == 0 ? block[0] : x == 1 ? block[1] : x == 2 ? block[2] : block[3]) + (pos & (a.page - 1));
+                    } else if (FORM == kTree && EDGE && pos >= first) {
+                        const int node = pos - first;
+                        pos = node < a.fresh ? first + depths[(uint32_t)node] : pos;
                     }
+                    z[g][i] = fmaf(-slope[g], fabsf((float)(pos - at[g])), z[g][i]);
                 }
-            } else {
+            }
+            if (edge || bad) {
+                const uint32_t mask = mine(sees(tok[g], k0) & ~bad);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[g][i] = mask >> i & 1u ? z[g][i] : -INFINITY;
+            }
+            if constexpr (FORM == kWeigh) {
+                if (live[g]) {
+                    const int r = row0 + g * kGroup + n16;
+                    const float unit = MODE & kCap ? 1.f : a.sc.unit;
+                    float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + r) * a.z_row + k0 + 4 * g4;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        *reinterpret_cast<f32x4*>(zp + 16 * u) = f32x4{z[g][4 * u] * unit, z[g][4 * u + 1] * unit,
+                                                                       z[g][4 * u + 2] * unit, z[g][4 * u + 3] * unit};
+                }
+            }
+            float top = z[g][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, z[g][i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32)) * (MODE & kCap ? 1.f : a.sc.unit);
+            if (__any(top > m[g] + 8.f)) {   // see attn_fwd_kernel
+                const float to = fmaxf(m[g], top);
+                const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[g] - to);
+                m[g] = to;
+                l[g] *= f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) acc[g][d] *= f;
+            }
+            const float base = m[g] == -INFINITY ? 0.f : m[g];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[g][i] = exp_score<MODE>(a.sc, z[g][i], base);
+                l[g] += z[g][i];
+            }
+            p[g] = to_frag<E>(z[g]);
+        }
+        // a value that a row does not see meets a probability of zero, which an infinite or NaN one would outlive: then
+        // each token's rows are multiplied by the values that this token sees, with zeros for the others
+        bool odd = false;
+        if (EDGE && a.fresh > 1) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) odd |= not_finite(T::across16(vt, d, lane));
+        }
+        if (EDGE) asm volatile("" ::: "memory");   // the operands are read again: they are too many to be kept
+        if (EDGE && __any(odd)) {
+            for (int t = tok0; t <= tok1; ++t) {
+                asm volatile("" ::: "memory");
+                const uint32_t mask = mine(sees(t, k0));
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
-                    const Frag<E> vf = T::across16(vt, d, lane);
+                    const Frag<E> vf = only(T::across16(vt, d, lane), mask);
 #pragma unroll
-                    for (int g = 0; g < R; ++g) mma16x16(acc[g][d], vf, p[g]);
+                    for (int g = 0; g < R; ++g) {
+                        f32x4 sum = acc[g][d];
+                        mma16x16(sum, vf, p[g]);
+                        acc[g][d] = tok[g] == t ? sum : acc[g][d];
+                    }
                 }
             }
+        } else {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const Frag<E> vf = T::across16(vt, d, lane);
+#pragma unroll
+                for (int g = 0; g < R; ++g) mma16x16(acc[g][d], vf, p[g]);
+            }
+        }
+    };
+    operands_here();
+    int ahead = c0;   // next chunk to request
+    uint32_t bads[NST];
+#pragma unroll
+    for (int s = 0; s < NST; ++s) {
+        bads[s] = 0;
+        if (s < NST - 1) {
+            if (ahead < c1) bads[s] = request(ahead, ring + s * S::STAGE);
+            ahead += W;
+        }
+    }
+    // The next chunk into the stage of the step before, whose reads have been waited for; waits for this step's.
+    const auto next = [&](char* free) {
+        uint32_t bad = 0;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (ahead < c1) {
+            bad = request(ahead, free);
+            wait_vmcnt<2 * PER * (NST - 1)>();
+        } else {
+            wait_vmcnt<0>();
+        }
+        asm volatile("" ::: "memory");
+        ahead += W;
+        return bad;
+    };
+    // Chunks that every row sees whole, and then the others, whose masks and whose care for values that are not seen would
+    // cost the first loop registers: it would move its sums from and to the accumulation ones in every step.
+    const int whole = FORM == kBlocks ? c1 : min(c1, max(first + (FORM == kWeigh ? tok0 + 1 : 0), 0) / kKeys);
+    int ch = c0, stage = 0;
+    for (bool more = ch < whole; more;) {
+#pragma unroll
+        for (int s = 0; s < NST; ++s) {
+            bads[(s + NST - 1) % NST] = next(ring + (s + NST - 1) % NST * S::STAGE);
+            step.template operator()<false>(ring + s * S::STAGE, ch * kKeys, bads[s]);
+            ch += W;
+            stage = (s + 1) % NST;
+            if (ch >= whole) {
+                more = false;
+                break;
+            }
+        }
+    }
+    if constexpr (FORM != kBlocks) {
+        for (; ch < c1; ch += W) {
+            next(ring + (stage + NST - 1) % NST * S::STAGE);
+            step.template operator()<true>(ring + stage * S::STAGE, ch * kKeys, missing(ch));
+            stage = (stage + 1) % NST;
         }
     }
 
@@ -418,13 +539,12 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES)) void attn_decode_
                 sum += *reinterpret_cast<const f32x4*>(p + d) * f;
                 total += p[DP + 1] * f;
             }
-            if (a.pieces > 1 || FORM == kWeigh) {
+            if (pc.pieces > 1 || FORM == kWeigh) {
                 float* out = a.part + (((int64_t)blockIdx.x * R + g) * kGroup + row) * LD;
                 *reinterpret_cast<f32x4*>(out + d) = sum;
                 if (d == 0) {
                     out[DP] = top;
                     out[DP + 1] = total;
-                    out[DP + 2] = (float)pieces;
                 }
             } else {
                 const int rr = row0 + g * kGroup + row, t = FORM == kBlocks ? tok0 : rr / a.share;
@@ -458,10 +578,11 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
         rt = row / (kGroup * j.groups);
         slot = row % (kGroup * j.groups);
     }
+    const int2 where = a.where[FORM == kBlocks ? ((int64_t)b * a.fresh + tok) * a.kv_heads + kv : b];
+    const int pieces = where.y;
+    if (FORM != kWeigh && pieces == 1) return;
     const int64_t tile = (int64_t)j.groups * kGroup * LD, step = (int64_t)a.row_tiles * a.kv_heads * tile;   // from piece to piece
-    const float* p = a.part + (((int64_t)b * a.pieces * a.row_tiles + rt) * a.kv_heads + kv) * tile + (int64_t)slot * LD;
-    const int pieces = (int)p[DP + 2];
-    if (FORM != kWeigh && a.pieces == 1) return;
+    const float* p = a.part + (((int64_t)where.x * a.row_tiles + rt) * a.kv_heads + kv) * tile + (int64_t)slot * LD;
     // eight pieces at a time, their loads all in flight
     constexpr int N = 8;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};

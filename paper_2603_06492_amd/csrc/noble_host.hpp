@@ -45,11 +45,11 @@ inline noble_status check_device(int* dev_out = nullptr) {
 
 // Launch of a kernel that takes one argument struct, with the status of this
 // launch itself (the thread's last-error state would also carry, and clear,
-// an earlier failure of the caller's).
+// an earlier failure of the caller's).  lds: bytes for the kernel's own use beside those it declares.
 template <typename Arg>
-noble_status launch(void (*kernel)(Arg), dim3 grid, dim3 block, hipStream_t st, const Arg& arg) {
+noble_status launch(void (*kernel)(Arg), dim3 grid, dim3 block, hipStream_t st, const Arg& arg, size_t lds = 0) {
     void* argv[] = {const_cast<Arg*>(&arg)};
-    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, 0, st) == hipSuccess
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, lds, st) == hipSuccess
                ? NOBLE_OK
                : NOBLE_ERR_HIP;
 }
