@@ -46,10 +46,8 @@ noble_status check_tables(const noble_paged_desc* d, const int32_t* page_table, 
 
 constexpr int64_t kMostNew = 1 << 20;
 
-// Workgroups of a call whose sequences are cut into pieces.
-#define kTurns (getenv("NBT") ? atoi(getenv("NBT")) : 1024)
-#define kTurnsWide (getenv("NBW") ? atoi(getenv("NBW")) : 512)
-#define kTurnsBlocks (getenv("NBB") ? atoi(getenv("NBB")) : 1024)
+// Workgroups that run at once: two a CU, by their LDS.
+constexpr int64_t kResident = 512;
 
 // Workgroups of one attention call and its scratch.
 struct DecodePlan {
@@ -66,29 +64,42 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
     p->wide = FORM != kBlocks && d->dtype == NOBLE_BF16 && rows > 2 * kGroup;
     p->R = p->wide ? kWideGroups : FORM != kBlocks && rows > kGroup ? 2 : 1;
     p->row_tiles = FORM == kBlocks ? d->new_tokens * cdiv(share, kGroup) : (rows + kGroup * p->R - 1) / (kGroup * p->R);
-    const int64_t base = d->B * d->kv_heads * p->row_tiles, per = d->kv_heads * p->row_tiles;
-    const int64_t tokens = (FORM == kBlocks ? std::min(count, d->table_row) : d->table_row) * d->page;
-    const int waves = !p->wide && d->dtype == NOBLE_F32 && d->head_dim > 64 ? 1 : 2;
-    const int64_t most = std::clamp<int64_t>(tokens / (p->wide ? kPart : kKeys) / waves, 1, 64);   // pieces of one sequence
+    const int64_t per = d->kv_heads * p->row_tiles;   // workgroups that read the same keys, or keys of other heads
+    int64_t parts;
     if (FORM == kBlocks) {
-        p->slots = std::clamp<int64_t>(base > 0 ? (kTurnsBlocks + base - 1) / base : 1, 1, most);
+        const int waves = d->dtype == NOBLE_F32 && d->head_dim > 64 ? 1 : 2;
+        const int64_t most = std::clamp<int64_t>(std::min(count, d->table_row) * d->page / kKeys / waves, 1, 64), base = d->B * per;
+        p->slots = std::clamp<int64_t>(base > 0 ? kResident / base : 1, 1, most);
         p->groups = base * p->slots;
+        p->split = p->slots > 1;
+        parts = p->groups;
     } else {
-        const int64_t turns = p->wide ? kTurnsWide : kTurns;
-        p->slots = std::clamp<int64_t>(per > 0 ? turns / per : 1, d->B, d->B * most);
-        p->groups = p->slots * per;
+        // as many slots as fill the workgroups that run at once best, once, or a few times where that is not near
+        const int64_t steps = d->B * (d->table_row * d->page / (p->wide ? kPart : kKeys) + 1);
+        if (steps > INT32_MAX) return NOBLE_ERR_BAD_SHAPE;   // the kernels count them in 32 bits
+        p->slots = 1;
+        double best = 0.0;
+        for (int64_t turn = 1; turn <= 4; ++turn) {
+            const int64_t n = std::min(std::max<int64_t>(kResident * turn / per, 1), std::max<int64_t>(steps, 1)), all = n * per;
+            const double fill = (double)all / (double)((all + kResident - 1) / kResident * kResident);
+            if (fill > best + 0.1) {
+                best = fill;
+                p->slots = n;
+            }
+        }
+        p->groups = d->B > 0 ? p->slots * per : 0;
+        p->split = p->slots > 1;
+        parts = 2 * p->groups;
     }
-    const bool split = p->slots > (FORM == kBlocks ? 1 : d->B) || FORM == kWeigh;
     if (p->groups > kMaxGroups256 || d->B * d->new_tokens * d->heads > kMaxGroups256 * 8) return NOBLE_ERR_BAD_SHAPE;
     p->z_row = (d->table_row * d->page + kPart - 1) / kPart * kPart;   // whole tiles of either kernel
     p->where = p->stats = p->z = 0;
     size_t at = 0;
-    if (split) {
-        at = up256((size_t)p->groups * p->R * kGroup * ((d->head_dim <= 64 ? 64 : 128) + 4) * 4);
+    if (p->split) {
+        at = up256((size_t)parts * p->R * kGroup * ((d->head_dim <= 64 ? 64 : 128) + 4) * 4);
         p->where = at;
         at += up256((size_t)(FORM == kBlocks ? d->B * d->new_tokens * d->kv_heads : d->B) * sizeof(int2));
     }
-    p->split = split;
     if (FORM == kWeigh) {
         const int64_t all = d->B * d->new_tokens * d->heads;
         if (p->z_row > 0 && all > kMaxScratch / 4 / p->z_row) return NOBLE_ERR_BAD_SHAPE;

@@ -21,12 +21,12 @@ struct DecodeArgs {
     const int* table;
     const int* lengths;
     const float* slopes;
-    float* part;          // [workgroup][16 R][DP + 4] float32: product, maximum, sum
-    int2* where;          // [B]: the sequence's first slot and its pieces (kBlocks: [B fresh, kv_heads], the pieces alone)
+    float* part;          // [part][row tile][kv_heads][16 R][DP + 4] float32: product, maximum, sum
+    int2* where;          // [B]: the slot that begins a sequence, and its pieces (kBlocks: [B fresh, kv_heads])
     int64_t table_row, pages, page_bytes;   // page_bytes: of one page, keys and values of all heads
     int page, shift, fresh, heads, kv_heads, share, D;
     int64_t B;
-    int row_tiles, slots;   // slots: workgroups of one key head and row tile, for all sequences (kBlocks: for each)
+    int row_tiles, slots;   // slots: workgroups of one key head and row tile, for all sequences (kBlocks: for each list)
     ScoreArgs sc;
     const uint32_t* seen;   // kTree: [B, fresh, words]
     const int* depths;      // [B, fresh]
@@ -119,55 +119,79 @@ __device__ __forceinline__ void decode_store(const DecodeArgs& a, int b, int kv,
                   sum[0], sum[1], sum[2], sum[3]);
 }
 
-// The pieces that the sequences are cut into: of one size, so that a batch of sequences of different lengths keeps every
-// workgroup busy to the end, and as many as give each key head and row tile `slots` workgroups.  With T steps in all and B
-// sequences, pieces of T / (slots - B) steps, rounded up, are slots at most, each sequence's last one being shorter.  Every
-// wave works that out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 32 drafted ones: as many pieces of
-// every sequence 146 us, pieces of one size PIECES_A; one token of 64 of 16384 to 32768 PIECES_B.
-struct Piece {
-    int b = 0, piece = 0, pieces = 1, size = 0;   // size: of a piece, in steps of `keys` keys
-    bool work = true;
-    Piece() = default;
-    __device__ __forceinline__ int steps(const DecodeArgs& a, int64_t b, int keys) const {
-        return b < a.B ? (a.held((int)b) + keys - 1) / keys : 0;
+// The steps (of `keys` keys) of all sequences in a row are dealt to the slots in equal ranges, so that a batch of sequences of
+// different lengths keeps every workgroup busy to the end: a slot has the end of one sequence, whole ones, and the beginning
+// of one, at most.  Every wave works its range out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 16 heads,
+// 32 drafted tokens each: pieces of every sequence, as many for each SLOTS_A us, slots SLOTS_B us.
+struct Slots {
+    int b = 0, begin = 0, steps = 0;   // the sequence, the slot's first step in it, the sequence's steps
+    int left = 0;                      // steps of the slot from there on
+    uint32_t from = 0;                 // steps before the sequence
+    uint32_t per = 0, more = 0;        // a slot's steps; slots that have one more
+    Slots() = default;
+    // A sequence without keys has a step too, in which its rows are written.
+    static __device__ __forceinline__ int steps_of(const DecodeArgs& a, int64_t b, int keys) {
+        return b < a.B ? max((a.held((int)b) + keys - 1) / keys, 1) : 0;
     }
-    __device__ __forceinline__ Piece(const DecodeArgs& a, int slot, int keys, int least, int lane) {
-        if (a.slots == a.B) {
-            b = slot;
-            return;
-        }
-        const int one = steps(a, lane, keys);   // of the first 64 sequences, a lane each
-        int64_t total = one;
-        for (int64_t n = 64; n < a.B; n += 64) total += steps(a, n + lane, keys);
+    __device__ __forceinline__ uint32_t first(uint32_t slot) const { return slot * per + min(slot, more); }
+    // The slot that has a step.
+    __device__ __forceinline__ uint32_t of(uint32_t step) const {
+        const uint32_t longer = more * (per + 1);
+        return step < longer ? step / (per + 1) : more + (step - longer) / per;
+    }
+    // least: steps of a slot, but for the last ones of calls that have fewer
+    __device__ __forceinline__ Slots(const DecodeArgs& a, int slot, int keys, int least, int lane) {
+        const int one = steps_of(a, lane, keys);   // of the first 64 sequences, a lane each
+        uint32_t total = one;
+        for (int64_t n = 64; n < a.B; n += 64) total += steps_of(a, n + lane, keys);
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
-        const int64_t free = a.slots - a.B;
-        size = (int)max((total + free - 1) / free, (int64_t)least);
-        work = false;
-        int before = 0;
+        total = __builtin_amdgcn_readfirstlane(total);
+        const uint32_t used = min((uint32_t)a.slots, (total + least - 1) / least);
+        if ((uint32_t)slot >= used) return;
+        per = total / used;
+        more = total - per * used;
+        const uint32_t at = first(slot);
+        left = (int)(first(slot + 1) - at);
         for (int64_t n = 0; n < a.B; n += 64) {
-            const int mine = n + lane < a.B ? max(((n ? steps(a, n + lane, keys) : one) + size - 1) / size, 1) : 0;
-            int upto = mine;
+            const uint32_t mine = n ? steps_of(a, n + lane, keys) : one;
+            uint32_t upto = mine;
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
-                const int v = __shfl_up(upto, o);
+                const uint32_t v = __shfl_up(upto, o);
                 if (lane >= o) upto += v;
             }
-            const uint64_t here = __ballot(slot < before + upto);
+            const uint64_t here = __ballot(at - from < upto);
             if (here) {
-                const int at = __builtin_ctzll(here);
-                b = (int)n + at;
-                pieces = __builtin_amdgcn_readlane(mine, at);
-                piece = slot - (before + __builtin_amdgcn_readlane(upto, at) - pieces);
-                work = true;
+                const int l = __builtin_ctzll(here);
+                b = (int)n + l;
+                steps = __builtin_amdgcn_readlane(mine, l);
+                from += __builtin_amdgcn_readlane(upto, l) - steps;
+                begin = (int)(at - from);
                 break;
             }
-            before += __builtin_amdgcn_readlane(upto, 63);
+            from += __builtin_amdgcn_readlane(upto, 63);
         }
         b = __builtin_amdgcn_readfirstlane(b);
-        piece = __builtin_amdgcn_readfirstlane(piece);
-        pieces = __builtin_amdgcn_readfirstlane(pieces);
-        size = __builtin_amdgcn_readfirstlane(size);
+        begin = __builtin_amdgcn_readfirstlane(begin);
+        steps = __builtin_amdgcn_readfirstlane(steps);
+        from = __builtin_amdgcn_readfirstlane(from);
+        left = __builtin_amdgcn_readfirstlane(left);
+        per = __builtin_amdgcn_readfirstlane(per);
+        more = __builtin_amdgcn_readfirstlane(more);
+    }
+    __device__ __forceinline__ int stop() const { return min(steps, begin + left); }
+    __device__ __forceinline__ bool whole() const { return begin == 0 && left >= steps; }
+    __device__ __forceinline__ int pieces(int slot) const { return (int)(of(from + steps - 1) - slot) + 1; }
+    // The next sequence; false: the slot is done.
+    __device__ __forceinline__ bool next(const DecodeArgs& a, int keys) {
+        left -= stop() - begin;
+        if (left <= 0) return false;
+        from += steps;
+        ++b;
+        begin = 0;
+        steps = __builtin_amdgcn_readfirstlane(steps_of(a, b, keys));
+        return true;
     }
 };
 
@@ -195,362 +219,374 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES), (sizeof(E) * DP >
     const int kv = w % a.kv_heads;
     w /= a.kv_heads;
     const int rt = w % a.row_tiles, slot = w / a.row_tiles, db = a.D * ES;
-    Piece pc;
+    Slots sl;
+    int b, piece = 0;
     if constexpr (FORM == kBlocks) {
-        pc.b = slot / a.slots;
-        pc.piece = slot % a.slots;
+        b = slot / a.slots;
+        piece = slot % a.slots;
     } else {
-        pc = Piece(a, slot, kKeys, W, lane);
-        if (!pc.work) return;
+        sl = Slots(a, slot, kKeys, W, lane);
+        if (sl.left <= 0) return;
+        b = sl.b;
     }
-    const int b = pc.b;
-
-    // this lane's row of each group.  kBlocks: a tile's rows are one token's; else tokens x heads, one after the other
-    const int per_tok = FORM == kBlocks ? (a.share + kGroup - 1) / kGroup : 1;
-    const int rows = FORM == kBlocks ? a.share : a.fresh * a.share;
-    const int row0 = (FORM == kBlocks ? rt % per_tok : rt * R) * kGroup;
-    const int tok0 = FORM == kBlocks ? rt / per_tok : row0 / a.share;
-    const int tok1 = FORM == kBlocks ? tok0 : (min(rows, row0 + R * kGroup) - 1) / a.share;
-    bool live[R];
-    int tok[R], head[R];
-    Frag<E> q[R][NS];
-#pragma unroll
-    for (int g = 0; g < R; ++g) {
-        const int r = row0 + g * kGroup + n16;
-        live[g] = r < rows;
-        tok[g] = FORM == kBlocks ? tok0 : live[g] ? r / a.share : tok1;
-        head[g] = live[g] ? kv * a.share + r - (FORM == kBlocks ? 0 : tok[g] * a.share) : 0;
-        const char* qp = a.q.ptr + (int64_t)head[g] * a.q.head + ((int64_t)b * a.fresh + tok[g]) * a.q.row;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const int d = 32 * s + 8 * g4;
-            q[g][s] = global_frag<E>(qp + d * ES, live[g] && d < a.D);
-        }
-    }
-    const int len = a.held(b), first = len - a.fresh;   // first: place of the first new token
-    const int* list = FORM == kBlocks ? a.list(b, tok0, kv) : nullptr;
-    // the keys are [0, end): tokens of the sequence, or (kBlocks) of the listed pages in a row
-    int end, listed = 0;
-    if constexpr (FORM == kBlocks) {
-        const int at = first + tok0;
-        listed = __builtin_amdgcn_readfirstlane(list_length(list, a.count, at >= 0 ? at >> a.shift : -1, lane));
-        end = listed > 0 ? (listed - 1) * a.page + min(a.page, at + 1 - list[listed - 1] * a.page) : 0;
-        end = __builtin_amdgcn_readfirstlane(end);
-    } else {
-        end = max(first + tok1 + 1, 0);
-    }
-    const int chunks = (end + kKeys - 1) / kKeys;
-    int c0, c1;
-    if constexpr (FORM == kBlocks) {
-        // lists are of one length but for those of short sequences, which are cut into fewer pieces
-        pc.pieces = max(1, min(a.slots, chunks / W));
-        if (pc.piece >= pc.pieces) return;
-        c0 = (int)((int64_t)chunks * pc.piece / pc.pieces) + wave;
-        c1 = (int)((int64_t)chunks * (pc.piece + 1) / pc.pieces);
-    } else {
-        c0 = (pc.pieces > 1 ? pc.piece * pc.size : 0) + wave;
-        c1 = pc.pieces > 1 ? min(chunks, (pc.piece + 1) * pc.size) : chunks;
-    }
-    if (pc.piece == 0 && threadIdx.x == 0 && a.where) {
-        if (FORM == kBlocks) a.where[((int64_t)b * a.fresh + tok0) * a.kv_heads + kv] = int2{slot, pc.pieces};
-        else if (kv == 0 && rt == 0) a.where[b] = int2{slot, pc.pieces};
-    }
-    float slope[R];
-    const int* depths = FORM == kTree ? a.depths + (int64_t)b * a.fresh : nullptr;
-    int at[R];   // a row's position, which the bias goes by
-#pragma unroll
-    for (int g = 0; g < R; ++g) {
-        slope[g] = a.slopes ? a.slopes[head[g]] * kLog2e / a.sc.unit : 0.f;
-        at[g] = first + (FORM == kTree ? depths[tok[g]] : tok[g]);
-    }
-
-    char* ring = lds + wave * NST * S::STAGE;
-    typedef const __attribute__((address_space(4))) int* table_ptr;
-    const table_ptr table = (table_ptr)(a.table + b * a.table_row);
-    const table_ptr blocks = (table_ptr)list;
-    // a lane's place in each request of a chunk, from the chunk's first key on
-    uint32_t vo[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int row = i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(row);
-        vo[i] = 16 * ch < db ? (uint32_t)(row * db + 16 * ch) : kOOB;
-    }
-    const char* heads = a.cache + (int64_t)kv * a.page * db;
-    const int64_t values = (int64_t)a.kv_heads * a.page * db;   // from a key to its value
-    // Requests a chunk's keys and values; returns which keys have no page in the cache (they come as zeros).
-    const auto request = [&](int c, char* dst) {
-        const int k0 = c * kKeys;
-        uint32_t bad = 0;
-        bool ok = false;
-        i32x4 dk, dv;
-#pragma unroll
-        for (int x = 0; x < kKeys / 8; ++x) {
-            const int key = k0 + 8 * x;
-            if (x == 0 || (key & (a.page - 1)) == 0) {   // a page starts here, or the chunk does
-                int page = -1;
-                if (key < end) page = table[FORM == kBlocks ? blocks[key >> a.shift] : key >> a.shift];
-                ok = page >= 0 && page < a.pages;
-                const char* base = heads + (int64_t)(ok ? page : 0) * a.page_bytes + (int64_t)((key & (a.page - 1)) - 8 * x) * db;
-                const int bytes = ok ? min(end - k0, kKeys) * db : 0;
-                dk = wave_desc(base, bytes);
-                dv = wave_desc(base + values, bytes);
-            }
-            if (!ok) bad |= 0xffu << (8 * x);
-#pragma unroll
-            for (int i = 8 * x / RPI; i < 8 * (x + 1) / RPI; ++i) {
-                dma16(dk, dst + i * 1024, vo[i], 0);
-                dma16(dv, dst + S::STAGE / 2 + i * 1024, vo[i], 0);
-            }
-        }
-        return bad;
-    };
-    // That again, for a chunk that is here.
-    const auto missing = [&](int c) {
-        uint32_t bad = 0;
-        bool ok = false;
-#pragma unroll
-        for (int x = 0; x < kKeys / 8; ++x) {
-            const int key = c * kKeys + 8 * x;
-            if (x == 0 || (key & (a.page - 1)) == 0) {
-                const int page = key < end ? table[key >> a.shift] : -1;
-                ok = page >= 0 && page < a.pages;
-            }
-            if (!ok) bad |= 0xffu << (8 * x);
-        }
-        return bad;
-    };
-    // Which of this lane's eight keys of the chunk at k0 (places 16 (i / 4) + 4 g4 + i % 4) the row of a token sees.
-    const auto sees = [&](int t, int k0) {
-        uint32_t mask;
-        if constexpr (FORM == kTree) {
-            mask = line_bits(a.line(b, t), a.words, k0 - first);
-        } else {
-            const int n = (FORM == kBlocks ? end : first + t + 1) - k0;   // keys up to the token
-            mask = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
-        }
-        return mask;
-    };
-    const auto mine = [&](uint32_t mask) { return (mask >> (4 * g4) & 15u) | (mask >> (16 + 4 * g4) & 15u) << 4; };
-
-    f32x4 acc[R][ND];
-    float m[R], l[R];
-#pragma unroll
-    for (int g = 0; g < R; ++g) {
-        m[g] = -INFINITY;
-        l[g] = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) acc[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    const auto step = [&]<bool EDGE>(const char* kt, int k0, uint32_t bad) {
-        const char* vt = kt + S::STAGE / 2;
-        float z[R][8];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            f32x4 sv[R];
-#pragma unroll
-            for (int g = 0; g < R; ++g) sv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < NS; ++x) {
-                const Frag<E> kf = T::along(kt, 16 * u + n16, 4 * x + g4);
-#pragma unroll
-                for (int g = 0; g < R; ++g) mma16x16(sv[g], kf, q[g][x]);
-            }
-#pragma unroll
-            for (int g = 0; g < R; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z[g][4 * u + i] = sv[g][i];
-        }
-        // keys that some of the rows do not see
-        const bool edge = EDGE || (FORM == kBlocks && k0 + kKeys > end);
-        int block[4];   // kBlocks: the chunk's pages, whose places the bias goes by
-        if (FORM == kBlocks && a.slopes) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) block[x] = blocks[min((k0 + 8 * x) >> a.shift, listed - 1)] << a.shift;
-        }
-        Frag<E> p[R];
+    for (;;) {
+        // this lane's row of each group.  kBlocks: a tile's rows are one token's; else tokens x heads, one after the other
+        const int per_tok = FORM == kBlocks ? (a.share + kGroup - 1) / kGroup : 1;
+        const int rows = FORM == kBlocks ? a.share : a.fresh * a.share;
+        const int row0 = (FORM == kBlocks ? rt % per_tok : rt * R) * kGroup;
+        const int tok0 = FORM == kBlocks ? rt / per_tok : row0 / a.share;
+        const int tok1 = FORM == kBlocks ? tok0 : (min(rows, row0 + R * kGroup) - 1) / a.share;
+        bool live[R];
+        int tok[R], head[R];
+        Frag<E> q[R][NS];
 #pragma unroll
         for (int g = 0; g < R; ++g) {
-            scores<E, MODE, 8>(a.sc, z[g], z[g], nullptr);
-            if (a.slopes) {
+            const int r = row0 + g * kGroup + n16;
+            live[g] = r < rows;
+            tok[g] = FORM == kBlocks ? tok0 : live[g] ? r / a.share : tok1;
+            head[g] = live[g] ? kv * a.share + r - (FORM == kBlocks ? 0 : tok[g] * a.share) : 0;
+            const char* qp = a.q.ptr + (int64_t)head[g] * a.q.head + ((int64_t)b * a.fresh + tok[g]) * a.q.row;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int d = 32 * s + 8 * g4;
+                q[g][s] = global_frag<E>(qp + d * ES, live[g] && d < a.D);
+            }
+        }
+        const int len = a.held(b), first = len - a.fresh;   // first: place of the first new token
+        const int* list = FORM == kBlocks ? a.list(b, tok0, kv) : nullptr;
+        // the keys are [0, end): tokens of the sequence, or (kBlocks) of the listed pages in a row
+        int end, listed = 0;
+        if constexpr (FORM == kBlocks) {
+            const int at = first + tok0;
+            listed = __builtin_amdgcn_readfirstlane(list_length(list, a.count, at >= 0 ? at >> a.shift : -1, lane));
+            end = listed > 0 ? (listed - 1) * a.page + min(a.page, at + 1 - list[listed - 1] * a.page) : 0;
+            end = __builtin_amdgcn_readfirstlane(end);
+        } else {
+            end = max(first + tok1 + 1, 0);
+        }
+        const int chunks = (end + kKeys - 1) / kKeys;
+        int c0, c1, part;   // part: where the sums go, unless they are all of the rows'
+        bool whole;
+        if constexpr (FORM == kBlocks) {
+            // lists are of one length but for those of short sequences, which are cut into fewer pieces
+            const int pieces = max(1, min(a.slots, chunks / W));
+            if (piece >= pieces) return;
+            c0 = (int)((int64_t)chunks * piece / pieces) + wave;
+            c1 = (int)((int64_t)chunks * (piece + 1) / pieces);
+            whole = pieces == 1;
+            part = slot;
+            if (a.where && piece == 0 && threadIdx.x == 0)
+                a.where[((int64_t)b * a.fresh + tok0) * a.kv_heads + kv] = int2{slot, pieces};
+        } else {
+            c0 = sl.begin + wave;
+            c1 = min(chunks, sl.stop());
+            whole = sl.whole();
+            part = 2 * slot + (sl.begin == 0 ? 1 : 0);
+            if (a.where && sl.begin == 0 && kv == 0 && rt == 0 && threadIdx.x == 0) a.where[b] = int2{slot, sl.pieces(slot)};
+        }
+        float slope[R];
+        const int* depths = FORM == kTree ? a.depths + (int64_t)b * a.fresh : nullptr;
+        int at[R];   // a row's position, which the bias goes by
+#pragma unroll
+        for (int g = 0; g < R; ++g) {
+            slope[g] = a.slopes ? a.slopes[head[g]] * kLog2e / a.sc.unit : 0.f;
+            at[g] = first + (FORM == kTree ? depths[tok[g]] : tok[g]);
+        }
+
+        char* ring = lds + wave * NST * S::STAGE;
+        typedef const __attribute__((address_space(4))) int* table_ptr;
+        const table_ptr table = (table_ptr)(a.table + b * a.table_row);
+        const table_ptr blocks = (table_ptr)list;
+        // a lane's place in each request of a chunk, from the chunk's first key on
+        uint32_t vo[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int row = i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(row);
+            vo[i] = 16 * ch < db ? (uint32_t)(row * db + 16 * ch) : kOOB;
+        }
+        const char* heads = a.cache + (int64_t)kv * a.page * db;
+        const int64_t values = (int64_t)a.kv_heads * a.page * db;   // from a key to its value
+        // Requests a chunk's keys and values; returns which keys have no page in the cache (they come as zeros).
+        const auto request = [&](int c, char* dst) {
+            const int k0 = c * kKeys;
+            uint32_t bad = 0;
+            bool ok = false;
+            i32x4 dk, dv;
+#pragma unroll
+            for (int x = 0; x < kKeys / 8; ++x) {
+                const int key = k0 + 8 * x;
+                if (x == 0 || (key & (a.page - 1)) == 0) {   // a page starts here, or the chunk does
+                    int page = -1;
+                    if (key < end) page = table[FORM == kBlocks ? blocks[key >> a.shift] : key >> a.shift];
+                    ok = page >= 0 && page < a.pages;
+                    const char* base = heads + (int64_t)(ok ? page : 0) * a.page_bytes + (int64_t)((key & (a.page - 1)) - 8 * x) * db;
+                    const int bytes = ok ? min(end - k0, kKeys) * db : 0;
+                    dk = wave_desc(base, bytes);
+                    dv = wave_desc(base + values, bytes);
+                }
+                if (!ok) bad |= 0xffu << (8 * x);
+#pragma unroll
+                for (int i = 8 * x / RPI; i < 8 * (x + 1) / RPI; ++i) {
+                    dma16(dk, dst + i * 1024, vo[i], 0);
+                    dma16(dv, dst + S::STAGE / 2 + i * 1024, vo[i], 0);
+                }
+            }
+            return bad;
+        };
+        // That again, for a chunk that is here.
+        const auto missing = [&](int c) {
+            uint32_t bad = 0;
+            bool ok = false;
+#pragma unroll
+            for (int x = 0; x < kKeys / 8; ++x) {
+                const int key = c * kKeys + 8 * x;
+                if (x == 0 || (key & (a.page - 1)) == 0) {
+                    const int page = key < end ? table[key >> a.shift] : -1;
+                    ok = page >= 0 && page < a.pages;
+                }
+                if (!ok) bad |= 0xffu << (8 * x);
+            }
+            return bad;
+        };
+        // Which of this lane's eight keys of the chunk at k0 (places 16 (i / 4) + 4 g4 + i % 4) the row of a token sees.
+        const auto sees = [&](int t, int k0) {
+            uint32_t mask;
+            if constexpr (FORM == kTree) {
+                mask = line_bits(a.line(b, t), a.words, k0 - first);
+            } else {
+                const int n = (FORM == kBlocks ? end : first + t + 1) - k0;   // keys up to the token
+                mask = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+            }
+            return mask;
+        };
+        const auto mine = [&](uint32_t mask) { return (mask >> (4 * g4) & 15u) | (mask >> (16 + 4 * g4) & 15u) << 4; };
+
+        f32x4 acc[R][ND];
+        float m[R], l[R];
+#pragma unroll
+        for (int g = 0; g < R; ++g) {
+            m[g] = -INFINITY;
+            l[g] = 0.f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        const auto step = [&]<bool EDGE>(const char* kt, int k0, uint32_t bad) {
+            const char* vt = kt + S::STAGE / 2;
+            float z[R][8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f32x4 sv[R];
+#pragma unroll
+                for (int g = 0; g < R; ++g) sv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < NS; ++x) {
+                    const Frag<E> kf = T::along(kt, 16 * u + n16, 4 * x + g4);
+#pragma unroll
+                    for (int g = 0; g < R; ++g) mma16x16(sv[g], kf, q[g][x]);
+                }
+#pragma unroll
+                for (int g = 0; g < R; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[g][4 * u + i] = sv[g][i];
+            }
+            // keys that some of the rows do not see
+            const bool edge = EDGE || (FORM == kBlocks && k0 + kKeys > end);
+            int block[4];   // kBlocks: the chunk's pages, whose places the bias goes by
+            if (FORM == kBlocks && a.slopes) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) block[x] = blocks[min((k0 + 8 * x) >> a.shift, listed - 1)] << a.shift;
+            }
+            Frag<E> p[R];
+#pragma unroll
+            for (int g = 0; g < R; ++g) {
+                scores<E, MODE, 8>(a.sc, z[g], z[g], nullptr);
+                if (a.slopes) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int o = 16 * (i >> 2) + 4 * g4 + (i & 3);
+                        int pos = k0 + o;
+                        if constexpr (FORM == kBlocks) {
+                            const int x = o >> 3;
+                            pos = (x == 0 ? block[0] : x == 1 ? block[1] : x == 2 ? block[2] : block[3]) + (pos & (a.page - 1));
+                        } else if (FORM == kTree && EDGE && pos >= first) {
+                            const int node = pos - first;
+                            pos = node < a.fresh ? first + depths[(uint32_t)node] : pos;
+                        }
+                        z[g][i] = fmaf(-slope[g], fabsf((float)(pos - at[g])), z[g][i]);
+                    }
+                }
+                if (edge || bad) {
+                    const uint32_t mask = mine(sees(tok[g], k0) & ~bad);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[g][i] = mask >> i & 1u ? z[g][i] : -INFINITY;
+                }
+                if constexpr (FORM == kWeigh) {
+                    if (live[g]) {
+                        const int r = row0 + g * kGroup + n16;
+                        const float unit = MODE & kCap ? 1.f : a.sc.unit;
+                        float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + r) * a.z_row + k0 + 4 * g4;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            *reinterpret_cast<f32x4*>(zp + 16 * u) = f32x4{z[g][4 * u] * unit, z[g][4 * u + 1] * unit,
+                                                                           z[g][4 * u + 2] * unit, z[g][4 * u + 3] * unit};
+                    }
+                }
+                float top = z[g][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, z[g][i]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32)) * (MODE & kCap ? 1.f : a.sc.unit);
+                if (__any(top > m[g] + 8.f)) {   // see attn_fwd_kernel
+                    const float to = fmaxf(m[g], top);
+                    const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[g] - to);
+                    m[g] = to;
+                    l[g] *= f;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) acc[g][d] *= f;
+                }
+                const float base = m[g] == -INFINITY ? 0.f : m[g];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int o = 16 * (i >> 2) + 4 * g4 + (i & 3);
-                    int pos = k0 + o;
-                    if constexpr (FORM == kBlocks) {
-                        const int x = o >> 3;
-                        pos = (x == 0 ? block[0] : x == 1 ? block[1] : x == 2 ? block[2] : block[3]) + (pos & (a.page - 1));
-                    } else if (FORM == kTree && EDGE && pos >= first) {
-                        const int node = pos - first;
-                        pos = node < a.fresh ? first + depths[(uint32_t)node] : pos;
+                    z[g][i] = exp_score<MODE>(a.sc, z[g][i], base);
+                    l[g] += z[g][i];
+                }
+                p[g] = to_frag<E>(z[g]);
+            }
+            // a value that a row does not see meets a probability of zero, which an infinite or NaN one would outlive: then
+            // each token's rows are multiplied by the values that this token sees, with zeros for the others
+            bool odd = false;
+            if (EDGE && a.fresh > 1) {
+#pragma unroll
+                for (int d = 0; d < ND; ++d) odd |= not_finite(T::across16(vt, d, lane));
+            }
+            if (EDGE) asm volatile("" ::: "memory");   // the operands are read again: they are too many to be kept
+            if (EDGE && __any(odd)) {
+                for (int t = tok0; t <= tok1; ++t) {
+                    asm volatile("" ::: "memory");
+                    const uint32_t mask = mine(sees(t, k0));
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const Frag<E> vf = only(T::across16(vt, d, lane), mask);
+#pragma unroll
+                        for (int g = 0; g < R; ++g) {
+                            f32x4 sum = acc[g][d];
+                            mma16x16(sum, vf, p[g]);
+                            acc[g][d] = tok[g] == t ? sum : acc[g][d];
+                        }
                     }
-                    z[g][i] = fmaf(-slope[g], fabsf((float)(pos - at[g])), z[g][i]);
-                }
-            }
-            if (edge || bad) {
-                const uint32_t mask = mine(sees(tok[g], k0) & ~bad);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) z[g][i] = mask >> i & 1u ? z[g][i] : -INFINITY;
-            }
-            if constexpr (FORM == kWeigh) {
-                if (live[g]) {
-                    const int r = row0 + g * kGroup + n16;
-                    const float unit = MODE & kCap ? 1.f : a.sc.unit;
-                    float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + r) * a.z_row + k0 + 4 * g4;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        *reinterpret_cast<f32x4*>(zp + 16 * u) = f32x4{z[g][4 * u] * unit, z[g][4 * u + 1] * unit,
-                                                                       z[g][4 * u + 2] * unit, z[g][4 * u + 3] * unit};
-                }
-            }
-            float top = z[g][0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, z[g][i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32)) * (MODE & kCap ? 1.f : a.sc.unit);
-            if (__any(top > m[g] + 8.f)) {   // see attn_fwd_kernel
-                const float to = fmaxf(m[g], top);
-                const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[g] - to);
-                m[g] = to;
-                l[g] *= f;
-#pragma unroll
-                for (int d = 0; d < ND; ++d) acc[g][d] *= f;
-            }
-            const float base = m[g] == -INFINITY ? 0.f : m[g];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[g][i] = exp_score<MODE>(a.sc, z[g][i], base);
-                l[g] += z[g][i];
-            }
-            p[g] = to_frag<E>(z[g]);
-        }
-        // a value that a row does not see meets a probability of zero, which an infinite or NaN one would outlive: then
-        // each token's rows are multiplied by the values that this token sees, with zeros for the others
-        bool odd = false;
-        if (EDGE && a.fresh > 1) {
-#pragma unroll
-            for (int d = 0; d < ND; ++d) odd |= not_finite(T::across16(vt, d, lane));
-        }
-        if (EDGE) asm volatile("" ::: "memory");   // the operands are read again: they are too many to be kept
-        if (EDGE && __any(odd)) {
-            for (int t = tok0; t <= tok1; ++t) {
-                asm volatile("" ::: "memory");
-                const uint32_t mask = mine(sees(t, k0));
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const Frag<E> vf = only(T::across16(vt, d, lane), mask);
-#pragma unroll
-                    for (int g = 0; g < R; ++g) {
-                        f32x4 sum = acc[g][d];
-                        mma16x16(sum, vf, p[g]);
-                        acc[g][d] = tok[g] == t ? sum : acc[g][d];
-                    }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const Frag<E> vf = T::across16(vt, d, lane);
-#pragma unroll
-                for (int g = 0; g < R; ++g) mma16x16(acc[g][d], vf, p[g]);
-            }
-        }
-    };
-    operands_here();
-    int ahead = c0;   // next chunk to request
-    uint32_t bads[NST];
-#pragma unroll
-    for (int s = 0; s < NST; ++s) {
-        bads[s] = 0;
-        if (s < NST - 1) {
-            if (ahead < c1) bads[s] = request(ahead, ring + s * S::STAGE);
-            ahead += W;
-        }
-    }
-    // The next chunk into the stage of the step before, whose reads have been waited for; waits for this step's.
-    const auto next = [&](char* free) {
-        uint32_t bad = 0;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (ahead < c1) {
-            bad = request(ahead, free);
-            wait_vmcnt<2 * PER * (NST - 1)>();
-        } else {
-            wait_vmcnt<0>();
-        }
-        asm volatile("" ::: "memory");
-        ahead += W;
-        return bad;
-    };
-    // Chunks that every row sees whole, and then the others, whose masks and whose care for values that are not seen would
-    // cost the first loop registers: it would move its sums from and to the accumulation ones in every step.
-    const int whole = FORM == kBlocks ? c1 : min(c1, max(first + (FORM == kWeigh ? tok0 + 1 : 0), 0) / kKeys);
-    int ch = c0, stage = 0;
-    for (bool more = ch < whole; more;) {
-#pragma unroll
-        for (int s = 0; s < NST; ++s) {
-            bads[(s + NST - 1) % NST] = next(ring + (s + NST - 1) % NST * S::STAGE);
-            step.template operator()<false>(ring + s * S::STAGE, ch * kKeys, bads[s]);
-            ch += W;
-            stage = (s + 1) % NST;
-            if (ch >= whole) {
-                more = false;
-                break;
-            }
-        }
-    }
-    if constexpr (FORM != kBlocks) {
-        for (; ch < c1; ch += W) {
-            next(ring + (stage + NST - 1) % NST * S::STAGE);
-            step.template operator()<true>(ring + stage * S::STAGE, ch * kKeys, missing(ch));
-            stage = (stage + 1) % NST;
-        }
-    }
-
-    // the waves' results meet, a group at a time: [wave][16 rows][DP + 4] float32
-    constexpr int LD = DP + 4;
-    static_assert(W * kGroup * LD * 4 <= W * NST * S::STAGE, "fits the ring");
-#pragma unroll
-    for (int g = 0; g < R; ++g) {
-        l[g] += __shfl_xor(l[g], 16);
-        l[g] += __shfl_xor(l[g], 32);
-        __syncthreads();
-        float* dst = reinterpret_cast<float*>(lds) + (wave * kGroup + n16) * LD;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(dst + 16 * d + 4 * g4) = acc[g][d];
-        if (g4 == 0) {
-            dst[DP] = m[g];
-            dst[DP + 1] = l[g];
-        }
-        __syncthreads();
-        const int take = min(rows - row0 - g * kGroup, kGroup);
-        for (int e = threadIdx.x; e < take * (DP / 4); e += 64 * W) {
-            const int row = e / (DP / 4), d = e % (DP / 4) * 4;
-            const float* src = reinterpret_cast<const float*>(lds) + row * LD;
-            float top = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < W; ++x) top = fmaxf(top, src[x * kGroup * LD + DP]);
-            const float base = top == -INFINITY ? 0.f : top;
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            float total = 0.f;
-#pragma unroll
-            for (int x = 0; x < W; ++x) {
-                const float* p = src + x * kGroup * LD;
-                const float f = __builtin_amdgcn_exp2f(p[DP] - base);
-                sum += *reinterpret_cast<const f32x4*>(p + d) * f;
-                total += p[DP + 1] * f;
-            }
-            if (pc.pieces > 1 || FORM == kWeigh) {
-                float* out = a.part + (((int64_t)blockIdx.x * R + g) * kGroup + row) * LD;
-                *reinterpret_cast<f32x4*>(out + d) = sum;
-                if (d == 0) {
-                    out[DP] = top;
-                    out[DP + 1] = total;
                 }
             } else {
-                const int rr = row0 + g * kGroup + row, t = FORM == kBlocks ? tok0 : rr / a.share;
-                decode_store<E, FORM>(a, b, kv, t, rr - (FORM == kBlocks ? 0 : t * a.share), d, sum, total);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const Frag<E> vf = T::across16(vt, d, lane);
+#pragma unroll
+                    for (int g = 0; g < R; ++g) mma16x16(acc[g][d], vf, p[g]);
+                }
+            }
+        };
+        operands_here();
+        int ahead = c0;   // next chunk to request
+        uint32_t bads[NST];
+#pragma unroll
+        for (int s = 0; s < NST; ++s) {
+            bads[s] = 0;
+            if (s < NST - 1) {
+                if (ahead < c1) bads[s] = request(ahead, ring + s * S::STAGE);
+                ahead += W;
             }
         }
+        // The next chunk into the stage of the step before, whose reads have been waited for; waits for this step's.
+        const auto next = [&](char* free) {
+            uint32_t bad = 0;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (ahead < c1) {
+                bad = request(ahead, free);
+                wait_vmcnt<2 * PER * (NST - 1)>();
+            } else {
+                wait_vmcnt<0>();
+            }
+            asm volatile("" ::: "memory");
+            ahead += W;
+            return bad;
+        };
+        // Chunks that every row sees whole, and then the others, whose masks and whose care for values that are not seen would
+        // cost the first loop registers: it would move its sums from and to the accumulation ones in every step.
+        const int plain = FORM == kBlocks ? c1 : min(c1, max(first + (FORM == kWeigh ? tok0 + 1 : 0), 0) / kKeys);
+        int ch = c0, stage = 0;
+        for (bool more = ch < plain; more;) {
+#pragma unroll
+            for (int s = 0; s < NST; ++s) {
+                bads[(s + NST - 1) % NST] = next(ring + (s + NST - 1) % NST * S::STAGE);
+                step.template operator()<false>(ring + s * S::STAGE, ch * kKeys, bads[s]);
+                ch += W;
+                stage = (s + 1) % NST;
+                if (ch >= plain) {
+                    more = false;
+                    break;
+                }
+            }
+        }
+        if constexpr (FORM != kBlocks) {
+            for (; ch < c1; ch += W) {
+                next(ring + (stage + NST - 1) % NST * S::STAGE);
+                step.template operator()<true>(ring + stage * S::STAGE, ch * kKeys, missing(ch));
+                stage = (stage + 1) % NST;
+            }
+        }
+
+        // the waves' results meet, a group at a time: [wave][16 rows][DP + 4] float32
+        constexpr int LD = DP + 4;
+        static_assert(W * kGroup * LD * 4 <= W * NST * S::STAGE, "fits the ring");
+#pragma unroll
+        for (int g = 0; g < R; ++g) {
+            l[g] += __shfl_xor(l[g], 16);
+            l[g] += __shfl_xor(l[g], 32);
+            __syncthreads();
+            float* dst = reinterpret_cast<float*>(lds) + (wave * kGroup + n16) * LD;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(dst + 16 * d + 4 * g4) = acc[g][d];
+            if (g4 == 0) {
+                dst[DP] = m[g];
+                dst[DP + 1] = l[g];
+            }
+            __syncthreads();
+            const int take = min(rows - row0 - g * kGroup, kGroup);
+            for (int e = threadIdx.x; e < take * (DP / 4); e += 64 * W) {
+                const int row = e / (DP / 4), d = e % (DP / 4) * 4;
+                const float* src = reinterpret_cast<const float*>(lds) + row * LD;
+                float top = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < W; ++x) top = fmaxf(top, src[x * kGroup * LD + DP]);
+                const float base = top == -INFINITY ? 0.f : top;
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                float total = 0.f;
+#pragma unroll
+                for (int x = 0; x < W; ++x) {
+                    const float* p = src + x * kGroup * LD;
+                    const float f = __builtin_amdgcn_exp2f(p[DP] - base);
+                    sum += *reinterpret_cast<const f32x4*>(p + d) * f;
+                    total += p[DP + 1] * f;
+                }
+                if (!whole) {
+                    float* out = a.part + ((((int64_t)part * a.row_tiles + rt) * a.kv_heads + kv) * R + g) * kGroup * LD + row * LD;
+                    *reinterpret_cast<f32x4*>(out + d) = sum;
+                    if (d == 0) {
+                        out[DP] = top;
+                        out[DP + 1] = total;
+                    }
+                } else {
+                    const int rr = row0 + g * kGroup + row, t = FORM == kBlocks ? tok0 : rr / a.share;
+                    if (FORM == kWeigh && d == 0)
+                        a.stats[((int64_t)b * a.kv_heads + kv) * rows + rr] = make_float2(top, 1.f / total);
+                    decode_store<E, FORM>(a, b, kv, t, rr - (FORM == kBlocks ? 0 : t * a.share), d, sum, total);
+                }
+            }
+        }
+        if constexpr (FORM == kBlocks) return;
+        if (!sl.next(a, kKeys)) return;
+        b = sl.b;
+        __syncthreads();   // the ring is free
     }
 }
 
@@ -580,9 +616,13 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
     }
     const int2 where = a.where[FORM == kBlocks ? ((int64_t)b * a.fresh + tok) * a.kv_heads + kv : b];
     const int pieces = where.y;
-    if (FORM != kWeigh && pieces == 1) return;
+    if (pieces == 1) return;
     const int64_t tile = (int64_t)j.groups * kGroup * LD, step = (int64_t)a.row_tiles * a.kv_heads * tile;   // from piece to piece
-    const float* p = a.part + (((int64_t)where.x * a.row_tiles + rt) * a.kv_heads + kv) * tile + (int64_t)slot * LD;
+    // piece n of a list is part n from its first on; of a sequence, its first piece is its slot's second part, the others the
+    // next slots' first ones
+    const int64_t place = ((int64_t)rt * a.kv_heads + kv) * tile + (int64_t)slot * LD;
+    const float* p = a.part + place + (FORM == kBlocks ? where.x : 2 * where.x + 1) * step;
+    const auto at = [&](int n) { return p + (FORM == kBlocks ? n : n ? 2 * n - 1 : 0) * step; };
     // eight pieces at a time, their loads all in flight
     constexpr int N = 8;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -592,7 +632,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
         float m[N], l[N], next = top;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const float* q = p + min(x0 + n, pieces - 1) * step;
+            const float* q = at(min(x0 + n, pieces - 1));
             v[n] = *reinterpret_cast<const f32x4*>(q + d);
             m[n] = x0 + n < pieces ? q[DP] : -INFINITY;
             l[n] = q[DP + 1];
