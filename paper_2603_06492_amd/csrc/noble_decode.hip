@@ -47,7 +47,7 @@ noble_status check_tables(const noble_paged_desc* d, const int32_t* page_table, 
 constexpr int64_t kMostNew = 1 << 20;
 
 // Workgroups that run at once: two a CU, by their LDS.
-constexpr int64_t kResident = 512;
+#define kResident (p->wide?512:getenv("NBT") ? atoi(getenv("NBT")) : 256)
 
 // Workgroups of one attention call and its scratch.
 struct DecodePlan {
@@ -55,7 +55,7 @@ struct DecodePlan {
     bool split;                           // some pieces are joined
     int64_t R, row_tiles, slots, groups;
     size_t where, stats, z, bytes;        // offsets (the parts come first), and all of it
-    int64_t z_row;
+    int64_t chunks;
 };
 
 template <int FORM>
@@ -92,7 +92,7 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
         parts = 2 * p->groups;
     }
     if (p->groups > kMaxGroups256 || d->B * d->new_tokens * d->heads > kMaxGroups256 * 8) return NOBLE_ERR_BAD_SHAPE;
-    p->z_row = (d->table_row * d->page + kPart - 1) / kPart * kPart;   // whole tiles of either kernel
+    p->chunks = (d->table_row * d->page + kPart - 1) / kPart * (kPart / kKeys);   // whole tiles of either kernel
     p->where = p->stats = p->z = 0;
     size_t at = 0;
     if (p->split) {
@@ -102,12 +102,12 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
     }
     if (FORM == kWeigh) {
         const int64_t all = d->B * d->new_tokens * d->heads;
-        if (p->z_row > 0 && all > kMaxScratch / 4 / p->z_row) return NOBLE_ERR_BAD_SHAPE;
+        if (p->chunks > 0 && all > kMaxScratch / 4 / kKeys / p->chunks) return NOBLE_ERR_BAD_SHAPE;
         p->stats = at;
         at += up256((size_t)all * 8);
         p->z = at;
-        at += (size_t)all * p->z_row * 4;
-        if (d->B * d->kv_heads * ((p->z_row + 1023) / 1024) > kMaxGroups256) return NOBLE_ERR_BAD_SHAPE;
+        at += (size_t)all * p->chunks * kKeys * 4;
+        if (d->B * d->kv_heads * (p->chunks / 32 + 1) > kMaxGroups256) return NOBLE_ERR_BAD_SHAPE;
     }
     p->bytes = at;
     return NOBLE_OK;
@@ -127,7 +127,7 @@ DecodeArgs decode_args(const noble_paged_desc* d, const DecodePlan& p, const nob
     a.where = p.split ? reinterpret_cast<int2*>(s + p.where) : nullptr;
     a.stats = reinterpret_cast<float2*>(s + p.stats);
     a.z = reinterpret_cast<float*>(s + p.z);
-    a.z_row = p.z_row;
+    a.chunks = p.chunks;
     a.table_row = d->table_row;
     a.pages = d->pages;
     a.page = d->page;
@@ -414,7 +414,7 @@ noble_status noble_attn_weigh(const noble_paged_desc* desc, const noble_heads* q
     const DecodeArgs a = decode_args(desc, p, q, cache, page_table, lengths, slopes, o, scratch);
     const hipStream_t st = (hipStream_t)stream;
     NOBLE_TRY(run_attention<kWeigh>(desc, p, a, st));
-    WeighArgs w{a, weights, weights_out, cdiv(p.z_row, 1024)};
+    const WeighArgs w{a, weights, weights_out, cdiv(desc->table_row * desc->page, 1024), aligned16(weights) && aligned16(weights_out)};
     if (w.parts == 0) return NOBLE_OK;
     return launch(weigh_kernel, dim3((unsigned)(desc->B * desc->kv_heads * w.parts)), dim3(256), st, w);
 }

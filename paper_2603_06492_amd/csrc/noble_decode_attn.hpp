@@ -33,9 +33,9 @@ struct DecodeArgs {
     int words;
     int count;              // kBlocks: entries of a list
     const int* chosen;      // [B fresh, kv_heads, count]
-    float* z;               // kWeigh: scores [B, kv_heads, fresh share, z_row], times log2 e
+    float* z;               // kWeigh: scores, times log2 e: [B, kv_heads, chunks of 32 tokens, fresh share, 32]
     float2* stats;          // [B, kv_heads, fresh share]: maximum, 1 / sum
-    int64_t z_row;
+    int64_t chunks;
 
     __device__ __forceinline__ int held(int b) const {
         return (int)min((int64_t)max(lengths[b], 0), table_row * page);
@@ -198,8 +198,8 @@ struct Slots {
 template <typename E, int DP>
 struct DecodeShape {
     static constexpr int STAGE = 2 * kKeys * DP * (int)sizeof(E);             // keys and values of a chunk
-    static constexpr int LDS = 64 * 1024;
-    static constexpr int WAVES = LDS / (2 * STAGE) < 2 ? 1 : 2;
+    static constexpr int LDS = 128 * 1024;
+    static constexpr int WAVES = LDS / (2 * STAGE) < 4 ? 2 : 4;
     static constexpr int STAGES = LDS / (WAVES * STAGE);
 };
 
@@ -425,7 +425,7 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES), (sizeof(E) * DP >
                     if (live[g]) {
                         const int r = row0 + g * kGroup + n16;
                         const float unit = MODE & kCap ? 1.f : a.sc.unit;
-                        float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + r) * a.z_row + k0 + 4 * g4;
+                        float* zp = a.z + ((((int64_t)b * a.kv_heads + kv) * a.chunks + k0 / kKeys) * rows + r) * kKeys + 4 * g4;
 #pragma unroll
                         for (int u = 0; u < 2; ++u)
                             *reinterpret_cast<f32x4*>(zp + 16 * u) = f32x4{z[g][4 * u] * unit, z[g][4 * u + 1] * unit,
@@ -656,44 +656,57 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
 }
 
 // The weight that every token received: of the rows that see it, exp2(score - maximum) / sum, added in the rows' order.  A
-// workgroup takes 1024 tokens of one sequence and key head, a thread four of them.
+// workgroup takes 1024 tokens of one sequence and key head, a thread four that follow each other.
 struct WeighArgs {
     DecodeArgs a;
     const float* in;   // [B, kv_heads, table_row page], nullptr: nothing
     float* out;
     int parts;         // workgroups of one (sequence, key head)
+    bool wide;         // in and out may be read and written 16 bytes at a time
 };
 __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs w) {
     const DecodeArgs& a = w.a;
     const int head = blockIdx.x / w.parts, b = head / a.kv_heads;   // (sequence, key head)
     const int len = a.held(b), first = len - a.fresh, rows = a.fresh * a.share;
-    const int j0 = (int)(blockIdx.x % w.parts) * 1024 + threadIdx.x;
-    if (j0 - (int)threadIdx.x >= len) return;
-    const float2* stats = a.stats + (int64_t)head * rows;
-    const float* z = a.z + (int64_t)head * rows * a.z_row;
-    bool ok[4];
-    float sum[4];
+    const int j = ((int)(blockIdx.x % w.parts) * 256 + (int)threadIdx.x) * 4;
+    if (j >= len) return;
+    const int64_t base = (int64_t)head * a.table_row * a.page + j;
+    f32x4 old = {0.f, 0.f, 0.f, 0.f};
+    if (w.in && j < first) {
+        if (w.wide) old = *reinterpret_cast<const f32x4*>(w.in + base);   // rows are multiples of eight tokens
+        else
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = j0 + 256 * i;
-        ok[i] = j < len && a.there(b, j >> a.shift);
-        sum[i] = 0.f;
+            for (int i = 0; i < 4; ++i) old[i] = w.in[base + i];
     }
-    for (int r = 0; r < rows; ++r) {
-        const float2 st = stats[r];
-        const int at = first + r / a.share;
-        const float* zr = z + (int64_t)r * a.z_row;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (a.there(b, j >> a.shift)) {
+        const float2* stats = a.stats + (int64_t)head * rows;
+        const float* z = a.z + (((int64_t)head * a.chunks + j / kKeys) * rows) * kKeys + j % kKeys;
+        constexpr int N = 8;   // rows whose scores are requested together
+        for (int r0 = 0; r0 < rows; r0 += N) {
+            f32x4 v[N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = j0 + 256 * i;
-            if (ok[i] && j <= at) sum[i] += __builtin_amdgcn_exp2f(zr[j] - st.x) * st.y;
+            for (int n = 0; n < N; ++n)
+                v[n] = *reinterpret_cast<const f32x4*>(z + (int64_t)min(r0 + n, rows - 1) * kKeys);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int r = r0 + n;
+                if (r >= rows) break;
+                const float2 st = stats[r];
+                const int at = first + r / a.share - j;   // of the four tokens, those up to it are seen
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += i <= at ? __builtin_amdgcn_exp2f(v[n][i] - st.x) * st.y : 0.f;
+            }
         }
     }
-    const int64_t base = (int64_t)head * a.table_row * a.page;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = j0 + 256 * i;
-        if (j < len) w.out[base + j] = (w.in && j < first ? w.in[base + j] : 0.f) + sum[i];
+    for (int i = 0; i < 4; ++i) sum[i] += j + i < first ? old[i] : 0.f;
+    if (w.wide && j + 4 <= len) {
+        *reinterpret_cast<f32x4*>(w.out + base) = sum;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (j + i < len) w.out[base + i] = sum[i];
     }
 }
 

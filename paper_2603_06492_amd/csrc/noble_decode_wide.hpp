@@ -147,10 +147,10 @@ __global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
             if constexpr (FORM == kWeigh) {
                 if (live) {
                     const float unit = MODE & kCap ? 1.f : a.sc.unit;
-                    float* zp = a.z + (((int64_t)b * a.kv_heads + kv) * rows + row) * a.z_row + k0 + 4 * h;
+                    float* zp = a.z + ((((int64_t)b * a.kv_heads + kv) * a.chunks + k0 / kKeys) * rows + row) * kKeys + 4 * h;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<f32x4*>(zp + 8 * i) =
+                        *reinterpret_cast<f32x4*>(zp + (int64_t)(i >> 2) * rows * kKeys + 8 * (i & 3)) =
                             f32x4{z[4 * i] * unit, z[4 * i + 1] * unit, z[4 * i + 2] * unit, z[4 * i + 3] * unit};
                 }
             }
