@@ -46,6 +46,7 @@ noble_status check_tables(const noble_paged_desc* d, const int32_t* page_table, 
 
 constexpr int64_t kMostNew = 1 << 20;
 
+#define kMoving (getenv("NBM") ? atoi(getenv("NBM")) : 512)
 // Workgroups that run at once: two a CU, by their LDS.
 #define kResident (p->wide?512:getenv("NBT") ? atoi(getenv("NBT")) : 256)
 
@@ -260,9 +261,11 @@ noble_status noble_cache_keep(const noble_keep_desc* desc, void* cache, const in
     if (d.kept_heads != 1 && d.kept_heads != d.kv_heads) return NOBLE_ERR_BAD_SHAPE;
     KeepArgs a{};
     a.bytes = d.head_dim * (int)elt(d.dtype);
-    a.slices = a.bytes > 128 && a.bytes % 128 == 0 ? a.bytes / 128 : 1;
-    a.lanes = a.bytes / 16 / a.slices;
     const int64_t groups = d.B * d.kv_heads * 2;
+    // shares of a head's 16-byte parts: one, unless that leaves CUs without a workgroup
+    a.lanes = a.bytes / 16;
+    while (a.lanes > 1 && groups * cdiv(a.bytes / 16, a.lanes) < kMoving) a.lanes = (a.lanes + 1) / 2;
+    a.slices = cdiv(a.bytes / 16, a.lanes);
     if (groups > kMaxGroups256 / a.slices) return NOBLE_ERR_BAD_SHAPE;
     const bool some = d.B > 0 && d.most > 0;
     NOBLE_TRY(need(cache, some && d.pages > 0));
@@ -282,7 +285,7 @@ noble_status noble_cache_keep(const noble_keep_desc* desc, void* cache, const in
     a.shift = __builtin_ctz((unsigned)d.page);
     a.kv_heads = d.kv_heads;
     a.kept_heads = d.kept_heads;
-    return launch(cache_keep_kernel, dim3((unsigned)(groups * a.slices)), dim3(256), (hipStream_t)stream, a);
+    return launch(d.most <= 2 * (256 / a.lanes) ? cache_keep_kernel<1> : cache_keep_kernel<8>, dim3((unsigned)(groups * a.slices)), dim3(256), (hipStream_t)stream, a);
 }
 
 noble_status noble_page_means(const noble_paged_desc* desc, const void* cache, const int32_t* page_table,
@@ -358,7 +361,7 @@ noble_status noble_block_select(const noble_paged_desc* desc, const noble_select
     const dim3 grid((unsigned)(rows * desc->kv_heads));
     const hipStream_t st = (hipStream_t)stream;
     const auto run = [&]<typename E>() {
-        return desc->table_row <= kFewBlocks ? launch(block_select_kernel<E, kFewBlocks, 512>, grid, dim3(512), st, a)
+        return desc->table_row <= kFewBlocks ? launch(block_select_kernel<E, kFewBlocks, 1024>, grid, dim3(1024), st, a)
                                              : launch(block_select_kernel<E, kManyBlocks, 1024>, grid, dim3(1024), st, a);
     };
     return desc->dtype == NOBLE_BF16 ? run.template operator()<uint16_t>() : run.template operator()<float>();

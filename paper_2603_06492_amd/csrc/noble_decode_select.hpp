@@ -75,8 +75,7 @@ __device__ __forceinline__ float element(const char* p) {
 }
 // Eight consecutive elements.
 template <typename E>
-__device__ __forceinline__ void elements8(const char* p, float* x) {
-    const Frag<E> f = global_frag<E>(p, true);
+__device__ __forceinline__ void elements8(const Frag<E>& f, float* x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (sizeof(E) == 2) x[i] = __uint_as_float(i & 1 ? f.v[i >> 1] & 0xffff0000u : f.v[i >> 1] << 16);
@@ -115,7 +114,7 @@ __global__ __launch_bounds__(256) void page_means_kernel(PageArgs a) {
     if (g < groups)
         for (int r = g; r < n; r += groups) {
             float v[8];
-            elements8<E>(k + ((int64_t)r * a.D + 8 * x) * ES, v);
+            elements8(global_frag<E>(k + ((int64_t)r * a.D + 8 * x) * ES, true), v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] += (double)v[i];
         }
@@ -147,12 +146,15 @@ __device__ __forceinline__ uint64_t ordered(double x) {
 }
 
 // The `need` largest of the keys key(lo) .. key(hi - 1), of equal ones the first, between places that are taken in any case:
-// out(i, j) for the i-th of all taken places j of [0, n), in their order.  The least key taken is found from its highest byte
-// down, by counting the keys that agree with it so far; places are then counted off by waves that each own a range.
+// out(i, j) for the i-th of all taken places j of [0, n), in their order.  The least key taken is found from its highest 11
+// bits down, by counting the keys that agree with it so far; places are then counted off by waves that each own a range.
+// Digits of 11 bits hold all of a float32's exponent and two bits more: with 8, nearly all weights fall into a few counts,
+// whose additions wait for each other (64 x 4 rows of 16384 to 32768 weights EVICT_8 and EVICT_11 us).
 template <typename K, int THREADS>
 struct Pick {
-    static constexpr int WAVES = THREADS / 64;
-    uint32_t hist[WAVES][257];
+    static constexpr int WAVES = THREADS / 64, BITS = 11, BINS = 1 << BITS, COPIES = 2, PER = BINS / THREADS;
+    uint32_t hist[COPIES][BINS];
+    uint32_t sums[WAVES];
     uint32_t above[WAVES], equal[WAVES];
     K prefix, mask;
     uint32_t left, done;
@@ -162,42 +164,49 @@ struct Pick {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         K pre = 0, msk = 0;
         uint32_t want = (uint32_t)need;
-        for (int shift = 8 * (int)sizeof(K) - 8; shift >= 0 && want > 0; shift -= 8) {
-            for (int i = lane; i < 256; i += 64) hist[wave][i] = 0;
+        for (int shift = 8 * (int)sizeof(K) - BITS; want > 0; shift = max(shift - BITS, 0)) {
+            for (int i = tid; i < COPIES * BINS; i += THREADS) hist[0][i] = 0;
             __syncthreads();
-            for (int j = lo + tid; j < hi; j += THREADS) {
-                const K k = key(j);
-                if ((k & msk) == pre) atomicAdd(&hist[wave][(uint32_t)(k >> shift) & 255u], 1u);
+            for (int j = (lo & ~3) + 4 * tid; j < hi; j += 4 * THREADS) {
+                K k[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) k[i] = key(j + i);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (j + i >= lo && j + i < hi && (k[i] & msk) == pre)
+                        atomicAdd(&hist[wave % COPIES][(uint32_t)(k[i] >> shift) & (BINS - 1)], 1u);
             }
             __syncthreads();
-            if (wave == 0) {
-                // lane l has the bins 255 - 4 l down to 252 - 4 l
-                uint32_t c[4], sum = 0;
+            // a thread has PER counts, the first thread the largest keys'
+            uint32_t c[PER], sum = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    c[i] = 0;
-                    for (int x = 0; x < WAVES; ++x) c[i] += hist[x][255 - 4 * lane - i];
-                    sum += c[i];
-                }
-                uint32_t upto = sum;   // of this lane's bins and the larger ones
+            for (int i = 0; i < PER; ++i) {
+                c[i] = 0;
 #pragma unroll
-                for (int o = 1; o < 64; o *= 2) {
-                    const uint32_t v = __shfl_up(upto, o);
-                    if (lane >= o) upto += v;
-                }
-                uint32_t before = upto - sum;
-                if (before < want && upto >= want) {
+                for (int x = 0; x < COPIES; ++x) c[i] += hist[x][BINS - 1 - PER * tid - i];
+                sum += c[i];
+            }
+            uint32_t upto = sum;   // of this thread's counts and those before them
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (before < want && before + c[i] >= want) {
-                            prefix = pre | (K)(255 - 4 * lane - i) << shift;
-                            mask = msk | (K)255 << shift;
-                            left = want - before;
-                            done = c[i] == want - before;   // the whole bin is taken
-                            break;
-                        }
-                        before += c[i];
+            for (int o = 1; o < 64; o *= 2) {
+                const uint32_t v = __shfl_up(upto, o);
+                if (lane >= o) upto += v;
+            }
+            if (lane == 63) sums[wave] = upto;
+            __syncthreads();
+            for (int x = 0; x < wave; ++x) upto += sums[x];
+            uint32_t before = upto - sum;
+            if (before < want && upto >= want) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    if (before + c[i] >= want) {
+                        prefix = pre | (K)(BINS - 1 - PER * tid - i) << shift;
+                        mask = msk | (K)(BINS - 1) << shift;
+                        left = want - before;
+                        done = shift == 0 || c[i] == want - before;   // or the whole bin is taken
+                        break;
                     }
+                    before += c[i];
                 }
             }
             __syncthreads();
@@ -207,23 +216,36 @@ struct Pick {
             if (done) break;
             __syncthreads();
         }
-        // places in order: those above the least key or taken in any case, and the first `want` of the least
-        const int span = ((n + THREADS - 1) / THREADS) * 64, j0 = min(wave * span, n), j1 = min(j0 + span, n);
-        const auto state = [&](int j, bool& is_above, bool& is_equal) {
-            is_above = j < j1 && (j < lo || j >= hi);
-            is_equal = false;
-            if (j < j1 && !is_above && need > 0) {
-                const K k = key(j) & msk;
-                is_above = k > pre;
-                is_equal = k == pre;
+        // places in order: those above the least key or taken in any case, and the first `want` of the least.  Waves own
+        // ranges, a lane four places that follow each other.
+        const int span = ((n + 4 * THREADS - 1) / (4 * THREADS)) * 256, j0 = min(wave * span, n), j1 = min(j0 + span, n);
+        const auto state = [&](int j, uint32_t& is_above, uint32_t& is_equal) {   // of the lane's four places, a bit each
+            is_above = is_equal = 0;
+            K k[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = need > 0 && j < j1 ? key(j + i) & msk : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool in = j + i < j1, any = in && (j + i < lo || j + i >= hi);
+                is_above |= (any || (in && need > 0 && k[i] > pre) ? 1u : 0u) << i;
+                is_equal |= (!any && in && need > 0 && k[i] == pre ? 1u : 0u) << i;
             }
         };
-        uint32_t na = 0, ne = 0;
-        for (int j = j0; j < j1; j += 64) {
-            bool u, e;
-            state(j + lane, u, e);
-            na += __popcll(__ballot(u));
-            ne += __popcll(__ballot(e));
+        // of the counts up to four of the lanes: those of the lanes below, and all
+        const uint64_t below = (1ull << lane) - 1;
+        const auto add = [&](uint32_t c, uint32_t& upto, uint32_t& sum) {
+            const uint64_t b0 = __ballot(c & 1), b1 = __ballot(c & 2), b2 = __ballot(c & 4);
+            upto = __popcll(b0 & below) + 2 * __popcll(b1 & below) + 4 * __popcll(b2 & below);
+            sum = __popcll(b0) + 2 * __popcll(b1) + 4 * __popcll(b2);
+        };
+        uint32_t na = 0, ne = 0, unused, c;
+        for (int j = j0; j < j1; j += 256) {
+            uint32_t u, e;
+            state(j + 4 * lane, u, e);
+            add(__popc(u), unused, c);
+            na += c;
+            add(__popc(e), unused, c);
+            ne += c;
         }
         if (lane == 0) {
             above[wave] = na;
@@ -239,15 +261,22 @@ struct Pick {
             all += above[x];
             every += equal[x];
         }
-        const uint64_t below = (1ull << lane) - 1;
-        for (int j = j0; j < j1; j += 64) {
-            bool u, e;
-            state(j + lane, u, e);
-            const uint64_t bu = __ballot(u), be = __ballot(e);
-            const uint32_t ae = same + __popcll(be & below);   // equal ones before this place
-            if (u || (e && ae < want)) out((int)(at + __popcll(bu & below) + min(ae, want)), j + lane);
-            at += __popcll(bu);
-            same += __popcll(be);
+        for (int j = j0; j < j1; j += 256) {
+            uint32_t u, e, ua, ea, us, es;
+            state(j + 4 * lane, u, e);
+            add(__popc(u), ua, us);
+            add(__popc(e), ea, es);
+            ua += at;
+            ea += same;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool iu = u >> i & 1u, ie = e >> i & 1u;
+                if (iu || (ie && ea < want)) out((int)(ua + min(ea, want)), j + 4 * lane + i);
+                ua += iu;
+                ea += ie;
+            }
+            at += us;
+            same += es;
         }
         return (int)(all + min(every, want));
     }
@@ -265,7 +294,7 @@ struct EvictArgs {
 // One workgroup a sequence and key head.  LDS holds the weights of up to N tokens; longer rows are read again each time.
 template <int N>
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
-    __shared__ uint32_t keys[N];
+    __shared__ __attribute__((aligned(16))) uint32_t keys[N];
     __shared__ Pick<uint32_t, 1024> pick;
     const int b = blockIdx.x / a.heads;
     const int n = (int)min((int64_t)max(a.lengths[b], 0), a.row);
@@ -286,7 +315,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
             __syncthreads();
             total = pick.run(n, lo, hi, need, [&](int j) { return keys[j]; }, out);
         } else {
-            total = pick.run(n, lo, hi, need, [&](int j) { return ordered(w[j]); }, out);
+            total = pick.run(n, lo, hi, need, [&](int j) { return ordered(w[min(j, n - 1)]); }, out);
         }
     }
     for (int i = total + threadIdx.x; i < a.keep; i += 1024) {
@@ -310,7 +339,7 @@ struct SelectArgs {
 // scores of up to N blocks; those of longer sequences lie in global memory.
 template <typename E, int N, int THREADS>
 __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
-    __shared__ uint64_t local_keys[N];
+    __shared__ __attribute__((aligned(16))) uint64_t local_keys[N];
     __shared__ Pick<uint64_t, THREADS> pick;
     const int ES = (int)sizeof(E), lanes = a.D <= 64 ? 8 : 16;
     const int kv = blockIdx.x % a.kv_heads, row = blockIdx.x / a.kv_heads, b = row / a.fresh;
@@ -333,28 +362,40 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
             if (in)
                 for (int h = 0; h < a.share; ++h) {
                     float v[8];
-                    elements8<E>(qp + h * a.q.head, v);
+                    elements8(global_frag<E>(qp + h * a.q.head, true), v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) q[i] += (double)v[i];
                 }
-            for (int j = lo + g; j < hi; j += THREADS / lanes) {
-                const int page = a.table[b * a.table_row + j];
-                const bool ok = page >= 0 && page < a.pages;
-                double s = 0.0;
-                if (ok && in) {
+            // eight blocks at a time: their pages, then their means, all in flight
+            constexpr int U = 8;
+            const int step = THREADS / lanes;
+            for (int j0 = lo + g; j0 < hi; j0 += U * step) {
+                int page[U];
+                Frag<E> mean[U];
+#pragma unroll
+                for (int n = 0; n < U; ++n) page[n] = j0 + n * step < hi ? a.table[b * a.table_row + j0 + n * step] : -1;
+#pragma unroll
+                for (int n = 0; n < U; ++n) {
+                    if (page[n] >= a.pages) page[n] = -1;
+                    mean[n] = global_frag<E>(a.means + (((int64_t)max(page[n], 0) * a.kv_heads + kv) * a.D + 8 * x) * ES,
+                                             page[n] >= 0 && in);
+                }
+#pragma unroll
+                for (int n = 0; n < U; ++n) {
                     float v[8];
-                    elements8<E>(a.means + (((int64_t)page * a.kv_heads + kv) * a.D + 8 * x) * ES, v);
+                    elements8(mean[n], v);
+                    double s = 0.0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s = fma(q[i], (double)v[i], s);
+                    for (int o = 1; o < lanes; o *= 2) s += __shfl_xor(s, o);
+                    if (x == 0 && j0 + n * step < hi) keys[j0 + n * step] = ordered(page[n] >= 0 ? s : -(double)INFINITY);
                 }
-                for (int o = 1; o < lanes; o *= 2) s += __shfl_xor(s, o);
-                if (x == 0) keys[j] = ordered(ok ? s : -(double)INFINITY);
             }
             __syncthreads();
         }
         // two copies, so that the one over LDS is compiled for it
         if (n <= N) total = pick.run(n, lo, hi, need, [&](int j) { return local_keys[j]; }, out);
-        else total = pick.run(n, lo, hi, need, [&](int j) { return keys[j]; }, out);
+        else total = pick.run(n, lo, hi, need, [&](int j) { return keys[min(j, hi - 1)]; }, out);
     }
     for (int i = total + threadIdx.x; i < a.count; i += THREADS) chosen[i] = -1;
 }
@@ -372,10 +413,11 @@ struct KeepArgs {
 };
 
 // One workgroup moves a share of one sequence's and key head's keys (or values), tokens in ascending order, a tile of them
-// through registers at a time.  A token never moves up, so what a tile writes no later tile reads; what it writes and an
-// earlier lane of the same tile reads, the barrier keeps.
+// through registers at a time, U a lane.  A token never moves up, so what a tile writes no later tile reads: the next tile is
+// requested, and the one after it looked up, while this one is on its way.  What a tile writes and an earlier lane of the same
+// tile reads, the barrier keeps.
+template <int U>
 __global__ __launch_bounds__(256) void cache_keep_kernel(KeepArgs a) {
-    constexpr int U = 8;
     int w = blockIdx.x;
     const int slice = w % a.slices;
     w /= a.slices;
@@ -388,37 +430,71 @@ __global__ __launch_bounds__(256) void cache_keep_kernel(KeepArgs a) {
     const int* kept = a.kept + ((int64_t)b * a.kept_heads + (a.kept_heads > 1 ? kv : 0)) * a.most;
     const int* table = a.table + b * a.table_row;
     const int64_t start = a.start ? a.start[b] : 0, held = a.table_row * a.page, head = (int64_t)a.page * a.bytes;
-    char* base = a.cache + ((int64_t)half * a.kv_heads + kv) * head + byte;
-    // the token's place in memory, nullptr: none
-    const auto place = [&](int64_t t) -> char* {
-        if (t < 0 || t >= held) return nullptr;
-        const int page = table[t >> a.shift];
-        if (page < 0 || page >= a.pages) return nullptr;
-        return base + (int64_t)page * 2 * a.kv_heads * head + (t & (a.page - 1)) * a.bytes;
+    char* base = a.cache + ((int64_t)half * a.kv_heads + kv) * head + (in ? byte : 0);
+    const int64_t page_bytes = 2 * a.kv_heads * head;
+    struct Look {
+        int from[U];          // the token that goes to place i0 + u per + r; -1: none
+        int src[U], dst[U];   // its page and that place's
     };
-    for (int64_t i0 = 0; i0 < a.most; i0 += per * U) {
-        u32x4 v[U];
-        char* to[U];
+    const auto tokens = [&](int64_t i0, Look& l) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = i0 + u * per + r;
-            to[u] = nullptr;
-            if (in && i < a.most) {
-                const int k = kept[i];
-                if (k > i) {
-                    const char* from = place(start + k);
-                    to[u] = place(start + i);
-                    if (!from) to[u] = nullptr;
-                    if (to[u]) v[u] = *reinterpret_cast<const u32x4*>(from);
-                }
-            }
+            l.from[u] = in && i < a.most ? kept[i] : -1;
         }
-        // every lane's loads have arrived before any lane stores
-        wait_vmcnt<0>();
-        __syncthreads();
+    };
+    const auto pages = [&](int64_t i0, Look& l) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (to[u]) *reinterpret_cast<u32x4*>(to[u]) = v[u];
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * per + r, s = start + l.from[u], d = start + i;
+            const bool ok = l.from[u] > i && s >= 0 && s < held && d >= 0 && d < held;
+            l.src[u] = ok ? table[s >> a.shift] : -1;
+            l.dst[u] = ok ? table[d >> a.shift] : -1;
+        }
+    };
+    struct Tile {
+        u32x4 v[U];
+        char* to[U];   // nullptr: nothing moves
+    };
+    const auto load = [&](int64_t i0, const Look& l, Tile& t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t s = start + l.from[u], d = start + i0 + u * per + r;
+            const bool ok = l.src[u] >= 0 && l.src[u] < a.pages && l.dst[u] >= 0 && l.dst[u] < a.pages;
+            t.to[u] = ok ? base + (int64_t)l.dst[u] * page_bytes + (d & (a.page - 1)) * a.bytes : nullptr;
+            // in any case: the compiler then knows how many loads are behind this tile's
+            t.v[u] = *reinterpret_cast<const u32x4*>(ok ? base + (int64_t)l.src[u] * page_bytes + (s & (a.page - 1)) * a.bytes : base);
+        }
+    };
+    const int64_t step = (int64_t)per * U;
+    Look l;
+    Tile t[2];
+    tokens(0, l);
+    pages(0, l);
+    load(0, l, t[0]);
+    if (step < a.most) {
+        tokens(step, l);
+        pages(step, l);
+    }
+    for (int64_t i0 = 0; i0 < a.most;) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (i0 + step < a.most) {
+                load(i0 + step, l, t[x ^ 1]);
+                tokens(i0 + 2 * step, l);
+            }
+            // this lane's loads of the tile have arrived, and every lane's: then any may store
+#pragma unroll
+            for (int u = 0; u < U; ++u) asm volatile("" : "+v"(t[x].v[u]));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (t[x].to[u]) *reinterpret_cast<u32x4*>(t[x].to[u]) = t[x].v[u];
+            pages(i0 + 2 * step, l);
+            i0 += step;
+            if (i0 >= a.most) break;
+        }
     }
 }
 
