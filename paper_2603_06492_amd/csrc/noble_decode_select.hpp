@@ -311,7 +311,15 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     } else {
         const int lo = a.sink, hi = n - a.recent, need = a.keep - a.sink - a.recent;
         if (n <= N) {
-            for (int j = threadIdx.x; j < n; j += 1024) keys[j] = ordered(w[j]);
+            constexpr int U = 8;   // loads in flight: one at a time, 32768 weights took EVICT_ONE us
+            for (int j0 = threadIdx.x; j0 < n; j0 += U * 1024) {
+                float v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = w[min(j0 + u * 1024, n - 1)];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (j0 + u * 1024 < n) keys[j0 + u * 1024] = ordered(v[u]);
+            }
             __syncthreads();
             total = pick.run(n, lo, hi, need, [&](int j) { return keys[j]; }, out);
         } else {
@@ -359,13 +367,18 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
             const bool in = 8 * x < a.D;
             double q[8] = {};
             const char* qp = a.q.ptr + (int64_t)row * a.q.row + (int64_t)kv * a.share * a.q.head + 8 * x * ES;
-            if (in)
-                for (int h = 0; h < a.share; ++h) {
+            for (int h0 = 0; h0 < a.share; h0 += 4) {
+                Frag<E> f[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) f[h] = global_frag<E>(qp + (h0 + h) * a.q.head, in && h0 + h < a.share);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
                     float v[8];
-                    elements8(global_frag<E>(qp + h * a.q.head, true), v);
+                    elements8(f[h], v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) q[i] += (double)v[i];
                 }
+            }
             // eight blocks at a time: their pages, then their means, all in flight
             constexpr int U = 8;
             const int step = THREADS / lanes;
