@@ -46,13 +46,12 @@ noble_status check_tables(const noble_paged_desc* d, const int32_t* page_table, 
 
 constexpr int64_t kMostNew = 1 << 20;
 
-#define kMoving (getenv("NBM") ? atoi(getenv("NBM")) : 512)
-// Workgroups that run at once: two a CU, by their LDS.
-#define kResident (p->wide?512:getenv("NBT") ? atoi(getenv("NBT")) : 256)
+// Workgroups that cache_keep_kernel is to have, at least.
+constexpr int64_t kMoving = 512;
 
 // Workgroups of one attention call and its scratch.
 struct DecodePlan {
-    bool wide;                            // attn_wide_kernel, else R groups of 16 rows of attn_decode_kernel
+    int wide;                             // waves of attn_wide_kernel; 0: R groups of 16 rows of attn_decode_kernel
     bool split;                           // some pieces are joined
     int64_t R, row_tiles, slots, groups;
     size_t where, stats, z, bytes;        // offsets (the parts come first), and all of it
@@ -62,15 +61,19 @@ struct DecodePlan {
 template <int FORM>
 noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p) {
     const int64_t share = d->heads / d->kv_heads, rows = d->new_tokens * share;
-    p->wide = FORM != kBlocks && d->dtype == NOBLE_BF16 && rows > 2 * kGroup;
-    p->R = p->wide ? kWideGroups : FORM != kBlocks && rows > kGroup ? 2 : 1;
+    p->wide = FORM == kBlocks || d->dtype != NOBLE_BF16 || rows <= 2 * kGroup ? 0 : rows > 128 ? 8 : 4;
+    p->R = p->wide ? 32 * p->wide / kGroup : FORM != kBlocks && rows > kGroup ? 2 : 1;
     p->row_tiles = FORM == kBlocks ? d->new_tokens * cdiv(share, kGroup) : (rows + kGroup * p->R - 1) / (kGroup * p->R);
+    // Workgroups that run at once: one a CU, by their LDS, or two of attn_wide_kernel's with four waves.  More of them in turn,
+    // or smaller ones beside each other, read the cache more slowly: one token of 64 sequences of 16384 to 32768 tokens, 256
+    // workgroups of four waves 0.60 ms, 1280 of one wave 0.68.
+    const int64_t resident = p->wide == 4 ? 512 : 256;
     const int64_t per = d->kv_heads * p->row_tiles;   // workgroups that read the same keys, or keys of other heads
     int64_t parts;
     if (FORM == kBlocks) {
         const int waves = d->dtype == NOBLE_F32 && d->head_dim > 64 ? 1 : 2;
         const int64_t most = std::clamp<int64_t>(std::min(count, d->table_row) * d->page / kKeys / waves, 1, 64), base = d->B * per;
-        p->slots = std::clamp<int64_t>(base > 0 ? kResident / base : 1, 1, most);
+        p->slots = std::clamp<int64_t>(base > 0 ? resident / base : 1, 1, most);
         p->groups = base * p->slots;
         p->split = p->slots > 1;
         parts = p->groups;
@@ -81,8 +84,8 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
         p->slots = 1;
         double best = 0.0;
         for (int64_t turn = 1; turn <= 4; ++turn) {
-            const int64_t n = std::min(std::max<int64_t>(kResident * turn / per, 1), std::max<int64_t>(steps, 1)), all = n * per;
-            const double fill = (double)all / (double)((all + kResident - 1) / kResident * kResident);
+            const int64_t n = std::min(std::max<int64_t>(resident * turn / per, 1), std::max<int64_t>(steps, 1)), all = n * per;
+            const double fill = (double)all / (double)((all + resident - 1) / resident * resident);
             if (fill > best + 0.1) {
                 best = fill;
                 p->slots = n;
@@ -167,13 +170,13 @@ noble_status run_attention(const noble_paged_desc* d, const DecodePlan& p, const
             if constexpr (FORM == kBlocks) return attn_decode_kernel<E, DP, FORM, MODE, 1>;
             else {
                 if constexpr (sizeof(E) == 2)
-                    if (p.wide) return attn_wide_kernel<DP, FORM, MODE>;
+                    if (p.wide) return p.wide == 8 ? attn_wide_kernel<DP, FORM, MODE, 8> : attn_wide_kernel<DP, FORM, MODE, 4>;
                 return p.R == 1 ? attn_decode_kernel<E, DP, FORM, MODE, 1> : attn_decode_kernel<E, DP, FORM, MODE, 2>;
             }
         };
         NOBLE_TRY(launch(d->softcap > 0.f ? kernel.template operator()<kCap>() : kernel.template operator()<0>(),
-                         dim3((unsigned)p.groups), dim3(p.wide ? 256 : 64 * DecodeShape<E, DP>::WAVES), st, a,
-                         p.wide ? 0 : DecodeShape<E, DP>::LDS));
+                         dim3((unsigned)p.groups), dim3(p.wide ? 64 * p.wide : 64 * DecodeShape<E, DP>::WAVES), st, a,
+                         p.wide == 8 ? WideShape<DP, 8>::LDS : p.wide ? WideShape<DP, 4>::LDS : DecodeShape<E, DP>::LDS));
         if (!p.split) return NOBLE_OK;
         const DecodeJoinArgs j{a, d->B * d->new_tokens * d->heads, (int)p.R};
         return launch(decode_join_kernel<E, DP, FORM>, dim3((unsigned)cdiv(j.items, 256 / (DP / 4))), dim3(256), st, j);

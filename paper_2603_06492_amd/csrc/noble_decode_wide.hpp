@@ -1,10 +1,11 @@
 // Attention of many new rows over the paged cache, bf16: trees (kTree) and prompts or long drafts whose scores are kept
 // (kWeigh), see noble_decode_attn.hpp.
 //
-// As in attn_fwd_kernel, each of a workgroup's four waves owns 32 rows (new tokens x query heads of one key head), the columns
-// of 32x32x16 MFMAs, and all share tiles of 64 keys in LDS, two stages; here the keys come by the page table, and long
-// sequences are cut into pieces that decode_join_kernel joins.  Tiles that every row sees run without masks; the last ones,
-// which hold the new tokens, in a loop of their own.
+// As in attn_fwd_kernel, each of a workgroup's waves owns 32 rows (new tokens x query heads of one key head), the columns of
+// 32x32x16 MFMAs, and all share tiles of 64 keys in LDS.  Here the keys come by the page table and from memory, not from a
+// cache that other workgroups have filled: three tiles are on their way while one is multiplied, in a ring of four that takes
+// a CU's LDS, and up to 256 rows share each.  Tiles that every row sees run without masks; the last ones, which hold the new
+// tokens, in a loop of their own.
 #pragma once
 
 #include "noble_attn_tile.hpp"
@@ -12,16 +13,21 @@
 
 namespace noble {
 
-constexpr int kWideRows = 128, kWideGroups = kWideRows / kGroup;
+// Eight waves take a CU's LDS, workgroups of four half of it.
+template <int DP, int NW>
+struct WideShape {
+    static constexpr int STAGE = 2 * Tile<uint16_t, DP>::bytes(kPart), STAGES = NW == 8 ? 4 : 2, LDS = STAGES * STAGE;
+};
 
-template <int DP, int FORM, int MODE>
-__global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
+// NW: waves, of 32 rows each.
+template <int DP, int FORM, int MODE, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_wide_kernel(DecodeArgs a) {
     using E = uint16_t;
     using T = Tile<E, DP>;
-    using S = TileShape<E, DP, false>;
-    constexpr int ES = T::ES, TB = S::TB, NS = DP / 16, ND = DP / 32, KEYS = kPart;
-    constexpr int RPI = 1024 / T::RB, PER = 16 / RPI;   // rows of a request, requests of a wave's share of a tile's keys
-    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
+    using S = WideShape<DP, NW>;
+    constexpr int ES = T::ES, TB = S::STAGE / 2, NS = DP / 16, ND = DP / 32, KEYS = kPart, NST = S::STAGES, kWideRows = 32 * NW;
+    constexpr int MINE = KEYS / NW, RPI = 1024 / T::RB, PER = MINE / RPI;   // a wave's share of a tile's keys, of a request, requests
+    extern __shared__ __attribute__((aligned(1024))) char lds[];   // S::LDS, see attn_decode_kernel
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     int w = blockIdx.x;
     const int kv = w % a.kv_heads;
@@ -50,11 +56,20 @@ __global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
 
         typedef const __attribute__((address_space(4))) int* table_ptr;
         const table_ptr table = (table_ptr)(a.table + b * a.table_row);
-        uint64_t bads[2] = {0, 0};   // keys of a tile without a page in the cache, of even tiles and of odd ones
-        const auto request = [&](int n, char* dst) {
+        uint32_t vo[PER];   // a lane's place in each request of the wave's share of a tile
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int r = wave * MINE + i * RPI + lane / T::NC, ch = (lane % T::NC) ^ T::swz(r);
+            vo[i] = 16 * ch < db ? (uint32_t)((lane / T::NC) * db + 16 * ch) : kOOB;
+        }
+        const char* heads = a.cache + (int64_t)kv * a.page * db;
+        const int64_t values = (int64_t)a.kv_heads * a.page * db;   // from a key to its value
+        // Requests the wave's share of a tile; returns which of the tile's keys have no page in the cache.
+        const auto request = [&](int n) {
             const int k0 = (t0 + n) * KEYS;
+            char* dst = lds + (n & (NST - 1)) * S::STAGE + wave * MINE * T::RB;
             uint64_t bad = 0;
-            int page = -1, own[2] = {-1, -1};
+            int page = -1, own[MINE / 8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
                 const int key = k0 + 8 * x;
@@ -64,22 +79,19 @@ __global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
                     if (page >= a.pages) page = -1;
                 }
                 if (page < 0) bad |= 0xffull << (8 * x);
-                if (x >> 1 == wave) own[x & 1] = page;
+                if (x / (MINE / 8) == wave) own[x % (MINE / 8)] = page;
             }
-            if (n & 1) bads[1] = bad;
-            else bads[0] = bad;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int r0 = wave * 16 + i * RPI, key = k0 + r0, pg = own[i * RPI >> 3];
-                const int64_t bytes = pg >= 0 ? (int64_t)max(min(end - key, RPI), 0) * db : 0;
-                const char* src = a.cache + (int64_t)max(pg, 0) * a.page_bytes + ((int64_t)kv * a.page + (key & (a.page - 1))) * db;
-                const int r = r0 + lane / T::NC, ch = (lane % T::NC) ^ T::swz(r);
-                const uint32_t vo = 16 * ch < db ? (uint32_t)((lane / T::NC) * db + 16 * ch) : kOOB;
-                dma16(wave_desc(src, bytes), dst + r0 * T::RB, vo, 0);
-                dma16(wave_desc(src + (int64_t)a.kv_heads * a.page * db, bytes), dst + TB + r0 * T::RB, vo, 0);
+                const int key = k0 + wave * MINE + i * RPI, pg = own[i * RPI >> 3];
+                const int bytes = pg >= 0 ? max(min(end - key, RPI), 0) * db : 0;
+                const char* src = heads + (int64_t)max(pg, 0) * a.page_bytes + (int64_t)(key & (a.page - 1)) * db;
+                dma16(wave_desc(src, bytes), dst + i * 1024, vo[i], 0);
+                dma16(wave_desc(src + values, bytes), dst + TB + i * 1024, vo[i], 0);
             }
+            return bad;
         };
-        const Tiles<E, DP, false, decltype(request)> ts(lds, wave, t1 - t0, request);
+        const int count = t1 - t0;
 
         f32x16 acc[ND];
 #pragma unroll
@@ -87,8 +99,12 @@ __global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
         float m = -INFINITY, l = 0.f;
-        const Reader<E, DP> rd(ts.lds, lane);
+        const Reader<E, DP> rd(lds, lane);
         operands_here();
+        uint64_t bad = 0, bad1 = 0, bad2 = 0, bad3 = 0;   // of this tile and the next three
+        if (count > 0) bad1 = request(0);
+        if (NST > 2 && count > 1) bad2 = request(1);
+        if (NST > 2 && count > 2) bad3 = request(2);
 
         // bits 32 u + 8 (i / 4) + i % 4 of the lane's 32 scores: of the tile's keys those that the row of a token sees
         const auto sees = [&](int t, int k0) {
@@ -102,10 +118,24 @@ __global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
         };
         const auto step = [&]<bool EDGE>(int n) {
             const int k0 = (t0 + n) * KEYS;
-            const uint64_t bad = n & 1 ? bads[1] : bads[0];
-            ts.at(n);
+            // this wave's share of the tile is here, and every wave's; and every wave has read the tile before
+            const int newer = count - 1 - n;
+            if (NST > 2 && newer >= 2) wait_vmcnt<4 * PER>();
+            else if (NST > 2 && newer == 1) wait_vmcnt<2 * PER>();
+            else wait_vmcnt<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            bad = bad1;
+            if constexpr (NST > 2) {
+                bad1 = bad2;
+                bad2 = bad3;
+                if (newer >= 3) bad3 = request(n + 3);
+            } else {
+                if (newer >= 1) bad1 = request(n + 1);
+            }
             if (!any) return;
-            const Reader<E, DP> at_tile = rd.at(ts.offset(n));
+            const Reader<E, DP> at_tile = rd.at((n & (NST - 1)) * S::STAGE);
             float z[32];
             f32x16 s[2];
 #pragma unroll
@@ -215,10 +245,10 @@ __global__ __launch_bounds__(256, 2) void attn_wide_kernel(DecodeArgs a) {
         };
         // keys that every row of the workgroup sees
         const int all = max(FORM == kTree ? first : first + row0 / a.share + 1, 0);
-        const int seen = min(max(all / KEYS - t0, 0), ts.count);
+        const int seen = min(max(all / KEYS - t0, 0), count);
         int n = 0;
         for (; n < seen; ++n) step.template operator()<false>(n);
-        for (; n < ts.count; ++n) step.template operator()<true>(n);
+        for (; n < count; ++n) step.template operator()<true>(n);
         l = sum_halves(l);
 
         if (!live) {
