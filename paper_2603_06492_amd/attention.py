@@ -527,54 +527,149 @@ def _values(qkv, k):
 
 class PagedCache:
     """Keys and values of a batch of sequences in pages of ``page`` tokens, for ``layers`` layers that share one page table
-    (``data[layer]`` is [pages, 2, kv_heads, page, head_dim]).  Which page belongs to which sequence is kept here."""
+    (``data[layer]`` is [pages, 2, kv_heads, page, head_dim]).  Which page belongs to which sequence is kept here.
+
+    ``means``: also the means of every page's keys (``means[layer]``), by which ``NobleSelfAttention.step`` selects pages.
+    ``weights``: also the attention weight that every token has received (``weights[layer]``, float32 [sequences, kv_heads,
+    tokens]), by which ``evict`` goes."""
 
     def __init__(self, sequences: int, longest: int, pages: int, *, kv_heads: int, head_dim: int, page: int = 16,
-                 layers: int = 1, dtype=torch.bfloat16, device="cuda"):
+                 layers: int = 1, dtype=torch.bfloat16, device="cuda", means: bool = False, weights: bool = False):
         per = -(-longest // page)
         self.page, self.longest = page, longest
         self.data = [torch.empty((pages, 2, kv_heads, page, head_dim), dtype=dtype, device=device) for _ in range(layers)]
         self.page_table = torch.full((sequences, per), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        new = lambda keep, *shape, **kw: [torch.zeros(*shape, device=device, **kw) for _ in range(layers)] if keep else None  # noqa: E731
+        self.means = new(means, (pages, kv_heads, head_dim), dtype=dtype)
+        self.weights = new(weights, (sequences, kv_heads, per * page))
         self._table = [[] for _ in range(sequences)]
         self._held = [0] * sequences
+        self._seen = [0] * sequences   # tokens that the sequence has had, evicted ones among them
         self._free = list(range(pages - 1, -1, -1))
+        self._drafted = 0
 
-    def extend(self, new: int):
-        """Room for ``new`` more tokens of every sequence: (positions int32, slots int64), both [sequences * new], a
-        sequence's tokens in a row.  Raises MemoryError when the pages run out and ValueError past ``longest``; nothing has
-        changed then."""
+    def _room(self, new: int):
+        """Pages for ``new`` more tokens of every sequence, and their slots."""
         if new < 0:
             raise ValueError(f"{new} new tokens")
+        if self._drafted:
+            raise RuntimeError("a draft is in the cache: accept what is to stay of it first")
         if max(self._held) + new > self.longest:
             raise ValueError(f"sequences of up to {self.longest} tokens: {max(self._held)} held, {new} more")
         need = [-(-(n + new) // self.page) - len(t) for n, t in zip(self._held, self._table)]
         if sum(need) > len(self._free):
             raise MemoryError(f"{sum(need)} more pages needed, {len(self._free)} free")
-        positions, slots = [], []
+        slots = []
         for b, pages in enumerate(self._table):
             pages += [self._free.pop() for _ in range(need[b])]
-            at = range(self._held[b], self._held[b] + new)
-            positions += at
-            slots += [pages[t // self.page] * self.page + t % self.page for t in at]
+            slots += [pages[t // self.page] * self.page + t % self.page for t in range(self._held[b], self._held[b] + new)]
             self._held[b] += new
-        dev = self.lengths.device
+            self._seen[b] += new
         if any(need):
-            per = self.page_table.shape[1]
-            self.page_table.copy_(torch.tensor([p + [-1] * (per - len(p)) for p in self._table], dtype=torch.int32))
+            self._write_table()
         self.lengths += new
-        return (torch.tensor(positions, dtype=torch.int32, device=dev),
-                torch.tensor(slots, dtype=torch.int64, device=dev))
+        return torch.tensor(slots, dtype=torch.int64, device=self.lengths.device)
+
+    def _write_table(self) -> None:
+        per = self.page_table.shape[1]
+        self.page_table.copy_(torch.tensor([p + [-1] * (per - len(p)) for p in self._table], dtype=torch.int32))
+
+    def extend(self, new: int):
+        """Room for ``new`` more tokens of every sequence: (positions int32, slots int64), both [sequences * new], a
+        sequence's tokens in a row.  Raises MemoryError when the pages run out and ValueError past ``longest``; nothing has
+        changed then."""
+        slots = self._room(new)
+        positions = [t for n in self._seen for t in range(n - new, n)]
+        return torch.tensor(positions, dtype=torch.int32, device=slots.device), slots
+
+    def draft(self, parents):
+        """Room for a tree of n drafted tokens of every sequence, parents int32 [sequences, n] as noble_tree_rows takes them:
+        (positions, slots, tree), for ``NobleSelfAttention.step(..., tree=tree)`` in every layer.  ``accept`` says which of
+        them stay, before anything else is put into the cache.  Raises as ``extend`` does."""
+        from . import decoding
+        parents = parents.to(device=self.lengths.device, dtype=torch.int32).contiguous()
+        if parents.dim() != 2 or parents.shape[0] != len(self._held) or not 1 <= parents.shape[1] <= decoding.TREE_MOST:
+            raise ValueError(f"parents must be [{len(self._held)} sequences, 1 to {decoding.TREE_MOST} nodes], got "
+                             f"{tuple(parents.shape)}")
+        slots = self._room(parents.shape[1])
+        self._drafted = parents.shape[1]
+        seen, depths, positions = decoding.noble_tree_rows(parents, self.lengths)
+        gone = [s - n for s, n in zip(self._seen, self._held)]
+        if any(gone):
+            positions += torch.tensor(gone, dtype=torch.int32, device=slots.device)[:, None]
+        return positions.view(-1), slots, (seen, depths)
+
+    def accept(self, kept) -> None:
+        """Of the drafted tree only the nodes kept[b] (a list of ascending numbers for each sequence, from the root down)
+        stay in sequence b, one after the other; the pages of the others are given back."""
+        from . import decoding
+        n = self._drafted
+        if not n:
+            raise RuntimeError("no draft is in the cache")
+        if len(kept) != len(self._held) or any(x < 0 or x >= n or (i and x <= k[i - 1]) for k in kept for i, x in enumerate(k)):
+            raise ValueError(f"kept must be {len(self._held)} lists of ascending numbers below {n}")
+        start = [h - n for h in self._held]
+        table = torch.tensor([[list(k) + [-1] * (n - len(k))] for k in kept], dtype=torch.int32, device=self.lengths.device)
+        first = torch.tensor(start, dtype=torch.int32, device=self.lengths.device)
+        for data in self.data:
+            decoding.noble_cache_keep(data, self.page_table, table, first)
+        for w in self.weights or ():   # they have received nothing yet
+            for b, k in enumerate(kept):
+                w[b, :, start[b]:start[b] + len(k)] = 0
+        self._drafted = 0
+        self._seen = [s - n + len(k) for s, k in zip(self._seen, kept)]
+        self._cut([s + len(k) for s, k in zip(start, kept)], n)
+
+    def evict(self, keep: int, *, sink: int = 0, recent: int = 0) -> None:
+        """Of every sequence with more than ``keep`` tokens, each layer and key head keeps that many: the first ``sink``, the
+        last ``recent`` and, of the others, those that have received the most attention weight (``weights``), in their order.
+        Later tokens' positions go on from all the sequence has had; a window and the distance bias count the tokens that
+        are left."""
+        from . import decoding
+        if self.weights is None:
+            raise ValueError("a cache without weights")
+        if self._drafted:
+            raise RuntimeError("a draft is in the cache: accept what is to stay of it first")
+        if keep < 1 or sink < 0 or recent < 0 or sink + recent > keep:
+            raise ValueError(f"keep={keep} tokens, the first {sink} and the last {recent} among them")
+        if max(self._held) <= keep:
+            return
+        for data, weights in zip(self.data, self.weights):
+            kept, left = decoding.noble_evict_select(weights, self.lengths, keep, sink=sink, recent=recent)
+            decoding.noble_cache_keep(data, self.page_table, kept)
+            weights[:, :, :keep] = left
+        self._cut([min(h, keep) for h in self._held], keep)
+
+    def _cut(self, held, changed: int) -> None:
+        """The sequences hold so many tokens from now on, of which the last ``changed`` have other places than before."""
+        from . import decoding
+        for b, n in enumerate(held):
+            used = -(-n // self.page)
+            self._free += reversed(self._table[b][used:])
+            del self._table[b][used:]
+        self._held = held
+        self._write_table()
+        self.lengths.copy_(torch.tensor(held, dtype=torch.int32))
+        for data, means in zip(self.data, self.means or ()):
+            decoding.noble_page_means(data, self.page_table, self.lengths, changed, means)
 
     @property
     def held(self) -> int:
         """Tokens of the sequence that holds the most."""
         return max(self._held, default=0)
 
+    @property
+    def seen(self) -> int:
+        """Tokens that the longest sequence has had, evicted ones among them."""
+        return max(self._seen, default=0)
+
     def release(self, sequence: int) -> None:
         """Gives a sequence's pages back; it holds no tokens then."""
+        if self._drafted:
+            raise RuntimeError("a draft is in the cache: accept what is to stay of it first")
         self._free += reversed(self._table[sequence])
-        self._table[sequence], self._held[sequence] = [], 0
+        self._table[sequence], self._held[sequence], self._seen[sequence] = [], 0, 0
         self.page_table[sequence] = -1
         self.lengths[sequence] = 0
 
@@ -636,16 +731,41 @@ class NobleSelfAttention(torch.nn.Module):
         return self.out(o.reshape(T, -1)).reshape(shape)
 
     @torch.no_grad()
-    def step(self, x, cache: PagedCache, positions, slots, layer: int = 0, window: int = 0):
+    def step(self, x, cache: PagedCache, positions, slots, layer: int = 0, window: int = 0, *, tree=None, blocks: int = 0,
+             sink: int = 0, local: int = 1):
         """The newest tokens of every sequence, x [sequences * new, d], with the positions and slots that
         ``cache.extend(new)`` gave: their keys and values go into the cache, their attention runs over it.  A whole prompt
         is a step too.  A token sees those up to itself, with a ``window`` (the one that ``mask`` took for training) only
-        that many; a mask with a prefix or without ``causal`` has no such form: feed its tokens to ``forward``."""
-        self._fits(cache.held)
-        q = noble_kv_append(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, slots,
-                            cache.data[layer], **self.how)
-        o = noble_attn_paged(q, cache.data[layer], cache.page_table, cache.lengths, self.slopes, softcap=self.softcap,
-                             window=window)
+        that many; a mask with a prefix or without ``causal`` has no such form: feed its tokens to ``forward``.
+
+        ``tree``: the tokens are drafted ones, from ``cache.draft(parents)``, and see the nodes above them.  ``blocks``: each
+        token and key head sees that many pages of its sequence, the first ``sink``, the last ``local`` and those whose means
+        (of a cache with ``means``) its queries favour.  With a cache that keeps ``weights`` the weight that every token
+        receives is added up.  These go one at a time, and without a window."""
+        from . import decoding
+        self._fits(cache.seen)
+        new = x.shape[0] // max(cache.lengths.shape[0], 1)
+        forms = [name for name, on in (("tree", tree is not None), ("blocks", blocks), ("weights", cache.weights is not None and
+                                                                                       tree is None)) if on]
+        if len(forms) > 1 or (forms and window):
+            raise ValueError(f"{' and '.join(forms + ['window'] * bool(window))} in one step")
+        if blocks and cache.means is None:
+            raise ValueError("blocks are selected by a cache's means: PagedCache(..., means=True)")
+        data, held = cache.data[layer], (cache.data[layer], cache.page_table, cache.lengths)
+        q = noble_kv_append(self.qkv(x), self.q_weight, self.k_weight, self.cos, self.sin, positions, slots, data, **self.how)
+        how = dict(softcap=self.softcap)
+        if tree is not None:
+            o = decoding.noble_attn_tree(q, *held, *tree, self.slopes, **how)
+            return self.out(o.reshape(x.shape[0], -1))
+        if cache.means is not None and new:
+            decoding.noble_page_means(*held, new, cache.means[layer])
+        if blocks:
+            chosen = decoding.noble_block_select(q, cache.means[layer], *held[1:], blocks, page=cache.page, sink=sink, local=local)
+            o = decoding.noble_attn_blocks(q, *held, chosen, self.slopes, **how)
+        elif cache.weights is not None:
+            o, _ = decoding.noble_attn_weigh(q, *held, cache.weights[layer], self.slopes, out=cache.weights[layer], **how)
+        else:
+            o = noble_attn_paged(q, *held, self.slopes, window=window, **how)
         return self.out(o.reshape(x.shape[0], -1))
 
     def param_groups(self, lr):

@@ -70,31 +70,34 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
     const int64_t resident = p->wide == 4 ? 512 : 256;
     const int64_t per = d->kv_heads * p->row_tiles;   // workgroups that read the same keys, or keys of other heads
     int64_t parts;
-    if (FORM == kBlocks) {
-        const int waves = d->dtype == NOBLE_F32 && d->head_dim > 64 ? 1 : 2;
-        const int64_t most = std::clamp<int64_t>(std::min(count, d->table_row) * d->page / kKeys / waves, 1, 64), base = d->B * per;
-        p->slots = std::clamp<int64_t>(base > 0 ? resident / base : 1, 1, most);
-        p->groups = base * p->slots;
-        p->split = p->slots > 1;
-        parts = p->groups;
-    } else {
-        // as many slots as fill the workgroups that run at once best, once, or a few times where that is not near
-        const int64_t steps = d->B * (d->table_row * d->page / (p->wide ? kPart : kKeys) + 1);
-        if (steps > INT32_MAX) return NOBLE_ERR_BAD_SHAPE;   // the kernels count them in 32 bits
-        p->slots = 1;
+    // Of so many workgroups `one`, up to `most` of them: as many as fill those that run at once best, once, or a few times
+    // where once is not near.
+    const auto filling = [&](int64_t one, int64_t most) {
+        int64_t slots = 1;
         double best = 0.0;
-        for (int64_t turn = 1; turn <= 4; ++turn) {
-            const int64_t n = std::min(std::max<int64_t>(resident * turn / per, 1), std::max<int64_t>(steps, 1)), all = n * per;
+        for (int64_t turn = 1; turn <= 4 && one > 0; ++turn) {
+            const int64_t n = std::clamp<int64_t>(resident * turn / one, 1, most), all = n * one;
             const double fill = (double)all / (double)((all + resident - 1) / resident * resident);
             if (fill > best + 0.1) {
                 best = fill;
-                p->slots = n;
+                slots = n;
             }
         }
+        return slots;
+    };
+    if (FORM == kBlocks) {
+        const int64_t waves = d->dtype == NOBLE_F32 && d->head_dim > 64 ? 2 : 4, lists = d->B * per;
+        p->slots = filling(lists, std::clamp<int64_t>(std::min(count, d->table_row) * d->page / kKeys / waves, 1, 64));
+        p->groups = lists * p->slots;
+        parts = p->groups;
+    } else {
+        const int64_t steps = d->B * (d->table_row * d->page / (p->wide ? kPart : kKeys) + 1);
+        if (steps > INT32_MAX) return NOBLE_ERR_BAD_SHAPE;   // the kernels count them in 32 bits
+        p->slots = filling(per, std::max<int64_t>(steps, 1));
         p->groups = d->B > 0 ? p->slots * per : 0;
-        p->split = p->slots > 1;
         parts = 2 * p->groups;
     }
+    p->split = p->slots > 1;
     if (p->groups > kMaxGroups256 || d->B * d->new_tokens * d->heads > kMaxGroups256 * 8) return NOBLE_ERR_BAD_SHAPE;
     p->chunks = (d->table_row * d->page + kPart - 1) / kPart * (kPart / kKeys);   // whole tiles of either kernel
     p->where = p->stats = p->z = 0;
