@@ -196,7 +196,7 @@ noble_status check_select(const noble_paged_desc* d, const noble_select_desc* s)
 }
 
 // Blocks whose scores LDS holds: those of a sequence of up to table_row pages.
-constexpr int64_t kFewBlocks = 2048, kManyBlocks = 16384;
+constexpr int64_t kFewestBlocks = 256, kFewBlocks = 2048, kManyBlocks = 16384;
 
 noble_status select_scratch(const noble_paged_desc* d, size_t* bytes) {
     const int64_t rows = d->B * d->new_tokens * d->kv_heads;
@@ -224,7 +224,8 @@ noble_status noble_tree_rows(int64_t B, int32_t new_tokens, const int32_t* paren
     if (!some) return NOBLE_OK;
     const TreeArgs a{parents, lengths, reinterpret_cast<uint32_t*>(seen), depths, positions, new_tokens,
                      NOBLE_TREE_WORDS(new_tokens)};
-    return launch(tree_rows_kernel, dim3((unsigned)B), dim3(kTreeMost), (hipStream_t)stream, a);
+    return new_tokens <= 64 ? launch(tree_rows_wave_kernel, dim3((unsigned)B), dim3(64), (hipStream_t)stream, a)
+                            : launch(tree_rows_kernel, dim3((unsigned)B), dim3(kTreeMost), (hipStream_t)stream, a);
 }
 
 noble_status noble_attn_tree_scratch_size(const noble_paged_desc* desc, size_t* scratch_bytes) {
@@ -291,7 +292,13 @@ noble_status noble_cache_keep(const noble_keep_desc* desc, void* cache, const in
     a.shift = __builtin_ctz((unsigned)d.page);
     a.kv_heads = d.kv_heads;
     a.kept_heads = d.kept_heads;
-    return launch(d.most <= 2 * (256 / a.lanes) ? cache_keep_kernel<1> : cache_keep_kernel<8>, dim3((unsigned)(groups * a.slices)), dim3(256), (hipStream_t)stream, a);
+    const hipStream_t st = (hipStream_t)stream;
+    if (d.kept_heads == 1 && d.most <= kFewMoves) {
+        a.slices = (int)std::clamp<int64_t>(kMoving / 2 / d.B, 1, 2 * d.kv_heads);
+        return launch(cache_move_few_kernel, dim3((unsigned)(d.B * a.slices)), dim3(256), st, a);
+    }
+    return launch(d.most <= 2 * (256 / a.lanes) ? cache_keep_kernel<1> : cache_keep_kernel<8>,
+                  dim3((unsigned)(groups * a.slices)), dim3(256), st, a);
 }
 
 noble_status noble_page_means(const noble_paged_desc* desc, const void* cache, const int32_t* page_table,
@@ -367,6 +374,7 @@ noble_status noble_block_select(const noble_paged_desc* desc, const noble_select
     const dim3 grid((unsigned)(rows * desc->kv_heads));
     const hipStream_t st = (hipStream_t)stream;
     const auto run = [&]<typename E>() {
+        if (desc->table_row <= kFewestBlocks) return launch(block_select_kernel<E, kFewestBlocks, 256>, grid, dim3(256), st, a);
         return desc->table_row <= kFewBlocks ? launch(block_select_kernel<E, kFewBlocks, 1024>, grid, dim3(1024), st, a)
                                              : launch(block_select_kernel<E, kManyBlocks, 1024>, grid, dim3(1024), st, a);
     };

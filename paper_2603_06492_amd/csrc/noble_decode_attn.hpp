@@ -119,6 +119,18 @@ __device__ __forceinline__ void decode_store(const DecodeArgs& a, int b, int kv,
                   sum[0], sum[1], sum[2], sum[3]);
 }
 
+// The sum of a wave's values up to this lane's, by row shifts and broadcasts (see wave_fold).
+__device__ __forceinline__ uint32_t wave_upto(uint32_t v) {
+    int x = (int)v;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+    return (uint32_t)x;
+}
+
 // The steps (of `keys` keys) of all sequences in a row are dealt to the slots in equal ranges, so that a batch of sequences of
 // different lengths keeps every workgroup busy to the end: a slot has the end of one sequence, whole ones, and the beginning
 // of one, at most.  Every wave works its range out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 16 heads,
@@ -142,11 +154,10 @@ struct Slots {
     // least: steps of a slot, but for the last ones of calls that have fewer
     __device__ __forceinline__ Slots(const DecodeArgs& a, int slot, int keys, int least, int lane) {
         const int one = steps_of(a, lane, keys);   // of the first 64 sequences, a lane each
-        uint32_t total = one;
-        for (int64_t n = 64; n < a.B; n += 64) total += steps_of(a, n + lane, keys);
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
-        total = __builtin_amdgcn_readfirstlane(total);
+        const uint32_t ones = wave_upto(one);
+        uint32_t total = __builtin_amdgcn_readlane(ones, 63);
+        for (int64_t n = 64; n < a.B; n += 64)
+            total += __builtin_amdgcn_readlane(wave_upto(steps_of(a, n + lane, keys)), 63);
         const uint32_t used = min((uint32_t)a.slots, (total + least - 1) / least);
         if ((uint32_t)slot >= used) return;
         per = total / used;
@@ -155,12 +166,7 @@ struct Slots {
         left = (int)(first(slot + 1) - at);
         for (int64_t n = 0; n < a.B; n += 64) {
             const uint32_t mine = n ? steps_of(a, n + lane, keys) : one;
-            uint32_t upto = mine;
-#pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                const uint32_t v = __shfl_up(upto, o);
-                if (lane >= o) upto += v;
-            }
+            const uint32_t upto = n ? wave_upto(mine) : ones;
             const uint64_t here = __ballot(at - from < upto);
             if (here) {
                 const int l = __builtin_ctzll(here);

@@ -4,7 +4,7 @@
 
 #include <type_traits>
 
-#include "noble_attn_common.hpp"
+#include "noble_decode_attn.hpp"
 
 namespace noble {
 
@@ -54,6 +54,37 @@ __global__ __launch_bounds__(kTreeMost) void tree_rows_kernel(TreeArgs a) {
     }
     a.depths[b * a.n + i] = depth;
     if (a.positions) a.positions[b * a.n + i] = node ? max(max(a.lengths[b], 0) - a.n + depth, 0) : 0;
+}
+
+// Up to 64 nodes: one wave a tree, the lines in registers.
+__global__ __launch_bounds__(64) void tree_rows_wave_kernel(TreeArgs a) {
+    const int i = threadIdx.x;
+    const int64_t b = blockIdx.x;
+    int up = -2;
+    if (i < a.n) {
+        const int p = a.parents[b * a.n + i];
+        up = p >= -1 && p < i ? p : -2;
+    }
+    const int first = a.positions ? max(a.lengths[b], 0) - a.n : 0;
+    uint32_t lo = i < 32 ? 1u << i : 0u, hi = i < 32 ? 0u : 1u << (i - 32);
+    for (int step = 1; step < a.n; step *= 2) {
+        const int from = max(up, 0);
+        const uint32_t l = __shfl(lo, from), h = __shfl(hi, from);
+        const int next = __shfl(up, from);
+        if (up >= 0) {
+            lo |= l;
+            hi |= h;
+            up = next;
+        }
+    }
+    if (i >= a.n) return;
+    const bool node = up == -1;
+    const int depth = node ? __popc(lo) + __popc(hi) - 1 : -1;
+    uint32_t* seen = a.seen + (b * a.n + i) * a.words;
+    seen[0] = node ? lo : 0u;
+    if (a.words > 1) seen[1] = node ? hi : 0u;
+    a.depths[b * a.n + i] = depth;
+    if (a.positions) a.positions[b * a.n + i] = node ? max(first + depth, 0) : 0;
 }
 
 // ------------------------------------------------------------------ pages --
@@ -133,6 +164,21 @@ __global__ __launch_bounds__(256) void page_means_kernel(PageArgs a) {
 
 // -------------------------------------------------------------- selection --
 
+// The sum of eight lanes' values, or sixteen's, in each of them: exchanges inside a row of 16 lanes.
+__device__ __forceinline__ double lanes_sum(double x, bool sixteen) {
+    const auto add = [&](auto ctrl) {
+        const uint64_t u = (uint64_t)__double_as_longlong(x);
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, 0xf, 0xf, false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
+        return x + __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+    };
+    x = add(std::integral_constant<int, 0xb1>{});    // quad_perm: lanes 1, 0, 3, 2
+    x = add(std::integral_constant<int, 0x4e>{});    // 2, 3, 0, 1
+    x = add(std::integral_constant<int, 0x141>{});   // row_half_mirror
+    if (sixteen) x = add(std::integral_constant<int, 0x140>{});   // row_mirror
+    return x;
+}
+
 // Whole numbers in the order of the values, NaN above all, -0 with 0.
 __device__ __forceinline__ uint32_t ordered(float x) {
     if (x != x) return ~0u;
@@ -154,8 +200,8 @@ template <typename K, int THREADS>
 struct Pick {
     static constexpr int WAVES = THREADS / 64, BITS = 11, BINS = 1 << BITS, COPIES = 2, PER = BINS / THREADS;
     uint32_t hist[COPIES][BINS];
-    uint32_t sums[WAVES];
-    uint32_t above[WAVES], equal[WAVES];
+    __attribute__((aligned(16))) uint32_t sums[WAVES];
+    __attribute__((aligned(16))) uint32_t above[WAVES], equal[WAVES];
     K prefix, mask;
     uint32_t left, done;
 
@@ -164,8 +210,8 @@ struct Pick {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         K pre = 0, msk = 0;
         uint32_t want = (uint32_t)need;
+        for (int i = tid; i < COPIES * BINS; i += THREADS) hist[0][i] = 0;
         for (int shift = 8 * (int)sizeof(K) - BITS; want > 0; shift = max(shift - BITS, 0)) {
-            for (int i = tid; i < COPIES * BINS; i += THREADS) hist[0][i] = 0;
             __syncthreads();
             for (int j = (lo & ~3) + 4 * tid; j < hi; j += 4 * THREADS) {
                 K k[4];
@@ -177,24 +223,23 @@ struct Pick {
                         atomicAdd(&hist[wave % COPIES][(uint32_t)(k[i] >> shift) & (BINS - 1)], 1u);
             }
             __syncthreads();
-            // a thread has PER counts, the first thread the largest keys'
+            // a thread has PER counts, the first thread the largest keys'; they are zero again for the next digit
             uint32_t c[PER], sum = 0;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 c[i] = 0;
 #pragma unroll
-                for (int x = 0; x < COPIES; ++x) c[i] += hist[x][BINS - 1 - PER * tid - i];
+                for (int x = 0; x < COPIES; ++x) {
+                    c[i] += hist[x][BINS - 1 - PER * tid - i];
+                    hist[x][BINS - 1 - PER * tid - i] = 0;
+                }
                 sum += c[i];
             }
-            uint32_t upto = sum;   // of this thread's counts and those before them
-#pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                const uint32_t v = __shfl_up(upto, o);
-                if (lane >= o) upto += v;
-            }
+            uint32_t upto = wave_upto(sum);   // of this thread's counts and those before them
             if (lane == 63) sums[wave] = upto;
             __syncthreads();
-            for (int x = 0; x < wave; ++x) upto += sums[x];
+#pragma unroll
+            for (int x = 0; x < WAVES; ++x) upto += x < wave ? sums[x] : 0u;
             uint32_t before = upto - sum;
             if (before < want && upto >= want) {
 #pragma unroll
@@ -214,7 +259,6 @@ struct Pick {
             msk = mask;
             want = left;
             if (done) break;
-            __syncthreads();
         }
         // places in order: those above the least key or taken in any case, and the first `want` of the least.  Waves own
         // ranges, a lane four places that follow each other.
@@ -253,11 +297,10 @@ struct Pick {
         }
         __syncthreads();
         uint32_t at = 0, same = 0, all = 0, every = 0;
+#pragma unroll
         for (int x = 0; x < WAVES; ++x) {
-            if (x < wave) {
-                at += above[x];
-                same += equal[x];
-            }
+            at += x < wave ? above[x] : 0u;
+            same += x < wave ? equal[x] : 0u;
             all += above[x];
             every += equal[x];
         }
@@ -400,7 +443,7 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
                     double s = 0.0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s = fma(q[i], (double)v[i], s);
-                    for (int o = 1; o < lanes; o *= 2) s += __shfl_xor(s, o);
+                    s = lanes_sum(s, lanes == 16);
                     if (x == 0 && j0 + n * step < hi) keys[j0 + n * step] = ordered(page[n] >= 0 ? s : -(double)INFINITY);
                 }
             }
@@ -507,6 +550,61 @@ __global__ __launch_bounds__(256) void cache_keep_kernel(KeepArgs a) {
             pages(i0 + 2 * step, l);
             i0 += step;
             if (i0 >= a.most) break;
+        }
+    }
+}
+
+
+// Lists that all key heads share, such as a tree's accepted branch: a workgroup takes some of the heads' keys and values of
+// one sequence.  Most entries move nothing; those that do are listed in LDS, and their parts dealt to the lanes.
+constexpr int kFewMoves = 256;
+__global__ __launch_bounds__(256) void cache_move_few_kernel(KeepArgs a) {
+    __shared__ int64_t from[kFewMoves], to[kFewMoves];
+    __shared__ int moves[4];
+    const int shares = a.slices;   // workgroups of a sequence
+    const int share = blockIdx.x % shares, b = blockIdx.x / shares;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = threadIdx.x;
+    const int64_t head = (int64_t)a.page * a.bytes, page_bytes = 2 * a.kv_heads * head, held = a.table_row * a.page;
+    const int64_t start = a.start ? a.start[b] : 0;
+    const int* table = a.table + b * a.table_row;
+    int64_t src = 0, dst = 0;
+    bool ok = false;
+    if (i < a.most) {
+        const int k = a.kept[b * a.most + i];
+        const int64_t s = start + k, d = start + i;
+        if (k > i && s >= 0 && s < held && d >= 0 && d < held) {
+            const int ps = table[s >> a.shift], pd = table[d >> a.shift];
+            ok = ps >= 0 && ps < a.pages && pd >= 0 && pd < a.pages;
+            src = (int64_t)ps * page_bytes + (s & (a.page - 1)) * a.bytes;
+            dst = (int64_t)pd * page_bytes + (d & (a.page - 1)) * a.bytes;
+        }
+    }
+    const uint64_t some = __ballot(ok);
+    if (lane == 0) moves[wave] = __popcll(some);
+    __syncthreads();
+    int at = __popcll(some & ((1ull << lane) - 1)), n = 0;
+    for (int x = 0; x < 4; ++x) {
+        at += x < wave ? moves[x] : 0;
+        n += moves[x];
+    }
+    if (ok) {
+        from[at] = src;
+        to[at] = dst;
+    }
+    __syncthreads();
+    // parts of 16 bytes: of a token's head, of the heads' keys and values that are this workgroup's, of the moves.  A tile of
+    // moves at a time, in ascending order, each part by the same lane for every move: it reads what no earlier move writes.
+    const int parts = a.bytes / 16, all = 2 * a.kv_heads, h0 = all * share / shares, h1 = all * (share + 1) / shares;
+    constexpr int U = 4;
+    for (int p = i; p < (h1 - h0) * parts; p += 256) {
+        char* base = a.cache + (int64_t)(h0 + p / parts) * head + p % parts * 16;
+        for (int m = 0; m < n; m += U) {
+            u32x4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const u32x4*>(base + from[min(m + u, n - 1)]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (m + u < n) *reinterpret_cast<u32x4*>(base + to[m + u]) = v[u];
         }
     }
 }
