@@ -192,7 +192,7 @@ __device__ __forceinline__ uint64_t ordered(double x) {
 }
 
 // The `need` largest of the keys key(lo) .. key(hi - 1), of equal ones the first, between places that are taken in any case:
-// out(i, j) for the i-th of all taken places j of [0, n), in their order.  The least key taken is found from its highest 11
+// out(i, taken, j) for four places j .. j + 3 of [0, n), a bit for each that is taken, the i-th of all taken.  The least key taken is found from its highest 11
 // bits down, by counting the keys that agree with it so far; places are then counted off by waves that each own a range.
 // Digits of 11 bits hold all of a float32's exponent and two bits more: with 8, nearly all weights fall into a few counts,
 // whose additions wait for each other (64 x 4 rows of 16384 to 32768 weights EVICT_8 and EVICT_11 us).
@@ -311,13 +311,17 @@ struct Pick {
             add(__popc(e), ea, es);
             ua += at;
             ea += same;
+            int places[4];
+            uint32_t taken = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool iu = u >> i & 1u, ie = e >> i & 1u;
-                if (iu || (ie && ea < want)) out((int)(ua + min(ea, want)), j + 4 * lane + i);
+                places[i] = (int)(ua + min(ea, want));
+                taken |= (iu || (ie && ea < want) ? 1u : 0u) << i;
                 ua += iu;
                 ea += ie;
             }
+            out(places, taken, j + 4 * lane);
             at += us;
             same += es;
         }
@@ -344,13 +348,23 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     const float* w = a.weights + (int64_t)blockIdx.x * a.row;
     int* kept = a.kept + (int64_t)blockIdx.x * a.keep;
     float* kw = a.kept_weights ? a.kept_weights + (int64_t)blockIdx.x * a.keep : nullptr;
-    const auto out = [&](int i, int j) {
-        kept[i] = j;
-        if (kw) kw[i] = w[j];
+    const auto out = [&](const int (&i)[4], uint32_t taken, int j) {
+        float v[4];   // the weights themselves: keys do not tell -0 from 0, nor one NaN from another
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = kw && taken >> x & 1u ? w[j + x] : 0.f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (taken >> x & 1u) {
+                kept[i[x]] = j + x;
+                if (kw) kw[i[x]] = v[x];
+            }
     };
     int total = n;
     if (n <= a.keep) {
-        for (int j = threadIdx.x; j < n; j += 1024) out(j, j);
+        for (int j = threadIdx.x; j < n; j += 1024) {
+            kept[j] = j;
+            if (kw) kw[j] = w[j];
+        }
     } else {
         const int lo = a.sink, hi = n - a.recent, need = a.keep - a.sink - a.recent;
         if (n <= N) {
@@ -398,10 +412,14 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
     const int64_t at = held - a.fresh + row % a.fresh;
     const int n = at >= 0 ? (int)(at >> a.shift) + 1 : 0;   // blocks up to the row's own
     int* chosen = a.chosen + (int64_t)blockIdx.x * a.count;
-    const auto out = [&](int i, int j) { chosen[i] = j; };
+    const auto out = [&](const int (&i)[4], uint32_t taken, int j) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (taken >> x & 1u) chosen[i[x]] = j + x;
+    };
     int total = n;
     if (n <= a.count) {
-        for (int j = threadIdx.x; j < n; j += THREADS) out(j, j);
+        for (int j = threadIdx.x; j < n; j += THREADS) chosen[j] = j;
     } else {
         const int lo = a.sink, hi = n - a.local, need = a.count - a.sink - a.local;
         uint64_t* keys = n <= N ? local_keys : a.keys + (int64_t)blockIdx.x * a.table_row;
