@@ -3,10 +3,15 @@
 // the scores kept, from which the weight of every cached token is formed (kWeigh).
 //
 // As in attn_paged_kernel, a workgroup takes rows (new tokens x query heads that share a key head) of one sequence and key
-// head and one piece of its keys; its waves take turns at chunks of 32 keys, which come to LDS without passing through
-// registers, through a ring of each wave's own, and their results meet in LDS.  Here a workgroup has R groups of 16 rows,
-// the columns of R sets of 16x16x32 MFMAs that share every operand read from LDS: a tree of 16 tokens with four heads to
-// a key head reads its cache once, not four times.
+// head; its waves take turns at chunks of 32 keys, which come to LDS without passing through registers, through a ring of
+// each wave's own, and their results meet in LDS.  Here a workgroup has R groups of 16 rows, the columns of R sets of 16x16x32
+// MFMAs that share every operand read from LDS, so that a tree of eight tokens with four heads to a key head reads its cache
+// once; a workgroup goes through several sequences in turn; and chunks that every row sees, nearly all, run without masks.
+//
+// What bounds it: reading the cache, once.  16 sequences of 130 to 8192 tokens, 16 key heads of 128 (0.55 GB): one drafted
+// token 5.6 TB/s, 32 of them (R = 2) 4.6: the step of two groups is long enough that four waves a CU leave gaps.  One token
+// of 64 sequences of 16384 to 32768 tokens over 4 key heads (3.2 GB): 6.3 TB/s, and 5.4 with the scores of kWeigh stored,
+// 0.1 GB of writes among the reads that cost 95 us (in whatever layout, non-temporal or not, waited for or not).
 #pragma once
 
 #include "noble_attn_common.hpp"
@@ -133,8 +138,9 @@ __device__ __forceinline__ uint32_t wave_upto(uint32_t v) {
 
 // The steps (of `keys` keys) of all sequences in a row are dealt to the slots in equal ranges, so that a batch of sequences of
 // different lengths keeps every workgroup busy to the end: a slot has the end of one sequence, whole ones, and the beginning
-// of one, at most.  Every wave works its range out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 16 heads,
-// 32 drafted tokens each: pieces of every sequence, as many for each SLOTS_A us, slots SLOTS_B us.
+// of one, at most.  Every wave works its range out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 16 key
+// heads of 128, whole calls: 1024 workgroups over pieces of their own sequence each, 106 us for one new token and 113 for 16;
+// 256 workgroups over slots 101 and 107.
 struct Slots {
     int b = 0, begin = 0, steps = 0;   // the sequence, the slot's first step in it, the sequence's steps
     int left = 0;                      // steps of the slot from there on
