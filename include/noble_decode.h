@@ -70,7 +70,7 @@ typedef struct noble_keep_desc {
     int64_t B;
     int64_t table_row;
     int64_t pages;
-    int64_t most;         /* up to table_row * page */
+    int64_t most;         /* up to 2^31 - 4096 */
     int32_t page;
     int32_t kv_heads, head_dim;
     int32_t kept_heads;

@@ -263,7 +263,7 @@ noble_status noble_cache_keep(const noble_keep_desc* desc, void* cache, const in
     if (d.reserved != 0 || d.B < 0 || d.B > kMaxRows || d.page < 8 || d.page > 4096 || (d.page & (d.page - 1)))
         return NOBLE_ERR_BAD_SHAPE;
     if (d.table_row < 0 || d.table_row > kMaxRows / d.page || d.pages < 0 || d.pages > INT32_MAX) return NOBLE_ERR_BAD_SHAPE;
-    if (d.most < 0 || d.most > d.table_row * d.page) return NOBLE_ERR_BAD_SHAPE;
+    if (d.most < 0 || d.most > kMaxRows) return NOBLE_ERR_BAD_SHAPE;
     if (d.kv_heads < 1 || d.kv_heads > kMaxHeads || !head_dim_ok(d.head_dim)) return NOBLE_ERR_BAD_SHAPE;
     if (d.kept_heads != 1 && d.kept_heads != d.kv_heads) return NOBLE_ERR_BAD_SHAPE;
     KeepArgs a{};

@@ -143,7 +143,7 @@ def _keep(**kw):
 
 def test_cache_keep():
     f = nd.lib().noble_cache_keep
-    for bad in (dict(B=-1), dict(table_row=-1), dict(pages=-1), dict(most=-1), dict(most=161), dict(page=4), dict(page=20),
+    for bad in (dict(B=-1), dict(table_row=-1), dict(pages=-1), dict(most=-1), dict(most=2 ** 31), dict(page=4), dict(page=20),
                 dict(kv_heads=0, kept_heads=0), dict(kept_heads=2), dict(kept_heads=0), dict(head_dim=12), dict(head_dim=256),
                 dict(reserved=1), dict(kv_heads=1025, kept_heads=1)):
         assert f(REF(_keep(**bad)), *FAKE[:4], None) == SHAPE, bad

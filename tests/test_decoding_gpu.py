@@ -245,6 +245,25 @@ def test_cache_keep_skips_what_is_not_there():
     assert _same(h.cache.cpu(), want)
 
 
+def test_lists_longer_than_the_sequences_may_be():
+    """Room for more tokens than the page table holds: the rest of the list is -1, and nothing moves there."""
+    h = _numbered(Held([40, 17], 2, 2, 64, 8, BF, 14, per=5))
+    w = torch.rand((2, 2, 40), generator=h.g, device="cuda")
+    before = h.cache.clone()
+    for keep, sink, recent in ((69, 4, 64), (300, 0, 0)):
+        kept, left = nd.noble_evict_select(w, h.len, keep, sink=sink, recent=recent)
+        for b, n in enumerate(h.lengths):
+            assert kept[b].tolist() == [list(range(n)) + [-1] * (keep - n)] * 2
+        nd.noble_cache_keep(h.cache, h.table, kept)
+        assert _same(h.cache, before)
+    kept[0, :, 3:40] = torch.arange(3, 40, device="cuda") + 20   # past the table from 40 on
+    nd.noble_cache_keep(h.cache, h.table, kept)
+    want = before.cpu()
+    table = h.table[0].tolist()
+    want[table] = ref.keep(before.cpu(), table, kept[0].tolist(), 0)[table]
+    assert _same(h.cache.cpu(), want)
+
+
 # ---------------------------------------------------------- selected pages --
 
 @pytest.mark.parametrize("K,D,page,dt", [(2, 128, 16, BF), (4, 80, 8, BF), (1, 8, 32, F32), (3, 64, 64, F32)])
