@@ -49,6 +49,9 @@ constexpr int64_t kMostNew = 1 << 20;
 // Workgroups that cache_keep_kernel is to have, at least.
 constexpr int64_t kMoving = 512;
 
+// Rows from which weigh_kernel splits them into slices.
+constexpr int kManyRows = 16, kManySlices = 16;
+
 // Workgroups of one attention call and its scratch.
 struct DecodePlan {
     int wide;                             // waves of attn_wide_kernel; 0: R groups of 16 rows of attn_decode_kernel
@@ -114,7 +117,7 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
         at += up256((size_t)all * 8);
         p->z = at;
         at += (size_t)all * p->chunks * kKeys * 4;
-        if (d->B * d->kv_heads * (p->chunks / 32 + 1) > kMaxGroups256) return NOBLE_ERR_BAD_SHAPE;
+        if (d->B * d->kv_heads * (p->chunks * kKeys / (1024 / kManySlices) + 1) > kMaxGroups256) return NOBLE_ERR_BAD_SHAPE;
     }
     p->bytes = at;
     return NOBLE_OK;
@@ -431,9 +434,12 @@ noble_status noble_attn_weigh(const noble_paged_desc* desc, const noble_heads* q
     const DecodeArgs a = decode_args(desc, p, q, cache, page_table, lengths, slopes, o, scratch);
     const hipStream_t st = (hipStream_t)stream;
     NOBLE_TRY(run_attention<kWeigh>(desc, p, a, st));
-    const WeighArgs w{a, weights, weights_out, cdiv(desc->table_row * desc->page, 1024), aligned16(weights) && aligned16(weights_out)};
+    const bool many = desc->new_tokens * a.share > kManyRows;
+    const WeighArgs w{a, weights, weights_out, cdiv(desc->table_row * desc->page, many ? 1024 / kManySlices : 1024),
+                      aligned16(weights) && aligned16(weights_out)};
     if (w.parts == 0) return NOBLE_OK;
-    return launch(weigh_kernel, dim3((unsigned)(desc->B * desc->kv_heads * w.parts)), dim3(256), st, w);
+    return launch(many ? weigh_kernel<kManySlices> : weigh_kernel<1>, dim3((unsigned)(desc->B * desc->kv_heads * w.parts)),
+                  dim3(256), st, w);
 }
 
 noble_status noble_evict_select(const noble_evict_desc* desc, const float* weights, const int32_t* lengths, int32_t* kept,

@@ -164,7 +164,8 @@ struct Slots {
         uint32_t total = __builtin_amdgcn_readlane(ones, 63);
         for (int64_t n = 64; n < a.B; n += 64)
             total += __builtin_amdgcn_readlane(wave_upto(steps_of(a, n + lane, keys)), 63);
-        const uint32_t used = min((uint32_t)a.slots, (total + least - 1) / least);
+        // short sequences side by side: 23 of up to 34 tokens, 7 drafted ones with 16 heads over 2, 37 us one after the other
+        const uint32_t used = min((uint32_t)a.slots, max((total + least - 1) / least, (uint32_t)a.B));
         if ((uint32_t)slot >= used) return;
         per = total / used;
         more = total - per * used;
@@ -668,7 +669,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
 }
 
 // The weight that every token received: of the rows that see it, exp2(score - maximum) / sum, added in the rows' order.  A
-// workgroup takes 1024 tokens of one sequence and key head, a thread four that follow each other.
+// thread takes four tokens that follow each other, and one of SLICES ranges of the rows, whose sums meet in LDS: 496 rows of
+// 388 tokens, 108 us with the attention for one range.
 struct WeighArgs {
     DecodeArgs a;
     const float* in;   // [B, kv_heads, table_row page], nullptr: nothing
@@ -676,41 +678,55 @@ struct WeighArgs {
     int parts;         // workgroups of one (sequence, key head)
     bool wide;         // in and out may be read and written 16 bytes at a time
 };
+template <int SLICES>
 __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs w) {
     const DecodeArgs& a = w.a;
+    constexpr int LANES = 256 / SLICES;
     const int head = blockIdx.x / w.parts, b = head / a.kv_heads;   // (sequence, key head)
     const int len = a.held(b), first = len - a.fresh, rows = a.fresh * a.share;
-    const int j = ((int)(blockIdx.x % w.parts) * 256 + (int)threadIdx.x) * 4;
-    if (j >= len) return;
+    const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
+    const int j0 = (int)(blockIdx.x % w.parts) * LANES * 4, j = j0 + lane * 4;
+    if (j0 >= len) return;
     const int64_t base = (int64_t)head * a.table_row * a.page + j;
     f32x4 old = {0.f, 0.f, 0.f, 0.f};
-    if (w.in && j < first) {
-        if (w.wide) old = *reinterpret_cast<const f32x4*>(w.in + base);   // rows are multiples of eight tokens
+    if (slice == 0 && w.in && j < first) {   // rows of weights are multiples of eight tokens
+        if (w.wide) old = *reinterpret_cast<const f32x4*>(w.in + base);
         else
 #pragma unroll
             for (int i = 0; i < 4; ++i) old[i] = w.in[base + i];
     }
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (a.there(b, j >> a.shift)) {
+    if (j < len && a.there(b, j >> a.shift)) {
         const float2* stats = a.stats + (int64_t)head * rows;
         const float* z = a.z + (((int64_t)head * a.chunks + j / kKeys) * rows) * kKeys + j % kKeys;
+        const int r1 = (int)((int64_t)rows * (slice + 1) / SLICES);
         constexpr int N = 8;   // rows whose scores are requested together
-        for (int r0 = 0; r0 < rows; r0 += N) {
+        for (int r0 = (int)((int64_t)rows * slice / SLICES); r0 < r1; r0 += N) {
             f32x4 v[N];
+            float2 st[N];
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < N; ++n) {
                 v[n] = *reinterpret_cast<const f32x4*>(z + (int64_t)min(r0 + n, rows - 1) * kKeys);
+                st[n] = stats[min(r0 + n, rows - 1)];
+            }
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int r = r0 + n;
-                if (r >= rows) break;
-                const float2 st = stats[r];
+                if (r >= r1) break;
                 const int at = first + r / a.share - j;   // of the four tokens, those up to it are seen
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] += i <= at ? __builtin_amdgcn_exp2f(v[n][i] - st.x) * st.y : 0.f;
+                for (int i = 0; i < 4; ++i) sum[i] += i <= at ? __builtin_amdgcn_exp2f(v[n][i] - st[n].x) * st[n].y : 0.f;
             }
         }
     }
+    if constexpr (SLICES > 1) {
+        __shared__ f32x4 sums[SLICES][LANES];
+        sums[slice][lane] = sum;
+        __syncthreads();
+        if (slice > 0) return;
+        for (int x = 1; x < SLICES; ++x) sum += sums[x][lane];
+    }
+    if (j >= len) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] += j + i < first ? old[i] : 0.f;
     if (w.wide && j + 4 <= len) {
