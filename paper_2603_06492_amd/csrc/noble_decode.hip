@@ -144,7 +144,6 @@ DecodeArgs decode_args(const noble_paged_desc* d, const DecodePlan& p, const nob
     a.shift = __builtin_ctz((unsigned)d->page);
     a.page_bytes = (int64_t)2 * d->kv_heads * d->page * d->head_dim * (int64_t)elt(d->dtype);
     a.fresh = d->new_tokens;
-    a.heads = d->heads;
     a.kv_heads = d->kv_heads;
     a.share = d->heads / d->kv_heads;
     a.D = d->head_dim;
@@ -324,7 +323,6 @@ noble_status noble_page_means(const noble_paged_desc* desc, const void* cache, c
     a.pages = desc->pages;
     a.fresh = desc->new_tokens;
     a.page = desc->page;
-    a.shift = __builtin_ctz((unsigned)desc->page);
     a.kv_heads = desc->kv_heads;
     a.D = desc->head_dim;
     return launch(desc->dtype == NOBLE_BF16 ? page_means_kernel<uint16_t> : page_means_kernel<float>,

@@ -29,7 +29,7 @@ struct DecodeArgs {
     float* part;          // [part][row tile][kv_heads][16 R][DP + 4] float32: product, maximum, sum
     int2* where;          // [B]: the slot that begins a sequence, and its pieces (kBlocks: [B fresh, kv_heads])
     int64_t table_row, pages, page_bytes;   // page_bytes: of one page, keys and values of all heads
-    int page, shift, fresh, heads, kv_heads, share, D;
+    int page, shift, fresh, kv_heads, share, D;
     int64_t B;
     int row_tiles, slots;   // slots: workgroups of one key head and row tile, for all sequences (kBlocks: for each list)
     ScoreArgs sc;

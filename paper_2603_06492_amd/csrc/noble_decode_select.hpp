@@ -95,7 +95,7 @@ struct PageArgs {
     const int* lengths;
     char* means;
     int64_t table_row, pages, fresh;
-    int page, shift, kv_heads, D, touched;   // touched: workgroups of one (sequence, key head)
+    int page, kv_heads, D, touched;   // touched: workgroups of one (sequence, key head)
     __device__ __forceinline__ int64_t held(int b) const { return min((int64_t)max(lengths[b], 0), table_row * page); }
 };
 

@@ -114,6 +114,9 @@ TREES = [   # lengths, n, H, K, D, page, dtype, softcap, bias
     ([140, 21, 20], 20, 8, 2, 128, 16, F32, 20.0, False),
     ([50], 1, 12, 4, 96, 128, F32, 0.0, False),
     ([33], 7, 64, 2, 40, 8, BF, 0.0, False),
+    ([2900, 1400], 6, 2, 1, 64, 16, BF, 0.0, True),
+    ([2000, 65], 40, 8, 2, 128, 64, BF, 30.0, True),
+    ([1800, 3], 3, 2, 1, 128, 8, F32, 0.0, True),
 ]
 
 
@@ -352,6 +355,8 @@ BLOCKS = [   # lengths, n, H, K, D, page, dtype, count, softcap, bias
     ([256, 255, 100], 3, 40, 2, 40, 32, BF, 5, 30.0, False),
     ([700], 1, 4, 2, 128, 64, F32, 7, 0.0, False),
     ([500, 129], 1, 2, 1, 96, 128, BF, 3, 0.0, True),
+    ([2000, 900], 2, 40, 2, 64, 32, BF, 45, 0.0, False),
+    ([1500], 1, 2, 1, 128, 16, BF, 80, 0.0, True),
 ]
 
 
@@ -412,6 +417,8 @@ WEIGHS = [   # lengths, n, H, K, D, page, dtype, softcap, bias
     ([97, 30], 13, 4, 2, 64, 16, F32, 0.0, True),
     ([140, 21, 20], 5, 8, 2, 128, 16, F32, 20.0, False),
     ([333], 333, 2, 1, 32, 64, F32, 0.0, False),
+    ([300, 150], 150, 2, 1, 64, 16, BF, 20.0, True),
+    ([2500, 1300], 1, 4, 1, 128, 16, BF, 0.0, True),
 ]
 
 
