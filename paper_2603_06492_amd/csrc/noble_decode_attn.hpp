@@ -700,19 +700,20 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs w) {
         const float2* stats = a.stats + (int64_t)head * rows;
         const float* z = a.z + (((int64_t)head * a.chunks + j / kKeys) * rows) * kKeys + j % kKeys;
         const int r1 = (int)((int64_t)rows * (slice + 1) / SLICES);
-        constexpr int N = 8;   // rows whose scores are requested together
+        constexpr int N = SLICES > 1 ? 8 : 4;   // rows whose scores are requested together
         for (int r0 = (int)((int64_t)rows * slice / SLICES); r0 < r1; r0 += N) {
             f32x4 v[N];
             float2 st[N];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 v[n] = *reinterpret_cast<const f32x4*>(z + (int64_t)min(r0 + n, rows - 1) * kKeys);
-                st[n] = stats[min(r0 + n, rows - 1)];
+                if (SLICES > 1) st[n] = stats[min(r0 + n, rows - 1)];   // else one row for the whole wave, read where it is used
             }
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int r = r0 + n;
                 if (r >= r1) break;
+                if (SLICES == 1) st[n] = stats[r];
                 const int at = first + r / a.share - j;   // of the four tokens, those up to it are seen
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] += i <= at ? __builtin_amdgcn_exp2f(v[n][i] - st[n].x) * st[n].y : 0.f;
