@@ -140,7 +140,8 @@ noble_status noble_attn_blocks(const noble_paged_desc* desc, int32_t count,
  * p being the rows' softmax; for the new tokens themselves the sum alone, so
  * what weights held there does not matter.  float32 [B, kv_heads, table_row *
  * page]; weights may be weights_out, or NULL: nothing yet.  Entries past a
- * sequence's tokens are not written. */
+ * sequence's tokens are not written.  The scratch holds the rows' scores, 4
+ * bytes for each row, query head and token of the page table. */
 noble_status noble_attn_weigh_scratch_size(const noble_paged_desc* desc,
                                            size_t* scratch_bytes);
 noble_status noble_attn_weigh(const noble_paged_desc* desc, const noble_heads* q,

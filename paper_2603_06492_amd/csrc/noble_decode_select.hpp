@@ -283,9 +283,12 @@ struct Pick {
             sum = __popcll(b0) + 2 * __popcll(b1) + 4 * __popcll(b2);
         };
         uint32_t na = 0, ne = 0, unused, c;
-        for (int j = j0; j < j1; j += 256) {
+        uint64_t states = 0;   // of the first eight steps, all there are where LDS holds the keys of a wave's range
+        int step = 0;
+        for (int j = j0; j < j1; j += 256, ++step) {
             uint32_t u, e;
             state(j + 4 * lane, u, e);
+            states |= step < 8 ? (uint64_t)(u | e << 4) << (8 * step) : 0ull;
             add(__popc(u), unused, c);
             na += c;
             add(__popc(e), unused, c);
@@ -304,9 +307,15 @@ struct Pick {
             all += above[x];
             every += equal[x];
         }
-        for (int j = j0; j < j1; j += 256) {
+        step = 0;
+        for (int j = j0; j < j1; j += 256, ++step) {
             uint32_t u, e, ua, ea, us, es;
-            state(j + 4 * lane, u, e);
+            if (step < 8) {
+                u = (uint32_t)(states >> (8 * step)) & 15u;
+                e = (uint32_t)(states >> (8 * step + 4)) & 15u;
+            } else {
+                state(j + 4 * lane, u, e);
+            }
             add(__popc(u), ua, us);
             add(__popc(e), ea, es);
             ua += at;
@@ -339,8 +348,8 @@ struct EvictArgs {
 };
 
 // One workgroup a sequence and key head.  LDS holds the weights of up to N tokens; longer rows are read again each time.  Bound
-// by its passes over LDS: 256 rows of 4096 weights 10 us, of 32768 40 us, of which reading them from memory is 6; of equal
-// weights, whose counts all fall into one, 19 and 111.
+// by its passes over LDS and by additions to the same count: 256 rows of 4096 weights 10 us, of 32768 39 us, of which reading
+// them from memory is 6; of equal weights, whose counts all fall into one, 19 and 109.
 template <int N>
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t keys[N];
