@@ -77,7 +77,7 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
     // where once is not near.
     const auto filling = [&](int64_t one, int64_t most) {
         int64_t slots = 1;
-        double best = 0.0;
+        double best = -1.0;
         for (int64_t turn = 1; turn <= 4 && one > 0; ++turn) {
             const int64_t n = std::clamp<int64_t>(resident * turn / one, 1, most), all = n * one;
             const double fill = (double)all / (double)((all + resident - 1) / resident * resident);
@@ -184,7 +184,12 @@ noble_status run_attention(const noble_paged_desc* d, const DecodePlan& p, const
                          p.wide == 8 ? WideShape<DP, 8>::LDS : p.wide ? WideShape<DP, 4>::LDS : DecodeShape<E, DP>::LDS));
         if (!p.split) return NOBLE_OK;
         const DecodeJoinArgs j{a, d->B * d->new_tokens * d->heads, (int)p.R};
-        return launch(decode_join_kernel<E, DP, FORM>, dim3((unsigned)cdiv(j.items, 256 / (DP / 4))), dim3(256), st, j);
+        // rows of more pieces than a set of lanes has in flight: a set for every eighth of them
+        const bool many = p.slots > 8 * (FORM == kBlocks ? 1 : d->B);
+        constexpr int rows = 256 / (DP / 4);   // of a workgroup, one set of lanes each
+        return many ? launch(decode_join_kernel<E, DP, FORM, kJoinSlices>, dim3((unsigned)cdiv(j.items, rows / kJoinSlices)),
+                             dim3(256), st, j)
+                    : launch(decode_join_kernel<E, DP, FORM, 1>, dim3((unsigned)cdiv(j.items, rows)), dim3(256), st, j);
     });
 }
 

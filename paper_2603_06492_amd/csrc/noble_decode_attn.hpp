@@ -603,20 +603,22 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES), (sizeof(E) * DP >
     }
 }
 
-// Joins the pieces of every row, in their order.  A row's DP / 4 lanes each take four elements.  kWeigh: and keeps the rows'
-// maxima and sums for weigh_kernel.
+// Joins the pieces of every row, in their order.  A row's DP / 4 lanes each take four elements; of rows with many pieces, that
+// many in each of SLICES sets of lanes, whose sums meet in LDS in the sets' order (one token after 32768, 4 key heads, 64
+// pieces, the whole call: 28 us for one set, 21 for eight).  kWeigh: and keeps the rows' maxima and sums for weigh_kernel.
 struct DecodeJoinArgs {
     DecodeArgs a;
     int64_t items;   // rows of all heads
     int groups;      // R
 };
-template <typename E, int DP, int FORM>
+constexpr int kJoinSlices = 8;
+template <typename E, int DP, int FORM, int SLICES>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
     const DecodeArgs& a = j.a;
-    constexpr int LANES = DP / 4, LD = DP + 4;
-    const int64_t item = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-    if (item >= j.items) return;
-    const int d = threadIdx.x % LANES * 4, rows = a.fresh * a.share;
+    constexpr int LANES = DP / 4, LD = DP + 4, ITEMS = 256 / LANES / SLICES;
+    const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES % SLICES;
+    const int64_t here = (int64_t)blockIdx.x * ITEMS + threadIdx.x / LANES / SLICES, item = min(here, j.items - 1);
+    const int d = lane * 4, rows = a.fresh * a.share;
     const int row = (int)(item % rows), kv = (int)(item / rows % a.kv_heads), b = (int)(item / rows / a.kv_heads);
     const int tok = row / a.share, in_tok = row - tok * a.share;
     int rt, slot;   // the row's tile and place in it
@@ -629,7 +631,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
     }
     const int2 where = a.where[FORM == kBlocks ? ((int64_t)b * a.fresh + tok) * a.kv_heads + kv : b];
     const int pieces = where.y;
-    if (pieces == 1) return;
+    const bool mine = here < j.items && pieces > 1;
+    if (SLICES == 1 && !mine) return;
     const int64_t tile = (int64_t)j.groups * kGroup * LD, step = (int64_t)a.row_tiles * a.kv_heads * tile;   // from piece to piece
     // piece n of a list is part n from its first on; of a sequence, its first piece is its slot's second part, the others the
     // next slots' first ones
@@ -640,14 +643,15 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
     constexpr int N = 8;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     float total = 0.f, top = -INFINITY;
-    for (int x0 = 0; x0 < pieces; x0 += N) {
+    const int n0 = pieces * slice / SLICES, n1 = mine ? pieces * (slice + 1) / SLICES : 0;
+    for (int x0 = n0; x0 < n1; x0 += N) {
         f32x4 v[N];
         float m[N], l[N], next = top;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const float* q = at(min(x0 + n, pieces - 1));
+            const float* q = at(min(x0 + n, n1 - 1));
             v[n] = *reinterpret_cast<const f32x4*>(q + d);
-            m[n] = x0 + n < pieces ? q[DP] : -INFINITY;
+            m[n] = x0 + n < n1 ? q[DP] : -INFINITY;
             l[n] = q[DP + 1];
         }
 #pragma unroll
@@ -658,10 +662,29 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
         top = next;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            if (x0 + n >= pieces) break;
+            if (x0 + n >= n1) break;
             const float f = __builtin_amdgcn_exp2f(m[n] - base);
             sum += v[n] * f;
             total += l[n] * f;
+        }
+    }
+    if constexpr (SLICES > 1) {
+        __shared__ f32x4 sums[256];
+        __shared__ float2 stats[256];
+        sums[threadIdx.x] = sum;
+        stats[threadIdx.x] = make_float2(top, total);
+        __syncthreads();
+        if (slice > 0 || !mine) return;
+        for (int x = 1; x < SLICES; ++x) top = fmaxf(top, stats[threadIdx.x + x * LANES].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        sum = {0.f, 0.f, 0.f, 0.f};
+        total = 0.f;
+#pragma unroll
+        for (int x = 0; x < SLICES; ++x) {
+            const float2 one = stats[threadIdx.x + x * LANES];
+            const float f = __builtin_amdgcn_exp2f(one.x - base);
+            sum += sums[threadIdx.x + x * LANES] * f;
+            total += one.y * f;
         }
     }
     if (FORM == kWeigh && d == 0) a.stats[item] = make_float2(top, 1.f / total);

@@ -228,6 +228,43 @@ def test_more_sequences_than_slots_and_lanes():
         assert abs(float(w.double().sum()) - total) < 1e-4 * total
 
 
+@pytest.mark.parametrize("lengths,n,H,K,D,dt", [([9001], 1, 4, 4, 128, BF), ([8200, 300], 3, 4, 2, 64, BF), ([5000], 2, 3, 1, 80, F32),
+                                                ([4100, 0], 5, 1, 1, 64, F32), ([6500], 12, 4, 1, 128, BF), ([7000], 70, 2, 1, 64, BF)],
+                         ids=["9001-1", "8200-3", "5000-2-f32", "4100-5-f32", "6500-48rows", "7000-140rows"])
+def test_rows_of_many_pieces(lengths, n, H, K, D, dt):
+    """Few long sequences, whose rows are put together from dozens of pieces: pieces without a page, and values that are no
+    numbers in the first, in one between and in the last, for the rows that see them."""
+    u = U16 if dt == BF else U32
+    for spoiled in (False, True):
+        h = Held(lengths, H, K, D, 16, dt, 97 + n)
+        rows = h.table.tolist()
+        if spoiled:
+            h.table[0, 20:200] = -1
+            h.cache[rows[0][0], 1, 0, 3, 1] = math.inf
+            h.cache[rows[0][-40], 1, K - 1, 7, 5] = math.nan
+            h.cache[rows[0][(lengths[0] - 1) // 16], 1, 0, (lengths[0] - 1) % 16, 0] = -math.inf   # its own row's alone
+        q, parents = h.q(n), _trees(random.Random(n), len(lengths), n, 0.0)
+        seen, depths, _ = nd.noble_tree_rows(_ints(parents), h.len)
+        t = nd.noble_attn_tree(q, *h.args(), seen, depths)
+        o, w = nd.noble_attn_weigh(q, *h.args())
+        blocks = max(lengths) // 16
+        lists = [[[j for j in range(max(0, x - n + i) // 16 + 1) if j % 3] for _ in range(K)] if x else [[]] * K
+                 for x in lengths for i in range(n)]
+        chosen = torch.tensor([[(x + [-1] * blocks)[:blocks] for x in y] for y in lists], dtype=torch.int32)
+        s = nd.noble_attn_blocks(q, *h.args(), chosen.cuda())
+        for b, cache, table, length in h.each():
+            mine = slice(b * n, (b + 1) * n)
+            want, mag, _, _ = ref.tree(q[mine].cpu(), cache, table, length, parents[b])
+            _near("tree", t[mine], want, mag, u)
+            want, mag, ww, size = ref.weigh(q[mine].cpu(), cache, table, length)
+            _near("o", o[mine], want, mag, u)
+            # as for the weights of shorter sequences: two scores' roundings, and one for every term of the sum
+            terms = (2 * (D + 3) * float(size.max() if size.numel() else 0) + 16 + n * H // K) * 2.0 ** -24
+            _near("weights", w[b, :, :ww.shape[1]], ww, torch.zeros_like(ww), terms)
+            want, mag, _, _ = ref.blocks(q[mine].cpu(), cache, table, length, chosen[mine])
+            _near("blocks", s[mine], want, mag, u)
+
+
 def test_rows_of_minus_infinity_and_large_scores():
     """Scores that are all minus infinity give NaN, as the formula does; scores of thousands neither overflow nor lose the
     largest."""
