@@ -164,19 +164,38 @@ __global__ __launch_bounds__(256) void page_means_kernel(PageArgs a) {
 
 // -------------------------------------------------------------- selection --
 
-// The sum of eight lanes' values, or sixteen's, in each of them: exchanges inside a row of 16 lanes.
-__device__ __forceinline__ double lanes_sum(double x, bool sixteen) {
-    const auto add = [&](auto ctrl) {
-        const uint64_t u = (uint64_t)__double_as_longlong(x);
-        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, 0xf, 0xf, false);
-        const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
-        return x + __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
-    };
-    x = add(std::integral_constant<int, 0xb1>{});    // quad_perm: lanes 1, 0, 3, 2
-    x = add(std::integral_constant<int, 0x4e>{});    // 2, 3, 0, 1
-    x = add(std::integral_constant<int, 0x141>{});   // row_half_mirror
-    if (sixteen) x = add(std::integral_constant<int, 0x140>{});   // row_mirror
-    return x;
+// A lane's value from the lane that a DPP control pairs it with.
+template <int CTRL>
+__device__ __forceinline__ double from_pair(double x) {
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, 0xf, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, false);
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+// Of 2 N sums a lane keeps half, the upper one if `upper`, and gives its pair, which keeps the other, the rest.
+template <int CTRL, int N>
+__device__ __forceinline__ void halve(double* s, bool upper) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const double mine = upper ? s[N + i] : s[i], other = upper ? s[i] : s[N + i];
+        s[i] = mine + from_pair<CTRL>(other);
+    }
+}
+// Eight sums over eight lanes, or sixteen, with 7 additions (8) in a lane where each by itself takes 24 (32): returns that of
+// place `which`, a lane's own.  All are added in one order, so that equal blocks have equal sums.
+__device__ __forceinline__ double lanes_sums(double (&s)[8], int x, bool sixteen, int& which) {
+    if (sixteen) {
+        halve<0x140, 4>(s, x & 8);   // row_mirror: lanes i and 15 - i
+        halve<0x141, 2>(s, x & 4);   // row_half_mirror: i and 7 - i
+        halve<0x4e, 1>(s, x & 2);    // quad_perm: i and i ^ 2
+        which = x >> 1;
+        return s[0] + from_pair<0xb1>(s[0]);   // i and i ^ 1
+    }
+    halve<0x141, 4>(s, x & 4);
+    halve<0x4e, 2>(s, x & 2);
+    halve<0xb1, 1>(s, x & 1);
+    which = x;
+    return s[0];
 }
 
 // Whole numbers in the order of the values, NaN above all, -0 with 0.
@@ -456,27 +475,33 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
             // eight blocks at a time: their pages, then their means, all in flight
             constexpr int U = 8;
             const int step = THREADS / lanes;
+            const uint32_t stride = (uint32_t)(a.kv_heads * a.D * ES);   // from a page's mean to the next one's
+            const char* means = a.means + (kv * a.D + 8 * x) * ES;
             for (int j0 = lo + g; j0 < hi; j0 += U * step) {
                 int page[U];
+                uint32_t there = 0;   // a bit each
                 Frag<E> mean[U];
 #pragma unroll
                 for (int n = 0; n < U; ++n) page[n] = j0 + n * step < hi ? a.table[b * a.table_row + j0 + n * step] : -1;
 #pragma unroll
                 for (int n = 0; n < U; ++n) {
-                    if (page[n] >= a.pages) page[n] = -1;
-                    mean[n] = global_frag<E>(a.means + (((int64_t)max(page[n], 0) * a.kv_heads + kv) * a.D + 8 * x) * ES,
-                                             page[n] >= 0 && in);
+                    const bool ok = page[n] >= 0 && page[n] < a.pages;
+                    there |= (uint32_t)ok << n;
+                    mean[n] = global_frag<E>(means + (uint64_t)(ok ? (uint32_t)page[n] : 0u) * stride, in && a.pages > 0);
                 }
+                double s[U];
 #pragma unroll
                 for (int n = 0; n < U; ++n) {
                     float v[8];
                     elements8(mean[n], v);
-                    double s = 0.0;
+                    s[n] = 0.0;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s = fma(q[i], (double)v[i], s);
-                    s = lanes_sum(s, lanes == 16);
-                    if (x == 0 && j0 + n * step < hi) keys[j0 + n * step] = ordered(page[n] >= 0 ? s : -(double)INFINITY);
+                    for (int i = 0; i < 8; ++i) s[n] = fma(q[i], (double)v[i], s[n]);
                 }
+                int n;
+                const double sum = lanes_sums(s, x, lanes == 16, n);
+                const int j = j0 + n * step;
+                if (j < hi) keys[j] = ordered(there >> n & 1u ? sum : -(double)INFINITY);
             }
             __syncthreads();
         }
