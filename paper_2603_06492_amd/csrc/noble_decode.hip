@@ -205,10 +205,19 @@ noble_status check_select(const noble_paged_desc* d, const noble_select_desc* s)
 // Blocks whose scores LDS holds: those of a sequence of up to table_row pages.
 constexpr int64_t kFewestBlocks = 256, kFewBlocks = 2048, kManyBlocks = 16384;
 
+// Few rows (times key heads) of many blocks each: workgroups of kScored blocks form their scores in a launch before the
+// selection's.  One row of 4 key heads of 128 over 512, 2048 and 16250 blocks 10.7 -> 9.6, 20 -> 11 and 118 -> 30 us; 32 rows
+// over 1023 16 -> 17, over 4092 49 -> 42.
+bool scored_apart(const noble_paged_desc* d) {
+    const int64_t rows = d->B * d->new_tokens * d->kv_heads;
+    return d->table_row >= 512 && rows <= std::min<int64_t>(d->table_row / 16, 128) &&
+           rows * cdiv(d->table_row, kScored) <= kMaxGroups256;
+}
+
 noble_status select_scratch(const noble_paged_desc* d, size_t* bytes) {
     const int64_t rows = d->B * d->new_tokens * d->kv_heads;
     *bytes = 0;
-    if (d->table_row <= kManyBlocks) return NOBLE_OK;
+    if (d->table_row <= kManyBlocks && !scored_apart(d)) return NOBLE_OK;
     if (rows > kMaxScratch / 8 / d->table_row) return NOBLE_ERR_BAD_SHAPE;
     *bytes = (size_t)rows * d->table_row * 8;
     return NOBLE_OK;
@@ -379,7 +388,9 @@ noble_status noble_block_select(const noble_paged_desc* desc, const noble_select
     a.local = select->local;
     const dim3 grid((unsigned)(rows * desc->kv_heads));
     const hipStream_t st = (hipStream_t)stream;
+    if (scored_apart(desc)) a.parts = cdiv(desc->table_row, kScored);
     const auto run = [&]<typename E>() {
+        if (a.parts) NOBLE_TRY(launch(block_keys_kernel<E>, dim3(grid.x * (unsigned)a.parts), dim3(256), st, a));
         if (desc->table_row <= kFewestBlocks) return launch(block_select_kernel<E, kFewestBlocks, 256>, grid, dim3(256), st, a);
         return desc->table_row <= kFewBlocks ? launch(block_select_kernel<E, kFewBlocks, 1024>, grid, dim3(1024), st, a)
                                              : launch(block_select_kernel<E, kManyBlocks, 1024>, grid, dim3(1024), st, a);

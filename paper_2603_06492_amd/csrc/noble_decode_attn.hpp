@@ -603,8 +603,8 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES), (sizeof(E) * DP >
     }
 }
 
-// Joins the pieces of every row, in their order.  A row's DP / 4 lanes each take four elements; of rows with many pieces, that
-// many in each of SLICES sets of lanes, whose sums meet in LDS in the sets' order (one token after 32768, 4 key heads, 64
+// Joins the pieces of every row, in their order.  A row's DP / 4 lanes each take four elements; the pieces of rows with many are
+// dealt to SLICES sets of such lanes, whose sums meet in LDS in the sets' order (one token after 32768, 4 key heads, 64
 // pieces, the whole call: 28 us for one set, 21 for eight).  kWeigh: and keeps the rows' maxima and sums for weigh_kernel.
 struct DecodeJoinArgs {
     DecodeArgs a;

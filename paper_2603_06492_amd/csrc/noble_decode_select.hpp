@@ -425,24 +425,91 @@ struct SelectArgs {
     const int* table;
     const int* lengths;
     int* chosen;
-    uint64_t* keys;     // [B fresh, kv_heads, table_row] where LDS does not hold them
+    uint64_t* keys;     // [B fresh, kv_heads, table_row] where LDS does not hold them, or other workgroups form them
     int64_t table_row, pages;
     int page, shift, fresh, kv_heads, share, D, count, sink, local;
+    int parts;          // workgroups that form a row's keys, 0: the one that selects
+
+    // Blocks up to the row's own.
+    __device__ __forceinline__ int blocks(int row) const {
+        const int64_t held = min((int64_t)max(lengths[row / fresh], 0), table_row * page), at = held - fresh + row % fresh;
+        return at >= 0 ? (int)(at >> shift) + 1 : 0;
+    }
 };
+
+// keys[lo .. hi - 1] of a row and key head, eight elements of a mean a lane.
+template <typename E, int THREADS>
+__device__ __forceinline__ void block_keys(const SelectArgs& a, int row, int kv, int lo, int hi, uint64_t* keys) {
+    const int ES = (int)sizeof(E), lanes = a.D <= 64 ? 8 : 16;
+    const int x = threadIdx.x % lanes, g = threadIdx.x / lanes;
+    const bool in = 8 * x < a.D;
+    double q[8] = {};
+    const char* qp = a.q.ptr + (int64_t)row * a.q.row + (int64_t)kv * a.share * a.q.head + 8 * x * ES;
+    for (int h0 = 0; h0 < a.share; h0 += 4) {
+        Frag<E> f[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) f[h] = global_frag<E>(qp + (h0 + h) * a.q.head, in && h0 + h < a.share);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float v[8];
+            elements8(f[h], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] += (double)v[i];
+        }
+    }
+    // eight blocks at a time: their pages, then their means, all in flight
+    constexpr int U = 8;
+    const int step = THREADS / lanes;
+    const uint32_t stride = (uint32_t)(a.kv_heads * a.D * ES);   // from a page's mean to the next one's
+    const char* means = a.means + (kv * a.D + 8 * x) * ES;
+    for (int j0 = lo + g; j0 < hi; j0 += U * step) {
+        int page[U];
+        uint32_t there = 0;   // a bit each
+        Frag<E> mean[U];
+#pragma unroll
+        for (int n = 0; n < U; ++n) page[n] = j0 + n * step < hi ? a.table[(int64_t)(row / a.fresh) * a.table_row + j0 + n * step] : -1;
+#pragma unroll
+        for (int n = 0; n < U; ++n) {
+            const bool ok = page[n] >= 0 && page[n] < a.pages;
+            there |= (uint32_t)ok << n;
+            mean[n] = global_frag<E>(means + (uint64_t)(ok ? (uint32_t)page[n] : 0u) * stride, in && a.pages > 0);
+        }
+        double s[U];
+#pragma unroll
+        for (int n = 0; n < U; ++n) {
+            float v[8];
+            elements8(mean[n], v);
+            s[n] = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[n] = fma(q[i], (double)v[i], s[n]);
+        }
+        int n;
+        const double sum = lanes_sums(s, x, lanes == 16, n);
+        const int j = j0 + n * step;
+        if (j < hi) keys[j] = ordered(there >> n & 1u ? sum : -(double)INFINITY);
+    }
+}
+
+constexpr int kScored = 128;   // blocks of a workgroup
+// The keys of a row's blocks by several workgroups, for block_select_kernel to select from (see scored_apart).
+template <typename E>
+__global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a) {
+    const int list = blockIdx.x / a.parts, row = list / a.kv_heads, n = a.blocks(row);
+    const int hi = n - a.local, j0 = a.sink + (int)(blockIdx.x % a.parts) * kScored;
+    if (n <= a.count || j0 >= hi) return;
+    block_keys<E, 256>(a, row, list % a.kv_heads, j0, min(j0 + kScored, hi), a.keys + (int64_t)list * a.table_row);
+}
 
 // One workgroup a row and key head: the scores of the row's blocks, eight elements a lane, then the selection.  LDS holds the
 // scores of up to N blocks; those of longer sequences lie in global memory.  Bound by latencies in a row (length, page, mean,
-// then some seven barriers): 512 blocks of heads of 128, 12 us for one row of 4 key heads, 15 for 64 (with the means read one
-// at a time 18 and 28).
+// then some seven barriers) and by float64's arithmetic: 512 blocks of heads of 128, 10 us for one row of 4 key heads, 14 for
+// 64 (with the means read one at a time 18 and 28, each block's sum over the lanes by itself 11 and 15; with the next means
+// under way during the sums 12.7 and 16).
 template <typename E, int N, int THREADS>
 __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
     __shared__ __attribute__((aligned(16))) uint64_t local_keys[N];
     __shared__ Pick<uint64_t, THREADS> pick;
-    const int ES = (int)sizeof(E), lanes = a.D <= 64 ? 8 : 16;
-    const int kv = blockIdx.x % a.kv_heads, row = blockIdx.x / a.kv_heads, b = row / a.fresh;
-    const int64_t held = min((int64_t)max(a.lengths[b], 0), a.table_row * a.page);
-    const int64_t at = held - a.fresh + row % a.fresh;
-    const int n = at >= 0 ? (int)(at >> a.shift) + 1 : 0;   // blocks up to the row's own
+    const int kv = blockIdx.x % a.kv_heads, row = blockIdx.x / a.kv_heads, n = a.blocks(row);
     int* chosen = a.chosen + (int64_t)blockIdx.x * a.count;
     const auto out = [&](const int (&i)[4], uint32_t taken, int j) {
 #pragma unroll
@@ -456,53 +523,9 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
         const int lo = a.sink, hi = n - a.local, need = a.count - a.sink - a.local;
         uint64_t* keys = n <= N ? local_keys : a.keys + (int64_t)blockIdx.x * a.table_row;
         if (need > 0) {
-            const int x = threadIdx.x % lanes, g = threadIdx.x / lanes;
-            const bool in = 8 * x < a.D;
-            double q[8] = {};
-            const char* qp = a.q.ptr + (int64_t)row * a.q.row + (int64_t)kv * a.share * a.q.head + 8 * x * ES;
-            for (int h0 = 0; h0 < a.share; h0 += 4) {
-                Frag<E> f[4];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) f[h] = global_frag<E>(qp + (h0 + h) * a.q.head, in && h0 + h < a.share);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    float v[8];
-                    elements8(f[h], v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) q[i] += (double)v[i];
-                }
-            }
-            // eight blocks at a time: their pages, then their means, all in flight
-            constexpr int U = 8;
-            const int step = THREADS / lanes;
-            const uint32_t stride = (uint32_t)(a.kv_heads * a.D * ES);   // from a page's mean to the next one's
-            const char* means = a.means + (kv * a.D + 8 * x) * ES;
-            for (int j0 = lo + g; j0 < hi; j0 += U * step) {
-                int page[U];
-                uint32_t there = 0;   // a bit each
-                Frag<E> mean[U];
-#pragma unroll
-                for (int n = 0; n < U; ++n) page[n] = j0 + n * step < hi ? a.table[b * a.table_row + j0 + n * step] : -1;
-#pragma unroll
-                for (int n = 0; n < U; ++n) {
-                    const bool ok = page[n] >= 0 && page[n] < a.pages;
-                    there |= (uint32_t)ok << n;
-                    mean[n] = global_frag<E>(means + (uint64_t)(ok ? (uint32_t)page[n] : 0u) * stride, in && a.pages > 0);
-                }
-                double s[U];
-#pragma unroll
-                for (int n = 0; n < U; ++n) {
-                    float v[8];
-                    elements8(mean[n], v);
-                    s[n] = 0.0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[n] = fma(q[i], (double)v[i], s[n]);
-                }
-                int n;
-                const double sum = lanes_sums(s, x, lanes == 16, n);
-                const int j = j0 + n * step;
-                if (j < hi) keys[j] = ordered(there >> n & 1u ? sum : -(double)INFINITY);
-            }
+            if (!a.parts) block_keys<E, THREADS>(a, row, kv, lo, hi, keys);
+            else if (n <= N)
+                for (int j = lo + threadIdx.x; j < hi; j += THREADS) local_keys[j] = a.keys[(int64_t)blockIdx.x * a.table_row + j];
             __syncthreads();
         }
         // two copies, so that the one over LDS is compiled for it

@@ -184,6 +184,18 @@ def test_block_select():
     assert size(REF(_desc()), REF(e), None) == NULL and size(None, REF(e), REF(n)) == NULL
 
 
+def test_block_select_scratch_of_few_rows_and_many():
+    """Few rows of many blocks take scratch for their scores; many rows, or few blocks, take none."""
+    f, size, n = nd.lib().noble_block_select, nd.lib().noble_block_select_scratch_size, ctypes.c_size_t(7)
+    q, e = _heads(FAKE[10]), nd.noble_select_desc(6, 1, 2, 0)
+    for row, B, some in ((511, 3, 0), (512, 3, 1), (640, 3, 1), (640, 50, 0), (16384, 3, 1), (16384, 50, 0)):
+        d = _desc(table_row=row, B=B)
+        assert size(REF(d), REF(e), REF(n)) == 0 and n.value == some * B * 4 * 2 * row * 8, (row, B)
+        if some:
+            assert f(REF(d), REF(e), REF(q), *FAKE[:4], FAKE[20], n.value - 1, None) == WS
+            assert f(REF(d), REF(e), REF(q), *FAKE[:4], None, n.value, None) == NULL
+
+
 def test_evict_select():
     f = nd.lib().noble_evict_select
     make = lambda B=2, row=100, heads=4, keep=10, sink=1, recent=2, r=(0, 0): nd.noble_evict_desc(B, row, heads, keep, sink, recent, r)  # noqa: E731

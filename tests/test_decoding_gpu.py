@@ -348,6 +348,29 @@ def test_block_select_of_long_sequences(blocks):
     assert got.cpu().tolist() == want.tolist()
 
 
+@pytest.mark.parametrize("B,n,H,K,D,dt,count,sink,local", [
+    (3, 2, 4, 2, 128, BF, 40, 2, 3), (20, 2, 4, 2, 128, BF, 40, 2, 3), (3, 1, 2, 1, 40, F32, 300, 0, 1), (45, 1, 2, 1, 64, F32, 6, 5, 1),
+    (2, 3, 6, 3, 72, BF, 130, 127, 2)], ids=str)
+def test_block_select_by_one_workgroup_or_several(B, n, H, K, D, dt, count, sink, local):
+    """Rows over hundreds of blocks, few and many; equal blocks far apart, pages that are none, shorter sequences."""
+    page, per = 8, 640
+    g = _gen(B + D)
+    lengths = [(per * page, per * page - 5, 300 * page + 1, count * page, 1023, 1)[b % 6] for b in range(B)]
+    table = torch.randperm(B * per, generator=g, device="cuda").view(B, per).to(torch.int32)
+    table[:, 30:600:7] = table[:, 20:21]           # one page many times: the first of them are taken
+    table[:, 33] = -1
+    table[:, 450] = B * per
+    means = torch.randn((B * per, K, D), generator=g, device="cuda").to(dt)
+    means[table[:, 20].long()] = means[table[:, 20].long()].abs() * 3
+    q = torch.randn((B * n, H, D), generator=g, device="cuda").abs().to(dt)
+    got = nd.noble_block_select(q, means, table, _ints(lengths), count, page=page, sink=sink, local=local).cpu()
+    rows = table.tolist()
+    for b in list(range(min(B, 6))) + [B - 1]:
+        mine = slice(b * n, (b + 1) * n)
+        want = ref.select(q[mine].cpu(), means.cpu(), rows[b], lengths[b], n, count, page, sink, local)
+        assert got[mine].tolist() == want.tolist(), b
+
+
 BLOCKS = [   # lengths, n, H, K, D, page, dtype, count, softcap, bias
     ([1000, 30, 0, 517], 1, 8, 2, 128, 8, BF, 20, 0.0, False),
     ([300, 64, 2], 5, 4, 4, 64, 16, BF, 9, 0.0, True),
