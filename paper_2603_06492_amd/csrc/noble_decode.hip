@@ -64,8 +64,13 @@ struct DecodePlan {
 template <int FORM>
 noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p) {
     const int64_t share = d->heads / d->kv_heads, rows = d->new_tokens * share;
-    p->wide = FORM == kBlocks || d->dtype != NOBLE_BF16 || rows <= 2 * kGroup ? 0 : rows > 128 ? 8 : 4;
-    p->R = p->wide ? 32 * p->wide / kGroup : FORM != kBlocks && rows > kGroup ? 2 : 1;
+    // Little work, up to eight chunks for each wave of 256 workgroups of one group of rows, is latencies and code that runs once:
+    // one group a workgroup, for all that the cache is read again.  47 trees of 8 with 8 heads to a key head over 8 to 155
+    // tokens 58 -> 28 us, 64 of one head over 1000 25 -> 15, 2 of 64 over 4000 35 -> 26.
+    const int64_t chunks = d->B * (d->table_row * d->page / kKeys + 1);
+    const bool little = chunks <= 8192 && chunks * d->kv_heads * cdiv(rows, kGroup) <= 8192;
+    p->wide = FORM == kBlocks || d->dtype != NOBLE_BF16 || rows <= 2 * kGroup || little ? 0 : rows > 128 ? 8 : 4;
+    p->R = p->wide ? 32 * p->wide / kGroup : FORM != kBlocks && rows > kGroup && !little ? 2 : 1;
     p->row_tiles = FORM == kBlocks ? d->new_tokens * cdiv(share, kGroup) : (rows + kGroup * p->R - 1) / (kGroup * p->R);
     // Workgroups that run at once: one a CU, by their LDS, or two of attn_wide_kernel's with four waves.  More of them in turn,
     // or smaller ones beside each other, read the cache more slowly: one token of 64 sequences of 16384 to 32768 tokens, 256

@@ -11,7 +11,7 @@ import _decoding as ref
 from _attention import U16, U32
 from paper_2603_06492_amd import attention as na
 from paper_2603_06492_amd import decoding as nd
-from test_decoding_gpu import BF, F32, Held, _gen, _ints, _near, _slopes, _trees
+from test_decoding_gpu import BF, F32, TREES, WEIGHS, Held, _gen, _ints, _near, _slopes, _trees
 
 pytestmark = pytest.mark.gpu
 
@@ -263,6 +263,43 @@ def test_rows_of_many_pieces(lengths, n, H, K, D, dt):
             _near("weights", w[b, :, :ww.shape[1]], ww, torch.zeros_like(ww), terms)
             want, mag, _, _ = ref.blocks(q[mine].cpu(), cache, table, length, chosen[mine])
             _near("blocks", s[mine], want, mag, u)
+
+
+def _roomy(h, n):
+    """Room for sequences so long that the calls take more than one group of 16 rows to a workgroup."""
+    tiles = -(-n * h.H // h.K // 16)
+    room = 8192 * 32 // (len(h.lengths) * h.K * tiles * h.page) + 1
+    h.table = torch.cat([h.table, torch.full((len(h.lengths), room), -1, dtype=torch.int32, device="cuda")], 1)
+    return h
+
+
+@pytest.mark.parametrize("case", [c for c in TREES if c[1] * c[2] > 16 * c[3]], ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}over{c[3]}")
+def test_trees_in_tables_with_room(case):
+    lengths, n, H, K, D, page, dt, cap, bias = case
+    h = _roomy(Held(lengths, H, K, D, page, dt, 3), n)
+    for b in range(1, len(lengths)):               # values that are no numbers, the last one seen by its own row alone
+        if lengths[b] > n:
+            h.cache[int(h.table[b, 0]), 1, 0, 1, 2] = math.inf
+            h.cache[int(h.table[b, (lengths[b] - 1) // page]), 1, K - 1, (lengths[b] - 1) % page, 3] = math.nan
+    q, parents, sl = h.q(n), _trees(random.Random(5), len(lengths), n), _slopes(H) if bias else None
+    seen, depths, _ = nd.noble_tree_rows(_ints(parents), h.len)
+    o = nd.noble_attn_tree(q, *h.args(), seen, depths, sl, softcap=cap)
+    for b, cache, table, length in h.each():
+        want, mag, _, _ = ref.tree(q[b * n:(b + 1) * n].cpu(), cache, table, length, parents[b], softcap=cap, slopes=sl)
+        _near(f"o of {b}", o[b * n:(b + 1) * n], want, mag, U16 if dt == BF else U32)
+
+
+@pytest.mark.parametrize("case", [c for c in WEIGHS if c[1] * c[2] > 16 * c[3]], ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}over{c[3]}")
+def test_weights_in_tables_with_room(case):
+    lengths, n, H, K, D, page, dt, cap, bias = case
+    h = _roomy(Held(lengths, H, K, D, page, dt, 31), n)
+    q, sl = h.q(n), _slopes(H) if bias else None
+    o, w = nd.noble_attn_weigh(q, *h.args(), None, sl, softcap=cap)
+    for b, cache, table, length in h.each():
+        want, mag, ww, size = ref.weigh(q[b * n:(b + 1) * n].cpu(), cache, table, length, softcap=cap, slopes=sl)
+        _near(f"o of {b}", o[b * n:(b + 1) * n], want, mag, U16 if dt == BF else U32)
+        u = (2 * (D + 3) * float(size.max() if size.numel() else 0) + 16 + n * H // K) * 2.0 ** -24   # see test_attn_weigh
+        _near(f"weights of {b}", w[b, :, :ww.shape[1]], ww, torch.zeros_like(ww), u)
 
 
 def test_rows_of_minus_infinity_and_large_scores():
