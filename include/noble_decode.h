@@ -162,7 +162,7 @@ typedef struct noble_evict_desc {
     int64_t B;
     int64_t row;          /* up to 2^31 - 4096 */
     int32_t heads;
-    int32_t keep;         /* >= 1 */
+    int32_t keep;         /* 1 to 2^31 - 4096 */
     int32_t sink, recent;
     int32_t reserved[2];  /* must be 0 */
 } noble_evict_desc;

@@ -467,7 +467,8 @@ noble_status noble_evict_select(const noble_evict_desc* desc, const float* weigh
     const noble_evict_desc& d = *desc;
     if (d.reserved[0] != 0 || d.reserved[1] != 0 || d.B < 0 || d.B > kMaxRows || d.row < 0 || d.row > kMaxRows || d.heads < 1 || d.heads > kMaxHeads)
         return NOBLE_ERR_BAD_SHAPE;
-    if (d.keep < 1 || d.sink < 0 || d.recent < 0 || d.sink > d.keep - d.recent) return NOBLE_ERR_BAD_SHAPE;
+    // the kernel counts places in 32 bits, 1024 beyond the last
+    if (d.keep < 1 || d.keep > kMaxRows || d.sink < 0 || d.recent < 0 || d.sink > d.keep - d.recent) return NOBLE_ERR_BAD_SHAPE;
     if (d.B * d.heads > kMaxGroups256 / 4) return NOBLE_ERR_BAD_SHAPE;
     NOBLE_TRY(need_array(weights, d.B > 0 && d.row > 0, 4));
     NOBLE_TRY(need_array(lengths, d.B > 0, 4));

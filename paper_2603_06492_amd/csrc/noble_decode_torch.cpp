@@ -270,7 +270,7 @@ PyObject* evict_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     d.row = t->size(2);
     const float* weights = c.floats(a[0], {d.B, d.heads, d.row});
     const int32_t* lengths = given(c, a[1], {d.B});
-    d.keep = (int32_t)c.integer(a[2], 1, INT32_MAX);
+    d.keep = (int32_t)c.integer(a[2], 1, INT32_MAX - 4095);
     d.sink = (int32_t)c.integer(a[3], 0, INT32_MAX);
     d.recent = (int32_t)c.integer(a[4], 0, INT32_MAX);
     const Output kept(c, a[5], {d.B, d.heads, d.keep}, at::kInt), kw(c, a[6], {d.B, d.heads, d.keep}, at::kFloat);

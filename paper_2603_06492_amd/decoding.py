@@ -357,6 +357,8 @@ def noble_evict_select(weights, lengths, keep: int, *, sink: int = 0, recent: in
         raise ValueError(f"weights must be [sequences, heads, tokens], got {tuple(weights.shape)}")
     B, H, row = weights.shape
     _whole(keep=keep, sink=sink, recent=recent)
+    if keep > 2 ** 31 - 4096:
+        raise ValueError(f"keep={keep}, 2 ** 31 - 4096 at most")
     d = noble_evict_desc(B, row, H, keep, sink, recent)
     args = [_tensor(weights, "weights", torch.float32, None, dev), _int32(lengths, "lengths", (B,), dev)]
     with _work(dev, stream) as (st, shared):
