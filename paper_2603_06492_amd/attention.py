@@ -547,7 +547,7 @@ class PagedCache:
         self._held = [0] * sequences
         self._seen = [0] * sequences   # tokens that the sequence has had, evicted ones among them
         self._free = list(range(pages - 1, -1, -1))
-        self._drafted = 0
+        self._drafted, self._parents = 0, None
 
     def _room(self, new: int):
         """Pages for ``new`` more tokens of every sequence, and their slots."""
@@ -593,7 +593,7 @@ class PagedCache:
             raise ValueError(f"parents must be [{len(self._held)} sequences, 1 to {decoding.TREE_MOST} nodes], got "
                              f"{tuple(parents.shape)}")
         slots = self._room(parents.shape[1])
-        self._drafted = parents.shape[1]
+        self._drafted, self._parents = parents.shape[1], parents.clone()
         seen, depths, positions = decoding.noble_tree_rows(parents, self.lengths)
         gone = [s - n for s, n in zip(self._seen, self._held)]
         if any(gone):
@@ -601,14 +601,18 @@ class PagedCache:
         return positions.view(-1), slots, (seen, depths)
 
     def accept(self, kept) -> None:
-        """Of the drafted tree only the nodes kept[b] (a list of ascending numbers for each sequence, from the root down)
-        stay in sequence b, one after the other; the pages of the others are given back."""
+        """Of the drafted tree only the nodes kept[b] stay in sequence b, one after the other; the pages of the others are
+        given back.  kept[b] is a branch: a list of node numbers whose first has the parent -1 and each other the one before it,
+        or empty.  Raises ValueError for any other list; nothing has changed then."""
         from . import decoding
         n = self._drafted
         if not n:
             raise RuntimeError("no draft is in the cache")
         if len(kept) != len(self._held) or any(x < 0 or x >= n or (i and x <= k[i - 1]) for k in kept for i, x in enumerate(k)):
             raise ValueError(f"kept must be {len(self._held)} lists of ascending numbers below {n}")
+        for b, (k, parents) in enumerate(zip(kept, self._parents.tolist())):
+            if any(parents[x] != above for above, x in zip([-1, *k], k)):   # its key stands at another place than it would have
+                raise ValueError(f"kept[{b}]={list(k)} is no branch of the tree with the parents {parents}")
         start = [h - n for h in self._held]
         table = torch.tensor([[list(k) + [-1] * (n - len(k))] for k in kept], dtype=torch.int32, device=self.lengths.device)
         first = torch.tensor(start, dtype=torch.int32, device=self.lengths.device)
@@ -617,7 +621,7 @@ class PagedCache:
         for w in self.weights or ():   # they have received nothing yet
             for b, k in enumerate(kept):
                 w[b, :, start[b]:start[b] + len(k)] = 0
-        self._drafted = 0
+        self._drafted, self._parents = 0, None
         self._seen = [s - n + len(k) for s, k in zip(self._seen, kept)]
         self._cut([s + len(k) for s, k in zip(start, kept)], n)
 
