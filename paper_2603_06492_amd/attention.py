@@ -530,8 +530,8 @@ class PagedCache:
     (``data[layer]`` is [pages, 2, kv_heads, page, head_dim]).  Which page belongs to which sequence is kept here.
 
     ``means``: also the means of every page's keys (``means[layer]``), by which ``NobleSelfAttention.step`` selects pages.
-    ``weights``: also the attention weight that every token has received (``weights[layer]``, float32 [sequences, kv_heads,
-    tokens]), by which ``evict`` goes."""
+    ``weights``: also the attention weight that every token has received from the tokens that were not drafted
+    (``weights[layer]``, float32 [sequences, kv_heads, tokens]), by which ``evict`` goes."""
 
     def __init__(self, sequences: int, longest: int, pages: int, *, kv_heads: int, head_dim: int, page: int = 16,
                  layers: int = 1, dtype=torch.bfloat16, device="cuda", means: bool = False, weights: bool = False):
@@ -745,7 +745,8 @@ class NobleSelfAttention(torch.nn.Module):
         ``tree``: the tokens are drafted ones, from ``cache.draft(parents)``, and see the nodes above them.  ``blocks``: each
         token and key head sees that many pages of its sequence, the first ``sink``, the last ``local`` and those whose means
         (of a cache with ``means``) its queries favour.  With a cache that keeps ``weights`` the weight that every token
-        receives is added up.  These go one at a time, and without a window."""
+        receives is added up, but for a tree's step, which adds none, its accepted nodes' rows neither: over such a cache
+        ``evict`` goes by the tokens of the other steps alone.  These go one at a time, and without a window."""
         from . import decoding
         self._fits(cache.seen)
         new = x.shape[0] // max(cache.lengths.shape[0], 1)
