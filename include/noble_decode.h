@@ -95,12 +95,14 @@ noble_status noble_page_means(const noble_paged_desc* desc, const void* cache,
 
 /* For the row of token t and each key head: block c is the c-th page of the
  * sequence, its score the product of its mean and the sum of the queries that
- * share the key head (in float64, so that it does not depend on an order).  Of
- * the blocks up to t's own the first `sink` and the last `local` are taken,
- * then those with the highest scores (of equal ones the first; NaN above all),
- * `count` in all.  chosen: int32 [B new_tokens, kv_heads, count], ascending,
- * -1 behind the last.  A block outside the cache has a score of minus
- * infinity.  count >= sink + local, local >= 1. */
+ * share the key head (float64 sums in one order for all blocks and calls: equal
+ * means have equal scores; scores no further apart than float64's rounding of
+ * such a sum may rank either way).  Of the blocks up to t's own the first `sink`
+ * and the last `local` are taken, then those with the highest scores (of equal
+ * ones the first; NaN above all), `count` in all.  chosen: int32
+ * [B new_tokens, kv_heads, count], ascending, -1 behind the last.  A block
+ * outside the cache has a score of minus infinity.  count >= sink + local,
+ * local >= 1. */
 typedef struct noble_select_desc {
     int32_t count;        /* 1 to 65536 */
     int32_t sink;

@@ -124,7 +124,7 @@ __device__ __forceinline__ uint16_t double_to_bf16(double x) {
 }
 
 // The mean of one page's keys of one head.  Eight elements a lane, D / 8 lanes a token, the workgroup's other lanes on other
-// tokens; float64 sums, so that the mean, rounded once, is the same in whatever order it is formed.
+// tokens; float64 sums in one order, by the head's size and the tokens held, and one rounding to the storage type.
 template <typename E>
 __global__ __launch_bounds__(256) void page_means_kernel(PageArgs a) {
     __shared__ double sums[256][9];
