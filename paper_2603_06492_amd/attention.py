@@ -531,7 +531,8 @@ class PagedCache:
 
     ``means``: also the means of every page's keys (``means[layer]``), by which ``NobleSelfAttention.step`` selects pages.
     ``weights``: also the attention weight that every token has received from the tokens that were not drafted
-    (``weights[layer]``, float32 [sequences, kv_heads, tokens]), by which ``evict`` goes."""
+    (``weights[layer]``, float32 [sequences, kv_heads, tokens]), by which ``evict`` goes.  A step over such a cache takes 4 bytes
+    of scratch for each new token, query head and token of ``longest``: long prompts go in in parts."""
 
     def __init__(self, sequences: int, longest: int, pages: int, *, kv_heads: int, head_dim: int, page: int = 16,
                  layers: int = 1, dtype=torch.bfloat16, device="cuda", means: bool = False, weights: bool = False):

@@ -5,6 +5,7 @@ import ctypes
 
 import pytest
 
+from paper_2603_06492_amd import attention as na
 from paper_2603_06492_amd import decoding as nd
 
 SHAPE = 2
@@ -32,3 +33,14 @@ def test_python_refuses_it_before_the_lists_are_made(monkeypatch):
     for keep in (MOST + 1, 2 ** 31 - 1, 2 ** 31):
         with pytest.raises(ValueError, match="keep"):
             nd.noble_evict_select(w, lengths, keep)
+
+
+@pytest.mark.parametrize("B,new,heads,tokens", [(8, 512, 32, 32768), (1, 1, 4, 1 << 20), (64, 1, 16, 32768), (3, 5, 8, 96)])
+def test_the_weights_scratch_goes_by_the_page_table(B, new, heads, tokens):
+    """Four bytes for each row, query head and token of the table, and little else."""
+    d = na.noble_paged_desc(B, tokens // 16, 100, 16, new, 0, heads, 4, 64, 0, 0.125, 0.0, 0)
+    n = ctypes.c_size_t(0)
+    assert nd.lib().noble_attn_weigh_scratch_size(ctypes.byref(d), ctypes.byref(n)) == 0
+    scores = B * new * heads * -(-tokens // 64) * 64 * 4
+    # maxima and sums of every row, and parts of 16 to 256 rows of 64 + 4 floats for up to some thousand workgroups
+    assert scores <= n.value <= scores + B * new * heads * 8 + 4096 * 256 * 68 * 4
