@@ -66,15 +66,16 @@ noble_status decode_plan(const noble_paged_desc* d, int64_t count, DecodePlan* p
     const int64_t share = d->heads / d->kv_heads, rows = d->new_tokens * share;
     // Little work, up to eight chunks for each wave of 256 workgroups of one group of rows, is latencies and code that runs once:
     // one group a workgroup, for all that the cache is read again.  47 trees of 8 with 8 heads to a key head over 8 to 155
-    // tokens 58 -> 28 us, 64 of one head over 1000 25 -> 15, 2 of 64 over 4000 35 -> 26.
+    // tokens 58 -> 28 us, 64 of one head over 1000 25 -> 16, 2 of 64 over 4000 35 -> 27.  It goes by the page table: in one
+    // for 4096 tokens the same 47 trees take 59.
     const int64_t chunks = d->B * (d->table_row * d->page / kKeys + 1);
     const bool little = chunks <= 8192 && chunks * d->kv_heads * cdiv(rows, kGroup) <= 8192;
     p->wide = FORM == kBlocks || d->dtype != NOBLE_BF16 || rows <= 2 * kGroup || little ? 0 : rows > 128 ? 8 : 4;
     p->R = p->wide ? 32 * p->wide / kGroup : FORM != kBlocks && rows > kGroup && !little ? 2 : 1;
     p->row_tiles = FORM == kBlocks ? d->new_tokens * cdiv(share, kGroup) : (rows + kGroup * p->R - 1) / (kGroup * p->R);
     // Workgroups that run at once: one a CU, by their LDS, or two of attn_wide_kernel's with four waves.  More of them in turn,
-    // or smaller ones beside each other, read the cache more slowly: one token of 64 sequences of 16384 to 32768 tokens, 256
-    // workgroups of four waves 0.60 ms, 1280 of one wave 0.68.
+    // or smaller ones beside each other, read the cache more slowly: one token of 64 sequences of 16384 to 32768 tokens with
+    // its weights, 256 workgroups of four waves 0.60 ms, 1280 of one wave 0.68.
     const int64_t resident = p->wide == 4 ? 512 : 256;
     const int64_t per = d->kv_heads * p->row_tiles;   // workgroups that read the same keys, or keys of other heads
     int64_t parts;
@@ -211,8 +212,8 @@ noble_status check_select(const noble_paged_desc* d, const noble_select_desc* s)
 constexpr int64_t kFewestBlocks = 256, kFewBlocks = 2048, kManyBlocks = 16384;
 
 // Few rows (times key heads) of many blocks each: workgroups of kScored blocks form their scores in a launch before the
-// selection's.  One row of 4 key heads of 128 over 512, 2048 and 16250 blocks 10.7 -> 9.6, 20 -> 11 and 118 -> 30 us; 32 rows
-// over 1023 16 -> 17, over 4092 49 -> 42.
+// selection's.  One row of 4 key heads of 128 over 512, 2048 and 16250 blocks 10.7 -> 9.7, 20 -> 12 and 118 -> 30 us; 32 rows
+// over 1023 16 and 16, over 4092 49 -> 42.
 bool scored_apart(const noble_paged_desc* d) {
     const int64_t rows = d->B * d->new_tokens * d->kv_heads;
     return d->table_row >= 512 && rows <= std::min<int64_t>(d->table_row / 16, 128) &&

@@ -8,10 +8,17 @@
 // MFMAs that share every operand read from LDS, so that a tree of eight tokens with four heads to a key head reads its cache
 // once; a workgroup goes through several sequences in turn; and chunks that every row sees, nearly all, run without masks.
 //
+// Probabilities are rounded to the storage type as the operand of their product with the values, so that bf16 values meet the
+// bf16 matrix instructions (large products 1250 TFLOP/s, float32's 155); their sums, and the weights of kWeigh, are of
+// unrounded ones.  Each is off by half a step, 2^-8 of itself, at most, and o with it by 2^-8 sum p |v|: over the performance
+// cases o lies 0.0020 to 0.0023 (norms) from 64 bits, where its own rounding to bf16 alone makes 0.0017.
+//
 // What bounds it: reading the cache, once.  16 sequences of 130 to 8192 tokens, 16 key heads of 128 (0.55 GB): one drafted
-// token 5.6 TB/s, 32 of them (R = 2) 4.6: the step of two groups is long enough that four waves a CU leave gaps.  One token
+// token 5.6 TB/s, 32 of them (R = 2) 4.7: the step of two groups is long enough that four waves a CU leave gaps.  One token
 // of 64 sequences of 16384 to 32768 tokens over 4 key heads (3.2 GB): 6.3 TB/s, and 5.4 with the scores of kWeigh stored,
 // 0.1 GB of writes among the reads that cost 95 us (in whatever layout, non-temporal or not, waited for or not).
+// float32, 8 sequences of 4096 to 8192 tokens, 32 drafted ones, 8 key heads of 128: 155 us for one query head to each (0.40 GB,
+// 2.6 TB/s), and 270 for two, whose 64 rows read the cache twice.
 #pragma once
 
 #include "noble_attn_common.hpp"
@@ -140,7 +147,7 @@ __device__ __forceinline__ uint32_t wave_upto(uint32_t v) {
 // different lengths keeps every workgroup busy to the end: a slot has the end of one sequence, whole ones, and the beginning
 // of one, at most.  Every wave works its range out for itself from the lengths.  16 sequences of 130 to 8192 tokens, 16 key
 // heads of 128, whole calls: 1024 workgroups over pieces of their own sequence each, 106 us for one new token and 113 for 16;
-// 256 workgroups over slots 101 and 107.
+// 256 workgroups over slots 100 and 106.
 struct Slots {
     int b = 0, begin = 0, steps = 0;   // the sequence, the slot's first step in it, the sequence's steps
     int left = 0;                      // steps of the slot from there on
@@ -605,7 +612,7 @@ __global__ __launch_bounds__((64 * DecodeShape<E, DP>::WAVES), (sizeof(E) * DP >
 
 // Joins the pieces of every row, in their order.  A row's DP / 4 lanes each take four elements; the pieces of rows with many are
 // dealt to SLICES sets of such lanes, whose sums meet in LDS in the sets' order (one token after 32768, 4 key heads, 64
-// pieces, the whole call: 28 us for one set, 21 for eight).  kWeigh: and keeps the rows' maxima and sums for weigh_kernel.
+// pieces, the whole call: 28 us for one set, 22 for eight).  kWeigh: and keeps the rows' maxima and sums for weigh_kernel.
 struct DecodeJoinArgs {
     DecodeArgs a;
     int64_t items;   // rows of all heads
@@ -693,7 +700,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeJoinArgs j) {
 
 // The weight that every token received: of the rows that see it, exp2(score - maximum) / sum, added in the rows' order.  A
 // thread takes four tokens that follow each other, and one of SLICES ranges of the rows, whose sums meet in LDS: 496 rows of
-// 388 tokens, 108 us with the attention for one range.
+// 388 tokens, 108 us with the attention for one range, 24 for sixteen.
 struct WeighArgs {
     DecodeArgs a;
     const float* in;   // [B, kv_heads, table_row page], nullptr: nothing

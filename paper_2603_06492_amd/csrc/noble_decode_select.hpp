@@ -367,8 +367,9 @@ struct EvictArgs {
 };
 
 // One workgroup a sequence and key head.  LDS holds the weights of up to N tokens; longer rows are read again each time.  Bound
-// by its passes over LDS and by additions to the same count: 256 rows of 4096 weights 10 us, of 32768 39 us, of which reading
-// them from memory is 6; of equal weights, whose counts all fall into one, 19 and 109.
+// by its passes over LDS and by additions to the same count: 256 rows of 4096 weights 10 us, of 32768 39 us, the same ones time
+// after time, and 44 for 16384 to 32768 beside the moves of their cache, which leave the weights in memory; of equal weights,
+// whose counts all fall into one, 19 and 109.
 template <int N>
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t keys[N];

@@ -5,13 +5,14 @@
 // 32x32x16 MFMAs, and all share tiles of 64 keys in LDS.  Here the keys come by the page table and from memory, not from a
 // cache that other workgroups have filled: three tiles are on their way while one is multiplied, in a ring of four that takes
 // a CU's LDS, and up to 256 rows share each.  Tiles that every row sees run without masks; the last ones, which hold the new
-// tokens, in a loop of their own.
+// tokens, in a loop of their own.  Probabilities are rounded to bf16 for their product with the values, as there.
 //
-// What bounds it: issue.  8 sequences of 16384 to 32768 tokens, 64 drafted tokens each, 16 heads of 128 over 4: 156 us, 0.66
-// PFLOP/s (0.40 GB, 2.6 TB/s); the matrix cores are busy for a third of the time, vector and scalar operations for half, and
-// waves of one workgroup, which pass the same barriers, do not fill each other's gaps as two workgroups would.  With four
-// waves and two stages, two workgroups a CU, which then read the cache twice, 188 us.  Up to 128 rows four waves and two
-// stages are faster: 16 drafted tokens 113 us, and 125 with one workgroup a CU and four stages.
+// What bounds it: issue.  8 sequences of 16384 to 32768 tokens, 64 drafted tokens each, 16 heads of 128 over 4: calls of 156
+// us, 0.66 PFLOP/s (0.40 GB, 2.6 TB/s; the kernel, traced, 165 us in the first twenty calls and 150 after a hundred); the
+// matrix cores are busy for a third of the time, vector and scalar operations for half, and waves of one workgroup, which
+// pass the same barriers, do not fill each other's gaps as two workgroups would.  With four waves and two stages, two
+// workgroups a CU, which then read the cache twice, 188 us.  Up to 128 rows four waves and two stages are faster: 16 drafted
+// tokens 113 us, and 125 with one workgroup a CU and four stages.
 #pragma once
 
 #include "noble_attn_tile.hpp"
