@@ -11,7 +11,7 @@
 // Probabilities are rounded to the storage type as the operand of their product with the values, so that bf16 values meet the
 // bf16 matrix instructions (large products 1250 TFLOP/s, float32's 155); their sums, and the weights of kWeigh, are of
 // unrounded ones.  Each is off by half a step, 2^-8 of itself, at most, and o with it by 2^-8 sum p |v|: over the performance
-// cases o lies 0.0020 to 0.0023 (norms) from 64 bits, where its own rounding to bf16 alone makes 0.0017.
+// cases o lies 0.0020 to 0.0024 (norms) from 64 bits, where its own rounding to bf16 alone makes 0.0017.
 //
 // What bounds it: reading the cache, once.  16 sequences of 130 to 8192 tokens, 16 key heads of 128 (0.55 GB): one drafted
 // token 5.6 TB/s, 32 of them (R = 2) 4.7: the step of two groups is long enough that four waves a CU leave gaps.  One token
